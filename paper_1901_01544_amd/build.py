@@ -1,4 +1,4 @@
-"""Build step: the HIP library (one hipcc invocation, gfx950 only) and the Python module that calls into it.
+"""Build step: the HIP library (one hipcc invocation a source, gfx950 only) and the Python module that calls into it.
 
     python -m paper_1901_01544_amd.build
 
@@ -13,7 +13,7 @@ import sys
 import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = os.path.join(HERE, "csrc", "iwp_api.hip")
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("iwp_api.hip", "iwp_losses.hip")]
 LIB = os.path.join(HERE, "libiwp.so")
 CALL_SRC = os.path.join(HERE, "csrc", "call.cpp")
 # named after the interpreter's version, so that another one fails to import it instead of loading it
@@ -25,7 +25,6 @@ HIPCC_FLAGS = [
     "-O3",
     "-std=c++17",
     "-fPIC",
-    "-shared",
     # IEEE binary32 as the method is defined: no contraction, no fast-math,
     # denormals kept, correctly rounded divide.
     "-ffp-contract=off",
@@ -49,11 +48,26 @@ def build(verbose: bool = False, extra_flags=(), out: str = LIB) -> str:
     """Compile csrc/ into libiwp.so (always recompiles); returns the path.
     extra_flags / out: build a tuning variant (e.g. -DIWP_LGROUP=4) somewhere else."""
     tmp = out + ".tmp.%d" % os.getpid()
-    cmd = [hipcc(), *HIPCC_FLAGS, *extra_flags, "-o", tmp, SRC]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
-    os.replace(tmp, out)
+    objects = ["%s.%d.o" % (tmp, i) for i in range(len(SOURCES))]
+    try:
+        running = []
+        for source, obj in zip(SOURCES, objects):
+            cmd = [hipcc(), *HIPCC_FLAGS, *extra_flags, "-c", "-o", obj, source]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            running.append((cmd, subprocess.Popen(cmd)))
+        for cmd, p in running:
+            if p.wait() != 0:
+                raise subprocess.CalledProcessError(p.returncode, cmd)
+        cmd = [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objects]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.check_call(cmd)
+        os.replace(tmp, out)
+    finally:
+        for obj in objects:
+            if os.path.exists(obj):
+                os.remove(obj)
     return out
 
 

@@ -1,5 +1,6 @@
-// The Python binding's way into the library: arguments of the hot calls -> the C functions of include/iwp.h.  Argument
-// marshalling only; the library itself is opened by iwp.py, which hands over its functions' addresses (bind).
+// The Python binding's way into the library: arguments of the hot calls -> the C functions of include/iwp.h and
+// include/iwp_losses.h.  Argument marshalling only; the library itself is opened by iwp.py, which hands over its functions'
+// addresses (bind, bind_losses).
 //
 // Bound by the host: a call is a few launches of 3 us each, and through ctypes the arguments of one took 4 to 8 us (0.4 us per
 // tensor for its three checks, 0.9 us per table of workers, 1.1 us for the call).  A small exchange (two calls, one launch
@@ -15,6 +16,7 @@
 #include <utility>
 
 #include "../../include/iwp.h"
+#include "../../include/iwp_losses.h"
 
 namespace {
 
@@ -96,6 +98,11 @@ template <> struct Arg<uint64_t> {
     bool from(PyObject* o) { return unsigned_from(o, &x); }
     uint64_t get() { return x; }
 };
+template <> struct Arg<int64_t> {
+    uint64_t x = 0;
+    bool from(PyObject* o) { return unsigned_from(o, &x); }
+    int64_t get() { return (int64_t)x; }
+};
 template <> struct Arg<float> {
     double x = 0;
     bool from(PyObject* o) { x = PyFloat_AsDouble(o); return x != -1.0 || !PyErr_Occurred(); }
@@ -132,17 +139,18 @@ PyObject* call(const char* name, int (*f)(A...), PyObject* const* args, Py_ssize
     DO(compact_pairs_segmented) DO(iwp_step_threshold_segmented) DO(iwp_step_threshold_random_segmented)          \
     DO(iwp_step_layerwise_segmented)
 
+#define EACH_LOSS_CALL(DO) DO(iwp_head_cross_entropy) DO(iwp_head_distill) DO(iwp_balance)
+
 #define DO(name)                                                                    \
     decltype(&::name) f_##name = nullptr;                                           \
     PyObject* py_##name(PyObject*, PyObject* const* args, Py_ssize_t n) {           \
         return call(#name, f_##name, args, n);                                      \
     }
 EACH_HOT_CALL(DO)
+EACH_LOSS_CALL(DO)
 #undef DO
 
-// bind({name: address}): where the loaded library's functions are.
-PyObject* bind(PyObject*, PyObject* addresses) {
-    if (!PyDict_Check(addresses)) return PyErr_Format(PyExc_TypeError, "a dict of addresses");
+// bind({name: address}), bind_losses({name: address}): where the loaded library's functions are.
 #define DO(name)                                                                                              \
     {                                                                                                         \
         PyObject* o = PyDict_GetItemString(addresses, #name);                                                 \
@@ -151,30 +159,45 @@ PyObject* bind(PyObject*, PyObject* addresses) {
         if (PyErr_Occurred()) return nullptr;                                                                 \
         f_##name = reinterpret_cast<decltype(&::name)>(at);                                                   \
     }
+PyObject* bind(PyObject*, PyObject* addresses) {
+    if (!PyDict_Check(addresses)) return PyErr_Format(PyExc_TypeError, "a dict of addresses");
     EACH_HOT_CALL(DO)
-#undef DO
     Py_RETURN_NONE;
 }
+PyObject* bind_losses(PyObject*, PyObject* addresses) {
+    if (!PyDict_Check(addresses)) return PyErr_Format(PyExc_TypeError, "a dict of addresses");
+    EACH_LOSS_CALL(DO)
+    Py_RETURN_NONE;
+}
+#undef DO
 
-PyObject* names(PyObject*, PyObject*) {
-    PyObject* out = PyList_New(0);
 #define DO(name)                                                   \
     if (out) {                                                     \
         PyObject* s = PyUnicode_FromString(#name);                 \
         if (!s || PyList_Append(out, s)) { Py_CLEAR(out); }        \
         Py_XDECREF(s);                                             \
     }
+PyObject* names(PyObject*, PyObject*) {
+    PyObject* out = PyList_New(0);
     EACH_HOT_CALL(DO)
-#undef DO
     return out;
 }
+PyObject* loss_names(PyObject*, PyObject*) {
+    PyObject* out = PyList_New(0);
+    EACH_LOSS_CALL(DO)
+    return out;
+}
+#undef DO
 
 PyMethodDef methods[] = {
 #define DO(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr},
     EACH_HOT_CALL(DO)
+    EACH_LOSS_CALL(DO)
 #undef DO
     {"bind", bind, METH_O, nullptr},
+    {"bind_losses", bind_losses, METH_O, nullptr},
     {"names", names, METH_NOARGS, nullptr},
+    {"loss_names", loss_names, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

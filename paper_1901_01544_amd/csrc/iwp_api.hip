@@ -14,6 +14,7 @@
 
 #include "iwp_common.hpp"
 #include "iwp_exchange.hpp"
+#include "iwp_host.hpp"
 #include "iwp_select.hpp"
 #include "iwp_small.hpp"
 #include "iwp_stream.hpp"
@@ -26,17 +27,6 @@ namespace {
 
 thread_local char g_hip_error[256] = "";
 
-int hip_fail(hipError_t e, const char* what) {
-    snprintf(g_hip_error, sizeof g_hip_error, "%s: %s", what, hipGetErrorString(e));
-    return IWP_EHIP;
-}
-
-#define IWP_HIP(call)                                         \
-    do {                                                      \
-        hipError_t e_ = (call);                               \
-        if (e_ != hipSuccess) return hip_fail(e_, #call);     \
-    } while (0)
-
 // Optional timing of one named kernel with HIP events on the stream it is launched
 // on (iwp_timing_*): off by default, costs one string compare per launch when on.
 struct Timing {
@@ -47,34 +37,28 @@ struct Timing {
     int used = 0;
 } g_timing;
 
-struct TimedLaunch {       // records an event pair around the launch made while it is alive
-    hipStream_t s;
-    int slot = -1;
-    TimedLaunch(const char* kernel, hipStream_t stream) : s(stream) {
-        if (!g_timing.enabled || strcmp(kernel, g_timing.name) != 0) return;
-        if (g_timing.used >= (int)g_timing.start.size()) return;
-        slot = g_timing.used++;
-        (void)hipEventRecord(g_timing.start[slot], s);
-    }
-    ~TimedLaunch() {
-        if (slot >= 0) (void)hipEventRecord(g_timing.stop[slot], s);
-    }
-};
+}  // namespace
 
-// Launch `kernel<<<grid, BLOCK, lds, s>>>(args...)`, timed if asked for, and turn a
-// launch failure into IWP_EHIP.  lds: bytes of LDS that no one uses, see few_at_a_time().
-#define IWP_LAUNCH(name, kernel, grid, s, ...) IWP_LAUNCH_AS(name, kernel, grid, BLOCK, 0u, s, __VA_ARGS__)
-#define IWP_LAUNCH_BLOCK(name, kernel, grid, block, s, ...) IWP_LAUNCH_AS(name, kernel, grid, block, 0u, s, __VA_ARGS__)
-#define IWP_LAUNCH_FEW(name, kernel, grid, lds, s, ...) IWP_LAUNCH_AS(name, kernel, grid, BLOCK, lds, s, __VA_ARGS__)
-#define IWP_LAUNCH_AS(name, kernel, grid, block, lds, s, ...)         \
-    do {                                                              \
-        {                                                             \
-            TimedLaunch tl_(name, s);                                 \
-            kernel<<<(grid), (block), (lds), (s)>>>(__VA_ARGS__);     \
-        }                                                             \
-        hipError_t e_ = hipGetLastError();                            \
-        if (e_ != hipSuccess) return hip_fail(e_, name);              \
-    } while (0)
+namespace iwp {
+
+int hip_fail(hipError_t e, const char* what) {
+    snprintf(g_hip_error, sizeof g_hip_error, "%s: %s", what, hipGetErrorString(e));
+    return IWP_EHIP;
+}
+
+TimedLaunch::TimedLaunch(const char* kernel, hipStream_t stream) : s(stream) {
+    if (!g_timing.enabled || strcmp(kernel, g_timing.name) != 0) return;
+    if (g_timing.used >= (int)g_timing.start.size()) return;
+    slot = g_timing.used++;
+    (void)hipEventRecord(g_timing.start[slot], s);
+}
+TimedLaunch::~TimedLaunch() {
+    if (slot >= 0) (void)hipEventRecord(g_timing.stop[slot], s);
+}
+
+}  // namespace iwp
+
+namespace {
 
 // Scratch of compress_segmented_static: device memory that belongs to the library, one copy per
 // GPU, held until the process ends.  In host code the array's name is only a handle for

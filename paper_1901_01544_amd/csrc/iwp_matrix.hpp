@@ -1,0 +1,206 @@
+// Matrix products on 16-bit operands (bf16, fp16) with binary32 sums, tiled for gfx950's matrix cores.  One tile loop for
+// every product of the head kernels; what differs is which way an operand lies in memory:
+//   rows of K     the summed index is contiguous; a lane's fragment is one 128-bit LDS read
+//   columns of K  the other index is contiguous; a lane's fragment is two transposing 64-bit LDS reads
+// The tile of P is the matrix instruction's first operand, that of Q its second, so a lane ends up with four consecutive
+// entries of P for one entry of Q: P is the index that is contiguous in the product, Q its row.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace iwp {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+struct Bf16 {
+    typedef __bf16 scalar;
+    static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint16_t bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+    static __device__ __forceinline__ float value(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+};
+struct F16 {
+    typedef _Float16 scalar;
+    static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint16_t bits(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
+    static __device__ __forceinline__ float value(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }
+};
+
+constexpr uint32_t BK = 64;                        // summed entries per LDS tile: 128 bytes of a row
+
+// An operand as the tile loop reads it.  Binary32 operands come as two planes of fp16 (see split_f32): `lo` is null for
+// operands of 16 bits.
+struct Operand {
+    const uint16_t* hi;
+    const uint16_t* lo;
+    uint32_t ld;           // elements from row to row; ld * 512 bytes stay below 2^32
+    uint32_t extent;       // valid entries of the index that is not summed
+    uint32_t summed;       // valid entries of the summed one
+};
+
+__device__ __forceinline__ void load_to_lds(const void* from, void* to) {     // 16 bytes per lane, `to` uniform
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// One operand's tile: R entries of its own index, BK of the summed one, WAVES wavefronts loading.
+//
+// Rows of K: LDS row r holds the 8 chunks (16 bytes) of entry r, chunk c at place c ^ turn(r).
+// Columns of K: LDS row k holds R entries, in pairs of chunks of 64 bytes, pair p at place p ^ turn.
+// Both turns spread what one LDS access reads over the banks.  The loads go straight to LDS, lane by lane in address order, so
+// it is the address in global memory that is turned.
+//
+// Entries past the operand's extent are read from a valid one: what they contribute to is never stored.  Summed entries past
+// an operand's end are read from the same row, or from its last row; of the two operands one always reaches to a multiple of BK
+// and holds zeros there.
+template <int R, int WAVES, bool COLUMNS>
+struct Tile {
+    static constexpr int BYTES = R * BK * 2;
+    static constexpr int LOADS = BYTES / 1024 / WAVES;      // 64 lanes of 16 bytes each
+    static_assert(LOADS * WAVES * 1024 == BYTES, "whole loads");
+    static constexpr int PER_ROW = COLUMNS ? R / 8 : BK / 8;
+    static constexpr int TURNS = COLUMNS ? (R / 32 < 8 ? R / 32 : 8) : 8;
+
+    uint32_t at[LOADS];        // byte offset of this lane's chunk in the tile at summed index 0
+    uint32_t within[LOADS];    // rows of K: the chunk's first summed index; columns of K: its summed index
+    uint32_t row_bytes;
+
+    static __device__ __forceinline__ uint32_t turn(uint32_t r) {
+        if (!COLUMNS) return (r >> 1) & 7u;
+        return ((r & 3u) | ((r >> 1) & 4u)) & (TURNS - 1);
+    }
+    __device__ __forceinline__ void init(const Operand& o, uint32_t first, int wave, int lane) {
+        row_bytes = o.ld * 2;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t slot = (wave * LOADS + i) * 64 + lane, row = slot / PER_ROW, place = slot % PER_ROW;
+            if (!COLUMNS) {
+                const uint32_t entry = min(first + row, o.extent - 1) - first, chunk = place ^ turn(row);
+                within[i] = chunk * 8;
+                at[i] = entry * row_bytes + chunk * 16;
+            } else {
+                const uint32_t chunk = (((place >> 2) ^ turn(row)) << 2) | (place & 3u);
+                const uint32_t entry = first + chunk * 8 < o.extent ? chunk * 8 : 0u;
+                within[i] = row;
+                at[i] = entry * 2;
+            }
+        }
+    }
+    // plane + first entry, as bytes: where the tile's entry 0 at summed index k lies
+    static __device__ __forceinline__ const char* origin(const uint16_t* plane, const Operand& o, uint32_t first, uint32_t k) {
+        return reinterpret_cast<const char*>(plane) + (COLUMNS ? ((size_t)k * o.ld + first) * 2 : ((size_t)first * o.ld + k) * 2);
+    }
+    // left: summed entries from k on (at least 1)
+    __device__ __forceinline__ void load(const char* from, uint32_t left, char* lds, int wave) const {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            uint32_t off;
+            if (!COLUMNS) off = within[i] < left ? at[i] : at[i] - within[i] * 2;
+            else off = at[i] + min(within[i], left - 1) * row_bytes;
+            load_to_lds(from + off, lds + (wave * LOADS + i) * 1024);
+        }
+    }
+    // Fragment of the 32 entries from `entry` (a multiple of 32) on, summed indices 16 s to 16 s + 15 of the tile.
+    static __device__ __forceinline__ s16x8 fragment(const char* lds, uint32_t entry, int s, int lane) {
+        if (!COLUMNS) {
+            const uint32_t row = entry + (lane & 31), chunk = 2 * s + (lane >> 5);
+            return *reinterpret_cast<const s16x8*>(lds + row * (BK * 2) + ((chunk ^ turn(row)) << 4));
+        }
+        const uint32_t i = lane & 15, half = lane >> 5;
+        const uint32_t k = 16 * s + 8 * half + (i >> 2);
+        const char* p = lds + k * (R * 2) + (((entry >> 5) ^ turn(k)) << 6) + ((lane >> 4) & 1) * 32 + (i & 3) * 8;
+        typedef __attribute__((address_space(3))) s16x4* lds_quad;
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quad)p);
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quad)(p + 4 * R * 2));
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+
+// The product of a BP x BQ tile: WP x WQ wavefronts, each BP / WP entries of P by BQ / WQ of Q.
+template <class E, int BP, int BQ, int WP, int WQ, bool P_COLUMNS, bool Q_COLUMNS>
+struct Product {
+    static constexpr int WAVES = WP * WQ, THREADS = WAVES * 64;
+    static constexpr int FP = BP / WP / 32, FQ = BQ / WQ / 32;     // fragments of 32 per wavefront
+    typedef Tile<BP, WAVES, P_COLUMNS> TP;
+    typedef Tile<BQ, WAVES, Q_COLUMNS> TQ;
+    static constexpr int STAGE = TP::BYTES + TQ::BYTES, LDS = 2 * STAGE;
+
+    f32x16 acc[FP][FQ];
+
+    // entries of P and Q of this wavefront inside the tile, and of register r of a fragment inside it
+    static __device__ __forceinline__ uint32_t p_of(int wave) { return (wave % WP) * (BP / WP); }
+    static __device__ __forceinline__ uint32_t q_of(int wave) { return (wave / WP) * (BQ / WQ); }
+
+    // Sum over summed indices [k_from, k_to), a multiple of BK, of P[p0 ..][k] Q[q0 ..][k].  Operands of two planes x = hi + 2^-11 lo (scaled, see
+    // split_f32) take three passes, lo hi + hi lo first, then times 2^-11, then hi hi; lo lo lies below binary32.
+    __device__ __forceinline__ void run(const Operand& P, const Operand& Q, uint32_t p0, uint32_t q0, uint32_t k_from,
+                                        uint32_t k_to, char* lds) {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int a = 0; a < FP; ++a)
+#pragma unroll
+            for (int b = 0; b < FQ; ++b) acc[a][b] = f32x16{};
+        if (k_from >= k_to) return;
+        TP tp;
+        TQ tq;
+        tp.init(P, p0, wave, lane);
+        tq.init(Q, q0, wave, lane);
+        const uint32_t steps = (k_to - k_from) / BK, passes = P.lo ? 3 : 1, total = steps * passes;
+        const uint32_t pw = p_of(wave), qw = q_of(wave);
+        const size_t p_step = (P_COLUMNS ? (size_t)P.ld * BK : BK) * 2, q_step = (Q_COLUMNS ? (size_t)Q.ld * BK : BK) * 2;
+        const char *pf = nullptr, *qf = nullptr;
+        uint32_t step = 0, pass = 0;                                   // of the next tile to be loaded
+        auto request = [&](int stage) {
+            if (step == 0) {
+                pf = TP::origin(passes == 3 && pass == 0 ? P.lo : P.hi, P, p0, k_from);
+                qf = TQ::origin(passes == 3 && pass == 1 ? Q.lo : Q.hi, Q, q0, k_from);
+            }
+            const uint32_t k = k_from + step * BK;
+            tp.load(pf, P.summed - k, lds + stage * STAGE, wave);
+            tq.load(qf, Q.summed - k, lds + stage * STAGE + TP::BYTES, wave);
+            pf += p_step;
+            qf += q_step;
+            if (++step == steps) step = 0, ++pass;
+        };
+        request(0);
+        for (uint32_t t = 0; t < total; ++t) {
+            __syncthreads();                                           // tile t has arrived, tile t - 1 is done with
+            if (t + 1 < total) request((t + 1) & 1);
+            if (passes == 3 && t == 2 * steps) {
+#pragma unroll
+                for (int a = 0; a < FP; ++a)
+#pragma unroll
+                    for (int b = 0; b < FQ; ++b) acc[a][b] *= 0x1p-11f;
+            }
+            const char* lp = lds + (t & 1) * STAGE;
+            const char* lq = lp + TP::BYTES;
+#pragma unroll
+            for (int s = 0; s < (int)BK / 16; ++s) {
+                s16x8 fp[FP], fq[FQ];
+#pragma unroll
+                for (int a = 0; a < FP; ++a) fp[a] = TP::fragment(lp, pw + a * 32, s, lane);
+#pragma unroll
+                for (int b = 0; b < FQ; ++b) fq[b] = TQ::fragment(lq, qw + b * 32, s, lane);
+#pragma unroll
+                for (int a = 0; a < FP; ++a)
+#pragma unroll
+                    for (int b = 0; b < FQ; ++b) acc[a][b] = E::mfma(fp[a], fq[b], acc[a][b]);
+            }
+        }
+        __syncthreads();                                               // the LDS is free for what follows
+    }
+};
+
+// Register r of a fragment: entry of P inside the fragment's 32 (the entry of Q is lane & 31).
+__device__ __forceinline__ uint32_t p_in_fragment(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+
+}  // namespace iwp

@@ -56,6 +56,7 @@ def load() -> C.CDLL:
                                 "`python -m paper_1901_01544_amd.build`" % e) from e
     L = C.CDLL(LIB_PATH)
     call.bind({name: C.cast(getattr(L, name), _vp).value for name in call.names()})
+    call.bind_losses({name: C.cast(getattr(L, name), _vp).value for name in call.loss_names()})
     # prototypes of every call, also of those that go through _call: for callers that use the library by ctypes
     L.iwp_workspace_bytes.argtypes = [C.c_uint32, C.c_uint32]
     L.iwp_workspace_bytes.restype = C.c_size_t
@@ -108,6 +109,10 @@ def load() -> C.CDLL:
     L.iwp_timing_enable.restype = C.c_int
     L.iwp_timing_collect.argtypes = [C.POINTER(C.c_double), C.POINTER(C.c_uint32)]
     L.iwp_timing_collect.restype = C.c_int
+    L.iwp_head_workspace_bytes.argtypes = [C.c_uint32] * 4 + [_vp, C.c_int64, C.c_uint32, C.c_uint32]
+    L.iwp_head_workspace_bytes.restype = C.c_size_t
+    L.iwp_balance_workspace_bytes.argtypes = [C.c_uint32, C.c_uint32]
+    L.iwp_balance_workspace_bytes.restype = C.c_size_t
     L.iwp_strerror.argtypes = [C.c_int]
     L.iwp_strerror.restype = C.c_char_p
     L.iwp_last_hip_error.argtypes = []
