@@ -354,28 +354,40 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_logits(Operand W, Operand
             g = row_gradient(R, q, S->most, t, SOFT);
         }
         if (MODE == STATISTICS) continue;
+        typedef Rows32<2> Out;
+        static_assert(BP / WP == Out::ENTRIES && M::WAVES * Out::BYTES <= M::LDS, "a wavefront's rows");
+        char* mine = lds + wave * Out::BYTES;
+        constexpr bool TWO = MODE == GRADIENT ? F32 : WIDE;
+        uint64_t hi[M::FP][4], lo[M::FP][4];
 #pragma unroll
         for (int a = 0; a < M::FP; ++a)
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                uint64_t hi = 0, lo = 0;
+                hi[a][c] = lo[a][c] = 0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     uint16_t x = 0, y = 0;
                     const uint32_t p = p0 + a * 32 + p_in_fragment(c * 4 + e, lane);
                     const float z = mm.acc[a][b][c * 4 + e];
                     if (MODE == GRADIENT) {
-                        if (row_in && p < G.n) put_dz<E, F32>(SOFT ? g.softmaxes(z) : g.c1 * exp_of(z - g.lse), &x, &y);
+                        const float d = SOFT ? g.softmaxes(z) : g.c1 * exp_of(z - g.lse);
+                        put_dz<E, F32>(row_in && p < G.n ? d : 0.0f, &x, &y);
                     } else {
                         keep_logit<WIDE>(z, m, &x, &y);
                     }
-                    hi |= (uint64_t)x << (16 * e);
-                    lo |= (uint64_t)y << (16 * e);
+                    hi[a][c] |= (uint64_t)x << (16 * e);
+                    lo[a][c] |= (uint64_t)y << (16 * e);
                 }
-                const size_t at = (size_t)q * G.ld + p0 + a * 32 + p_in_fragment(c * 4, lane);
-                *reinterpret_cast<uint64_t*>(G.hi + at) = hi;
-                if (MODE == GRADIENT ? F32 : WIDE) *reinterpret_cast<uint64_t*>(G.lo + at) = lo;
             }
+#pragma unroll
+        for (int plane = 0; plane < (TWO ? 2 : 1); ++plane) {
+#pragma unroll
+            for (int a = 0; a < M::FP; ++a)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) Out::put(mine, a * 32 + p_in_fragment(c * 4, lane), lane, plane ? &lo[a][c] : &hi[a][c]);
+            uint16_t* to = (plane ? G.lo : G.hi) + (size_t)(q0 + b * 32) * G.ld + p0;
+            Out::each(mine, lane, [&](uint32_t row, uint32_t p, uint4 v) { *reinterpret_cast<uint4*>(to + (size_t)row * G.ld + p) = v; });
+        }
     }
 }
 
@@ -575,10 +587,10 @@ __global__ void __launch_bounds__(256) k_head_dh_out(const float* __restrict__ s
     }
 }
 
-// dW of a piece: rows of the vocabulary, summed over the rows of tokens.
+// dW of a piece: rows of the vocabulary, summed over the rows of tokens.  wide_rows: every row of dw is 4-byte aligned.
 template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool F32>
 __global__ void __launch_bounds__(WP * WQ * 64) k_head_dw(Operand H, Operand G, float scale, void* __restrict__ dw, int64_t ld_dw,
-                                                          uint32_t first, uint32_t dim, const HeadScalars* __restrict__ S) {
+                                                          bool wide_rows, uint32_t first, uint32_t dim, const HeadScalars* __restrict__ S) {
     typedef Product<E, BP, BQ, WP, WQ, true, true> M;
     __shared__ __align__(1024) char lds[M::LDS];
     const uint32_t count = S->count, n = G.extent;
@@ -591,17 +603,43 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_dw(Operand H, Operand G, 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t p0 = tp * BP + M::p_of(wave), q0 = tq * BQ + M::q_of(wave);
     const float factor = scale * S->most * (1.0f / DZ_SCALE), s = F32 ? 1.0f / split_scale(S->h_max) : 1.0f;
+    typedef Rows32<OUT == OUT_F32 ? 4 : 2> Out;
+    static_assert(BP / WP == Out::ENTRIES && M::WAVES * Out::BYTES <= M::LDS, "a wavefront's rows");
+    char* mine = lds + wave * Out::BYTES;
+    constexpr uint32_t SIZE = OUT == OUT_F32 ? 4 : 2;
 #pragma unroll
     for (int b = 0; b < M::FQ; ++b) {
-        const uint32_t q = q0 + b * 32 + (lane & 31);
-        if (q >= n) continue;
 #pragma unroll
         for (int a = 0; a < M::FP; ++a)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const uint32_t p = p0 + a * 32 + p_in_fragment(r, lane);
-                if (p < dim) put<OUT>(dw, (int64_t)(first + q) * ld_dw + p, mm.acc[a][b][r] * s * factor);
+            for (int c = 0; c < 4; ++c) {
+                f32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = mm.acc[a][b][c * 4 + e] * s * factor;
+                uint64_t four = 0;
+                if (OUT != OUT_F32)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) four |= (uint64_t)(OUT == OUT_BF16 ? Bf16::bits(v[e]) : F16::bits(v[e])) << (16 * e);
+                Out::put(mine, a * 32 + p_in_fragment(c * 4, lane), lane, OUT == OUT_F32 ? (const void*)&v : (const void*)&four);
             }
+        // 128-bit stores need no more than 4-byte alignment
+        Out::each(mine, lane, [&](uint32_t row, uint32_t p, uint4 v) {
+            const uint32_t q = q0 + b * 32 + row;
+            if (q >= n || p0 + p >= dim) return;
+            char* to = static_cast<char*>(dw) + ((int64_t)(first + q) * ld_dw + p0 + p) * SIZE;
+            if (p0 + p + Out::PER_CHUNK <= dim && (OUT == OUT_F32 || wide_rows)) {
+                typedef uint32_t quad_any __attribute__((ext_vector_type(4), aligned(4)));
+                *reinterpret_cast<quad_any*>(to) = quad_any{v.x, v.y, v.z, v.w};
+            } else {
+                const uint32_t word[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < Out::PER_CHUNK; ++e)
+                    if (p0 + p + e < dim) {
+                        if (OUT == OUT_F32) reinterpret_cast<uint32_t*>(to)[e] = word[e];
+                        else reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(word[e / 2] >> (16 * (e & 1)));
+                    }
+            }
+        });
     }
 }
 

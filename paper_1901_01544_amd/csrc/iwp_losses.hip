@@ -144,7 +144,8 @@ template <class K, class T, int OUT>
 int launch_dw(const HeadPlan& p, const HeadCall& c, const Operand& H, const Operand& G, uint32_t first) {
     const uint32_t tiles = (p.dim + T::BP - 1) / T::BP * ((G.extent + T::BQ - 1) / T::BQ);
     auto kernel = k_head_dw<typename K::E, T::BP, T::BQ, T::WP, T::WQ, OUT, K::F32>;
-    IWP_LAUNCH_BLOCK("k_head_dw", kernel, tiles, T::THREADS, c.s, H, G, c.scale, c.dw, c.ld_dw, first, p.dim, p.scalars);
+    IWP_LAUNCH_BLOCK("k_head_dw", kernel, tiles, T::THREADS, c.s, H, G, c.scale, c.dw, c.ld_dw,
+                     aligned(c.dw, 4) && c.ld_dw % 2 == 0, first, p.dim, p.scalars);
     return IWP_OK;
 }
 

@@ -47,9 +47,22 @@ struct Operand {
     uint32_t summed;       // valid entries of the summed one
 };
 
-__device__ __forceinline__ void load_to_lds(const void* from, void* to) {     // 16 bytes per lane, `to` uniform
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+// 16 bytes per lane from `base` + the lane's offset straight to LDS, lane after lane from `lds` (uniform) on.  In assembly,
+// because the compiler waits for such loads before any transposing read, of whichever tile; wait_for_loads() waits for them.
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory", "m0");
+}
+// Until at most LEFT of this wavefront's loads are on their way and all of its LDS reads are done.
+template <int LEFT>
+__device__ __forceinline__ void wait_for_loads() {
+    static_assert(LEFT < 16, "fits the counter's low bits");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
+}
+__device__ __forceinline__ void workgroup_barrier() {
+    asm volatile("s_barrier" ::: "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
 }
 
 // One operand's tile: R entries of its own index, BK of the summed one, WAVES wavefronts loading.
@@ -100,13 +113,13 @@ struct Tile {
         return reinterpret_cast<const char*>(plane) + (COLUMNS ? ((size_t)k * o.ld + first) * 2 : ((size_t)first * o.ld + k) * 2);
     }
     // left: summed entries from k on (at least 1)
-    __device__ __forceinline__ void load(const char* from, uint32_t left, char* lds, int wave) const {
+    __device__ __forceinline__ void load(const char* from, uint32_t left, uint32_t lds, int wave) const {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             uint32_t off;
             if (!COLUMNS) off = within[i] < left ? at[i] : at[i] - within[i] * 2;
             else off = at[i] + min(within[i], left - 1) * row_bytes;
-            load_to_lds(from + off, lds + (wave * LOADS + i) * 1024);
+            load_to_lds(from, off, lds + (wave * LOADS + i) * 1024);
         }
     }
     // Fragment of the 32 entries from `entry` (a multiple of 32) on, summed indices 16 s to 16 s + 15 of the tile.
@@ -159,42 +172,77 @@ struct Product {
         const size_t p_step = (P_COLUMNS ? (size_t)P.ld * BK : BK) * 2, q_step = (Q_COLUMNS ? (size_t)Q.ld * BK : BK) * 2;
         const char *pf = nullptr, *qf = nullptr;
         uint32_t step = 0, pass = 0;                                   // of the next tile to be loaded
+        const uint32_t lds_at = lds_address(lds);
         auto request = [&](int stage) {
             if (step == 0) {
                 pf = TP::origin(passes == 3 && pass == 0 ? P.lo : P.hi, P, p0, k_from);
                 qf = TQ::origin(passes == 3 && pass == 1 ? Q.lo : Q.hi, Q, q0, k_from);
             }
             const uint32_t k = k_from + step * BK;
-            tp.load(pf, P.summed - k, lds + stage * STAGE, wave);
-            tq.load(qf, Q.summed - k, lds + stage * STAGE + TP::BYTES, wave);
+            tp.load(pf, P.summed - k, lds_at + stage * STAGE, wave);
+            tq.load(qf, Q.summed - k, lds_at + stage * STAGE + TP::BYTES, wave);
             pf += p_step;
             qf += q_step;
             if (++step == steps) step = 0, ++pass;
         };
+        // Fragments are read one step of 16 ahead of the matrix instructions that take them, the first of a tile during the last
+        // step of the tile before.  At that point every wavefront has read all it needs of the old tile, whose place the
+        // loads of the tile after the next then take: a tile's loads have a whole tile's products to arrive in.
+        constexpr int STEPS = BK / 16;
+        s16x8 fp[2][FP], fq[2][FQ];
+        auto read = [&](int stage, int s, int to) {
+            const char* lp = lds + stage * STAGE;
+#pragma unroll
+            for (int b = 0; b < FQ; ++b) fq[to][b] = TQ::fragment(lp + TP::BYTES, qw + b * 32, s, lane);
+#pragma unroll
+            for (int a = 0; a < FP; ++a) fp[to][a] = TP::fragment(lp, pw + a * 32, s, lane);
+        };
+        auto multiply = [&](int from) {
+#pragma unroll
+            for (int a = 0; a < FP; ++a)
+#pragma unroll
+                for (int b = 0; b < FQ; ++b) acc[a][b] = E::mfma(fp[from][a], fq[from][b], acc[a][b]);
+        };
+        // A step's reads go out between its matrix instructions, not in front of those that take them.
+        constexpr int READS = (P_COLUMNS ? 2 : 1) * FP + (Q_COLUMNS ? 2 : 1) * FQ, PRODUCTS = FP * FQ;
+        auto interleave = [&]() {
+            constexpr int EACH = (READS + PRODUCTS - 1) / PRODUCTS;
+#pragma unroll
+            for (int i = 0; i < PRODUCTS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);  // LDS reads
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);     // matrix instructions
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
         request(0);
+        if (total > 1) {
+            request(1);
+            wait_for_loads<TP::LOADS + TQ::LOADS>();
+        } else {
+            wait_for_loads<0>();
+        }
+        workgroup_barrier();
+        read(0, 0, 0);
         for (uint32_t t = 0; t < total; ++t) {
-            __syncthreads();                                           // tile t has arrived, tile t - 1 is done with
-            if (t + 1 < total) request((t + 1) & 1);
             if (passes == 3 && t == 2 * steps) {
 #pragma unroll
                 for (int a = 0; a < FP; ++a)
 #pragma unroll
                     for (int b = 0; b < FQ; ++b) acc[a][b] *= 0x1p-11f;
             }
-            const char* lp = lds + (t & 1) * STAGE;
-            const char* lq = lp + TP::BYTES;
 #pragma unroll
-            for (int s = 0; s < (int)BK / 16; ++s) {
-                s16x8 fp[FP], fq[FQ];
-#pragma unroll
-                for (int a = 0; a < FP; ++a) fp[a] = TP::fragment(lp, pw + a * 32, s, lane);
-#pragma unroll
-                for (int b = 0; b < FQ; ++b) fq[b] = TQ::fragment(lq, qw + b * 32, s, lane);
-#pragma unroll
-                for (int a = 0; a < FP; ++a)
-#pragma unroll
-                    for (int b = 0; b < FQ; ++b) acc[a][b] = E::mfma(fp[a], fq[b], acc[a][b]);
+            for (int s = 0; s + 1 < STEPS; ++s) {
+                read(t & 1, s + 1, (s + 1) & 1);
+                multiply(s & 1);
+                interleave();
             }
+            if (t + 1 < total) {
+                wait_for_loads<0>();
+                workgroup_barrier();
+                read((t + 1) & 1, 0, 0);
+                if (t + 2 < total) request(t & 1);
+            }
+            multiply((STEPS - 1) & 1);
         }
         __syncthreads();                                               // the LDS is free for what follows
     }
@@ -202,5 +250,29 @@ struct Product {
 
 // Register r of a fragment: entry of P inside the fragment's 32 (the entry of Q is lane & 31).
 __device__ __forceinline__ uint32_t p_in_fragment(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+
+// A wavefront's way from accumulators to memory: 32 rows (entries of Q) of 128 entries of P, through LDS, so that a store instruction
+// writes whole rows of 256 bytes and more.  As the matrix instructions leave them, a lane holds four entries of a row and neighbouring
+// lanes neighbouring rows.  Chunks of 16 bytes are turned by the row, which keeps both sides off each other's banks.
+template <int SIZE>        // bytes per entry: 2 or 4
+struct Rows32 {
+    static constexpr int ENTRIES = 128, CHUNKS = ENTRIES * SIZE / 16, BYTES = 32 * ENTRIES * SIZE, PER_CHUNK = 16 / SIZE;
+    static __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t chunk) { return (row * CHUNKS + (chunk ^ (row & 15u))) * 16; }
+    // four entries from p on (a multiple of 4) of this lane's row
+    static __device__ __forceinline__ void put(char* lds, uint32_t p, int lane, const void* four) {
+        char* to = lds + place(lane & 31, p / PER_CHUNK) + (p % PER_CHUNK) * SIZE;
+        if (SIZE == 2) *reinterpret_cast<uint64_t*>(to) = *static_cast<const uint64_t*>(four);
+        else *reinterpret_cast<f32x4*>(to) = *static_cast<const f32x4*>(four);
+    }
+    // store(row, first entry, 16 bytes) for every chunk
+    template <class F>
+    static __device__ __forceinline__ void each(const char* lds, int lane, F store) {
+#pragma unroll
+        for (int i = 0; i < 32 * CHUNKS / 64; ++i) {
+            const uint32_t at = i * 64 + lane, row = at / CHUNKS, chunk = at % CHUNKS;
+            store(row, chunk * PER_CHUNK, *reinterpret_cast<const uint4*>(lds + place(row, chunk)));
+        }
+    }
+};
 
 }  // namespace iwp
