@@ -9,6 +9,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace iwp {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -83,8 +85,8 @@ struct Tile {
     static constexpr int PER_ROW = COLUMNS ? R / 8 : BK / 8;
     static constexpr int TURNS = COLUMNS ? (R / 32 < 8 ? R / 32 : 8) : 8;
 
-    uint32_t at[LOADS];        // byte offset of this lane's chunk in the tile at summed index 0
-    uint32_t within[LOADS];    // rows of K: the chunk's first summed index; columns of K: its summed index
+    uint32_t at[LOADS];        // byte offset of this lane's chunk from the tile's origin
+    uint32_t within[LOADS];    // its (first) summed index in the tile
     uint32_t row_bytes;
 
     static __device__ __forceinline__ uint32_t turn(uint32_t r) {
@@ -104,7 +106,7 @@ struct Tile {
                 const uint32_t chunk = (((place >> 2) ^ turn(row)) << 2) | (place & 3u);
                 const uint32_t entry = first + chunk * 8 < o.extent ? chunk * 8 : 0u;
                 within[i] = row;
-                at[i] = entry * 2;
+                at[i] = entry * 2 + row * row_bytes;
             }
         }
     }
@@ -112,15 +114,10 @@ struct Tile {
     static __device__ __forceinline__ const char* origin(const uint16_t* plane, const Operand& o, uint32_t first, uint32_t k) {
         return reinterpret_cast<const char*>(plane) + (COLUMNS ? ((size_t)k * o.ld + first) * 2 : ((size_t)first * o.ld + k) * 2);
     }
-    // left: summed entries from k on (at least 1)
-    __device__ __forceinline__ void load(const char* from, uint32_t left, uint32_t lds, int wave) const {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            uint32_t off;
-            if (!COLUMNS) off = within[i] < left ? at[i] : at[i] - within[i] * 2;
-            else off = at[i] + min(within[i], left - 1) * row_bytes;
-            load_to_lds(from, off, lds + (wave * LOADS + i) * 1024);
-        }
+    // The i-th load; left: summed entries from the tile's first on (at least 1)
+    __device__ __forceinline__ void load(int i, const char* from, uint32_t left, uint32_t lds, int wave) const {
+        const uint32_t inside = COLUMNS ? at[i] - (within[i] - (left - 1)) * row_bytes : at[i] - within[i] * 2;
+        load_to_lds(from, within[i] < left ? at[i] : inside, lds + (wave * LOADS + i) * 1024);
     }
     // Fragment of the 32 entries from `entry` (a multiple of 32) on, summed indices 16 s to 16 s + 15 of the tile.
     static __device__ __forceinline__ s16x8 fragment(const char* lds, uint32_t entry, int s, int lane) {
@@ -141,7 +138,7 @@ struct Tile {
 // The product of a BP x BQ tile: WP x WQ wavefronts, each BP / WP entries of P by BQ / WQ of Q.
 template <class E, int BP, int BQ, int WP, int WQ, bool P_COLUMNS, bool Q_COLUMNS>
 struct Product {
-    static constexpr int WAVES = WP * WQ, THREADS = WAVES * 64;
+    static constexpr int WAVES = WP * WQ;
     static constexpr int FP = BP / WP / 32, FQ = BQ / WQ / 32;     // fragments of 32 per wavefront
     typedef Tile<BP, WAVES, P_COLUMNS> TP;
     typedef Tile<BQ, WAVES, Q_COLUMNS> TQ;
@@ -173,77 +170,97 @@ struct Product {
         const char *pf = nullptr, *qf = nullptr;
         uint32_t step = 0, pass = 0;                                   // of the next tile to be loaded
         const uint32_t lds_at = lds_address(lds);
-        auto request = [&](int stage) {
-            if (step == 0) {
-                pf = TP::origin(passes == 3 && pass == 0 ? P.lo : P.hi, P, p0, k_from);
-                qf = TQ::origin(passes == 3 && pass == 1 ? Q.lo : Q.hi, Q, q0, k_from);
-            }
-            const uint32_t k = k_from + step * BK;
-            tp.load(pf, P.summed - k, lds_at + stage * STAGE, wave);
-            tq.load(qf, Q.summed - k, lds_at + stage * STAGE + TP::BYTES, wave);
+        constexpr int LOADS = TP::LOADS + TQ::LOADS, STEPS = BK / 16, PRODUCTS = FP * FQ;
+        // load i of the tile `step` of `pass`, into a stage; advance() goes on to the next tile
+        auto origin = [&]() {
+            pf = TP::origin(passes == 3 && pass == 0 ? P.lo : P.hi, P, p0, k_from);
+            qf = TQ::origin(passes == 3 && pass == 1 ? Q.lo : Q.hi, Q, q0, k_from);
+        };
+        auto load = [&](int i, uint32_t stage) {
+            const uint32_t k = k_from + step * BK, to = lds_at + stage * STAGE;
+            if (i < TP::LOADS) tp.load(i, pf, P.summed - k, to, wave);
+            else tq.load(i - TP::LOADS, qf, Q.summed - k, to + TP::BYTES, wave);
+        };
+        auto advance = [&]() {
             pf += p_step;
             qf += q_step;
-            if (++step == steps) step = 0, ++pass;
-        };
-        // Fragments are read one step of 16 ahead of the matrix instructions that take them, the first of a tile during the last
-        // step of the tile before.  At that point every wavefront has read all it needs of the old tile, whose place the
-        // loads of the tile after the next then take: a tile's loads have a whole tile's products to arrive in.
-        constexpr int STEPS = BK / 16;
-        s16x8 fp[2][FP], fq[2][FQ];
-        auto read = [&](int stage, int s, int to) {
-            const char* lp = lds + stage * STAGE;
-#pragma unroll
-            for (int b = 0; b < FQ; ++b) fq[to][b] = TQ::fragment(lp + TP::BYTES, qw + b * 32, s, lane);
-#pragma unroll
-            for (int a = 0; a < FP; ++a) fp[to][a] = TP::fragment(lp, pw + a * 32, s, lane);
-        };
-        auto multiply = [&](int from) {
-#pragma unroll
-            for (int a = 0; a < FP; ++a)
-#pragma unroll
-                for (int b = 0; b < FQ; ++b) acc[a][b] = E::mfma(fp[from][a], fq[from][b], acc[a][b]);
-        };
-        // A step's reads go out between its matrix instructions, not in front of those that take them.
-        constexpr int READS = (P_COLUMNS ? 2 : 1) * FP + (Q_COLUMNS ? 2 : 1) * FQ, PRODUCTS = FP * FQ;
-        auto interleave = [&]() {
-            constexpr int EACH = (READS + PRODUCTS - 1) / PRODUCTS;
-#pragma unroll
-            for (int i = 0; i < PRODUCTS; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);  // LDS reads
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);     // matrix instructions
+            if (++step == steps) {
+                step = 0;
+                ++pass;
+                origin();
             }
-            __builtin_amdgcn_sched_barrier(0);
         };
-        request(0);
+        origin();
+        s16x8 fp[2][FP], fq[2][FQ];
+        auto read = [&](int i, uint32_t stage, int s, int to) {        // fragment i of a step
+            const char* lp = lds + stage * STAGE;
+            if (i < FQ) fq[to][i] = TQ::fragment(lp + TP::BYTES, qw + i * 32, s, lane);
+            else fp[to][i - FQ] = TP::fragment(lp, pw + (i - FQ) * 32, s, lane);
+        };
+        // One tile.  Fragments are read a step of 16 ahead of the matrix instructions that take them, the first of a tile during the
+        // last step of the tile before.  At that point every wavefront has read all it needs of the old tile, whose place the loads
+        // of the tile after the next then take: they have a whole tile's products to arrive in.  Reads and loads go out one
+        // by one between the matrix instructions; left to itself the compiler puts them in front of these, in bursts.
+        auto tile = [&](auto next, auto more, uint32_t stage) {
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                const bool last = s + 1 == STEPS;
+                if (last && next) {
+                    wait_for_loads<0>();
+                    workgroup_barrier();
+                }
+#pragma unroll
+                for (int i = 0; i < PRODUCTS; ++i) {
+#pragma unroll
+                    for (int r = i; r < FP + FQ; r += PRODUCTS) {
+                        if (!last) read(r, stage, s + 1, (s + 1) & 1);
+                        else if (next) read(r, stage ^ 1, 0, 0);
+                    }
+                    if (last && more)
+#pragma unroll
+                        for (int l = i; l < LOADS; l += PRODUCTS) load(l, stage);
+                    acc[i / FQ][i % FQ] = E::mfma(fp[s & 1][i / FQ], fq[s & 1][i % FQ], acc[i / FQ][i % FQ]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if (more) advance();
+        };
+        constexpr std::true_type yes{};
+        constexpr std::false_type no{};
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load(i, 0);
+        advance();
         if (total > 1) {
-            request(1);
-            wait_for_loads<TP::LOADS + TQ::LOADS>();
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) load(i, 1);
+            advance();
+            wait_for_loads<LOADS>();
         } else {
             wait_for_loads<0>();
         }
         workgroup_barrier();
-        read(0, 0, 0);
-        for (uint32_t t = 0; t < total; ++t) {
+#pragma unroll
+        for (int i = 0; i < FP + FQ; ++i) read(i, 0, 0, 0);
+        uint32_t t = 0;
+        auto rescale = [&]() {
             if (passes == 3 && t == 2 * steps) {
 #pragma unroll
                 for (int a = 0; a < FP; ++a)
 #pragma unroll
                     for (int b = 0; b < FQ; ++b) acc[a][b] *= 0x1p-11f;
             }
-#pragma unroll
-            for (int s = 0; s + 1 < STEPS; ++s) {
-                read(t & 1, s + 1, (s + 1) & 1);
-                multiply(s & 1);
-                interleave();
-            }
-            if (t + 1 < total) {
-                wait_for_loads<0>();
-                workgroup_barrier();
-                read((t + 1) & 1, 0, 0);
-                if (t + 2 < total) request(t & 1);
-            }
-            multiply((STEPS - 1) & 1);
+        };
+        for (; t + 2 < total; ++t) {
+            rescale();
+            tile(yes, yes, t & 1);
         }
+        if (t + 1 < total) {
+            rescale();
+            tile(yes, no, t & 1);
+            ++t;
+        }
+        rescale();
+        tile(no, no, t & 1);
         __syncthreads();                                               // the LDS is free for what follows
     }
 };
