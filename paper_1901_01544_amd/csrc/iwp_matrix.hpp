@@ -57,7 +57,7 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, u
 // Until at most LEFT of this wavefront's loads are on their way and all of its LDS reads are done.
 template <int LEFT>
 __device__ __forceinline__ void wait_for_loads() {
-    static_assert(LEFT < 16, "fits the counter's low bits");
+    static_assert(LEFT < 64, "six bits");
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
 }
 __device__ __forceinline__ void workgroup_barrier() {
@@ -208,7 +208,9 @@ struct Product {
                 if (last && next) {
                     wait_for_loads<0>();
                     workgroup_barrier();
+                    __builtin_amdgcn_s_setprio(1);                     // the wavefront whose loads are due goes first
                 }
+                if (s == 0) __builtin_amdgcn_s_setprio(0);
 #pragma unroll
                 for (int i = 0; i < PRODUCTS; ++i) {
 #pragma unroll
