@@ -40,28 +40,41 @@ struct HeadRows {          // the tokens that count, in order
 };
 
 struct Teacher {           // per token
-    int32_t* index;        // [tokens, top], -1: left out
-    float* q;
+    int32_t* index;        // [tokens, top], -1: left out, or an index that stands before it
+    float* q;              // softmax over the entries; an index that occurs several times has the sum
     float* z;              // by row: the head's logit there
-    float* entropy;        // sum q log q
-    uint8_t* any;
+    float* entropy;        // sum q log q, entry by entry
+    uint8_t* any;          // 1: there are entries, 2: the label is among them
     uint32_t top;
     float t;
+    // The entries by where the logits' product will find them: for every 64 rows, sorted into stretches of `width` vocabulary entries.
+    uint32_t *start;       // [rows / 64, stretches + 1]
+    uint32_t *found;       // [rows / 64, 64 * top]: place in the stretch, row of the 64, entry
+    uint32_t width, stretches;
 };
+constexpr uint32_t STRETCHES = 8192;               // at most: their counts lie in LDS
+__device__ __forceinline__ uint32_t found_word(uint32_t place, uint32_t row, uint32_t k) { return place << 16 | row << 10 | k; }
+static_assert(IWP_MAX_TOP <= 1u << 10 && IWP_MAX_VOCAB / STRETCHES <= 1u << 16, "found_word");
 
 // ------------------------------------------------------------------ tokens
 
-// softmax of the teacher's entries of one token at temperature t; a wavefront per token
+// Softmax of the teacher's entries of one token at temperature t; a wavefront per token.
 __global__ void __launch_bounds__(256) k_head_teacher(const int32_t* __restrict__ index, const float* __restrict__ logit,
-                                                      uint32_t tokens, uint32_t vocab, Teacher T) {
-    const uint32_t i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+                                                      const int32_t* __restrict__ label, uint32_t tokens, uint32_t vocab, Teacher T) {
+    __shared__ int32_t at[4][IWP_MAX_TOP];
+    __shared__ float qs[4][IWP_MAX_TOP];
+    const uint32_t wave = threadIdx.x >> 6, i = blockIdx.x * 4 + wave, lane = threadIdx.x & 63;
     if (i >= tokens) return;
     const size_t base = (size_t)i * T.top;
     float m = -INFINITY;
     bool any = false, nan = false;
     for (uint32_t k = lane; k < T.top; k += 64) {
         const float s = logit[base + k];
-        if ((uint32_t)index[base + k] < vocab && !(s == -INFINITY)) {
+        const int32_t j = index[base + k];
+        const bool in = (uint32_t)j < vocab && !(s == -INFINITY);
+        at[wave][k] = in ? j : -1;
+        qs[wave][k] = s;
+        if (in) {
             any = true;
             nan |= s != s;
             m = fmaxf(m, s);
@@ -71,25 +84,38 @@ __global__ void __launch_bounds__(256) k_head_teacher(const int32_t* __restrict_
     any = __ballot(any) != 0;
     if (__ballot(nan)) m = NAN;
     float sum = 0.0f;
-    for (uint32_t k = lane; k < T.top; k += 64) {
-        const float s = logit[base + k];
-        if ((uint32_t)index[base + k] < vocab && !(s == -INFINITY)) sum += expf((s - m) / T.t);
-    }
+    for (uint32_t k = lane; k < T.top; k += 64)
+        if (at[wave][k] >= 0) sum += expf((qs[wave][k] - m) / T.t);
     for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
     const float log_sum = logf(sum);
     float entropy = 0.0f;
     for (uint32_t k = lane; k < T.top; k += 64) {
-        const float s = logit[base + k];
-        const bool in = (uint32_t)index[base + k] < vocab && !(s == -INFINITY);
-        const float log_q = (s - m) / T.t - log_sum, q = in ? expf(log_q) : 0.0f;
-        T.index[base + k] = in ? index[base + k] : -1;
-        T.q[base + k] = q;
+        const bool in = at[wave][k] >= 0;
+        const float log_q = (qs[wave][k] - m) / T.t - log_sum, q = in ? expf(log_q) : 0.0f;
+        qs[wave][k] = q;
         if (in && q != 0.0f) entropy += q * log_q;
     }
     for (int o = 32; o; o >>= 1) entropy += __shfl_xor(entropy, o);
+    const int32_t y = label ? label[i] : -1;
+    bool is_label = false;
+    for (uint32_t k = lane; k < T.top; k += 64) {
+        const int32_t j = at[wave][k];
+        float q = 0.0f;
+        bool first = j >= 0;
+#pragma unroll 8
+        for (uint32_t v = 0; v < T.top; ++v)
+            if (at[wave][v] == j) {
+                q += qs[wave][v];
+                first = first && v >= k;
+            }
+        T.index[base + k] = first ? j : -1;
+        T.q[base + k] = first ? q : 0.0f;
+        is_label |= first && j == y;
+    }
+    is_label = __ballot(is_label) != 0;
     if (lane == 0) {
         T.entropy[i] = entropy;
-        T.any[i] = any;
+        T.any[i] = any + 2 * is_label;
     }
 }
 
@@ -112,8 +138,9 @@ __global__ void __launch_bounds__(1024) k_head_rows(const int32_t* __restrict__ 
             const float a = weight ? weight[i] : 1.0f;
             if (label && (uint32_t)label[i] < vocab) y = label[i];
             if (y >= 0) ch = a * hard;
-            if (any && any[i]) cs = a * (soft * t * t);
-            in = a != 0.0f && ((y >= 0 && hard != 0.0f) || (any && any[i] && soft != 0.0f));
+            const bool entries = any && any[i];
+            if (entries) cs = a * (soft * t * t);
+            in = a != 0.0f && ((y >= 0 && hard != 0.0f) || (entries && soft != 0.0f));
         }
         const uint64_t mask = __ballot(in);
         if (lane == 0) in_wave[wave] = __popcll(mask);
@@ -148,6 +175,52 @@ __global__ void __launch_bounds__(1024) k_head_rows(const int32_t* __restrict__ 
     }
 }
 
+// Sorts the teacher's entries of 64 rows into stretches of the vocabulary.  Inside a stretch their order is nobody's concern.
+__global__ void __launch_bounds__(1024) k_head_sort(HeadRows R, Teacher T, const HeadScalars* __restrict__ S) {
+    __shared__ uint32_t n[STRETCHES], in_wave[16];
+    const uint32_t count = S->count, row0 = blockIdx.x * 64, thread = threadIdx.x;
+    if (row0 >= count) return;
+    const uint32_t entries = min(64u, count - row0) * T.top;
+    for (uint32_t b = thread; b < T.stretches; b += 1024) n[b] = 0;
+    __syncthreads();
+    for (uint32_t e = thread; e < entries; e += 1024) {
+        const int32_t j = T.index[(size_t)R.token[row0 + e / T.top] * T.top + e % T.top];
+        if (j >= 0) atomicAdd(&n[(uint32_t)j / T.width], 1u);
+    }
+    __syncthreads();
+    uint32_t* start = T.start + (size_t)blockIdx.x * (T.stretches + 1);
+    uint32_t before = 0;
+    for (uint32_t b0 = 0; b0 < T.stretches; b0 += 1024) {
+        const uint32_t b = b0 + thread, mine = b < T.stretches ? n[b] : 0;
+        uint32_t sum = mine;
+        for (uint32_t o = 1; o < 64; o <<= 1) {
+            const uint32_t other = __shfl_up(sum, o);
+            if ((thread & 63) >= o) sum += other;
+        }
+        if ((thread & 63) == 63) in_wave[thread >> 6] = sum;
+        __syncthreads();
+        uint32_t all = 0, ahead = before;
+        for (uint32_t v = 0; v < 16; ++v) {
+            if (v < thread >> 6) ahead += in_wave[v];
+            all += in_wave[v];
+        }
+        if (b < T.stretches) {
+            n[b] = ahead + sum - mine;
+            start[b] = ahead + sum - mine;
+        }
+        before += all;
+        __syncthreads();
+    }
+    if (thread == 0) start[T.stretches] = before;
+    for (uint32_t e = thread; e < entries; e += 1024) {
+        const uint32_t row = e / T.top, k = e % T.top;
+        const int32_t j = T.index[(size_t)R.token[row0 + row] * T.top + k];
+        if (j < 0) continue;
+        const uint32_t stretch = (uint32_t)j / T.width, at = atomicAdd(&n[stretch], 1u);
+        T.found[(size_t)row0 * T.top + at] = found_word((uint32_t)j - stretch * T.width, row, k);
+    }
+}
+
 // ------------------------------------------------------------------ operands
 
 // Binary32 operands: x s = hi + 2^-11 lo with hi, lo in fp16 and s the power of two that takes the largest finite |x| to 2^13 or
@@ -159,25 +232,63 @@ __device__ __forceinline__ float split_scale(uint32_t max_bits) {
 // A sum of products of two split operands -> the sum itself, in two factors that are normal numbers.
 __device__ __forceinline__ float unsplit(float sum, float sp, float sq) { return sum * (1.0f / sp) * (1.0f / sq); }
 
-__global__ void __launch_bounds__(256) k_head_max(const float* __restrict__ x, int64_t ld, uint32_t rows, uint32_t dim,
-                                                  const uint32_t* __restrict__ token, const uint32_t* __restrict__ count,
-                                                  uint32_t* __restrict__ max_bits) {
-    if (count) rows = *count;
+struct HeadMatrix {        // rows of a caller's matrix; those of `token` alone where it is given, `count` of them
+    const void* x;
+    int64_t ld;
+    uint32_t rows, dim;
+    const uint32_t* token;
+    const uint32_t* count;
+};
+
+// 128-bit accesses at an element's own alignment
+typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t words4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+// How a kernel's 256 threads lie over rows of `chunks` units: 2^shift threads to a row, the rest of the row by further workgroups.
+struct Spread {
+    uint32_t shift, across;
+    __device__ __forceinline__ uint32_t row() const { return blockIdx.x / across * (256u >> shift) + (threadIdx.x >> shift); }
+    __device__ __forceinline__ uint32_t unit() const { return (blockIdx.x % across << shift) + (threadIdx.x & ((1u << shift) - 1)); }
+};
+
+// The first `blocks` workgroups take one matrix, the others another; 16 rows of 1024 elements at a time.  Few and large workgroups: each
+// ends in an atomic on one word, and those take 20 ns one after the other.
+__global__ void __launch_bounds__(1024) k_head_max(HeadMatrix A, HeadMatrix B, uint32_t blocks, HeadScalars* __restrict__ S) {
+    const bool second = blockIdx.x >= blocks;
+    const HeadMatrix M = second ? B : A;
+    const uint32_t block = second ? blockIdx.x - blocks : blockIdx.x, n_blocks = second ? gridDim.x - blocks : blocks;
+    const uint32_t rows = M.count ? *M.count : M.rows, across = (M.dim + 1023) / 1024, units = (rows + 15) / 16 * across;
     uint32_t m = 0;
-    for (uint32_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const float* p = x + (int64_t)(token ? token[r] : r) * ld;
-        for (uint32_t c = threadIdx.x; c < dim; c += 256) {
-            const uint32_t b = __float_as_uint(p[c]) & 0x7fffffffu;
-            if (b < 0x7f800000u) m = max(m, b);
+    for (uint32_t u = block; u < units; u += n_blocks) {
+        const uint32_t r0 = u / across * 16 + threadIdx.x / 256 * 4, c = u % across * 1024 + threadIdx.x % 256 * 4;
+        if (c >= M.dim) continue;
+        words4 v[4];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const uint32_t r = min(r0 + i, rows - 1);
+            const float* p = static_cast<const float*>(M.x) + (int64_t)(M.token ? M.token[r] : r) * M.ld + c;
+            if (c + 4 <= M.dim) {
+                v[i] = *reinterpret_cast<const words4*>(p);
+            } else {
+                v[i] = words4{};
+                for (uint32_t e = 0; c + e < M.dim; ++e) v[i][e] = __float_as_uint(p[e]);
+            }
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t b = v[i][e] & 0x7fffffffu;
+                m = max(m, b < 0x7f800000u ? b : 0u);
+            }
     }
     for (int o = 32; o; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
-    __shared__ uint32_t of[4];
+    __shared__ uint32_t of[16];
     if ((threadIdx.x & 63) == 0) of[threadIdx.x >> 6] = m;
     __syncthreads();
     if (threadIdx.x == 0) {
-        m = max(max(of[0], of[1]), max(of[2], of[3]));
-        if (m) atomicMax(max_bits, m);
+        for (int v = 1; v < 16; ++v) m = max(m, of[v]);
+        if (m) atomicMax(second ? &S->w_max : &S->h_max, m);
     }
 }
 
@@ -188,28 +299,50 @@ __device__ __forceinline__ void split_f32(float x, float s, uint16_t* hi, uint16
     *lo = __builtin_bit_cast(uint16_t, (_Float16)((y - (float)h) * 2048.0f));
 }
 
-// Rows of a matrix (those of `token` if given, zeros up to the next multiple of 64 behind them) into rows of ld_out, zeros past dim.
+// A matrix into rows of ld_out, zeros past its width; with `count`, zeros in the rows behind it up to the next multiple of 64.  Eight
+// elements of four rows a thread.
+constexpr uint32_t PACK_ROWS = 4;
 template <bool F32>
-__global__ void __launch_bounds__(256) k_head_pack(const void* __restrict__ x, int64_t ld, uint32_t rows, uint32_t dim,
-                                                   const uint32_t* __restrict__ token, const uint32_t* __restrict__ count,
-                                                   const uint32_t* __restrict__ max_bits, uint16_t* __restrict__ hi,
-                                                   uint16_t* __restrict__ lo, uint32_t ld_out) {
-    const uint32_t end = count ? (*count + 63) & ~63u : rows;
-    if (count) rows = *count;
+__global__ void __launch_bounds__(256) k_head_pack(HeadMatrix M, Spread spread, const uint32_t* __restrict__ max_bits,
+                                                   uint16_t* __restrict__ hi, uint16_t* __restrict__ lo, uint32_t ld_out) {
+    const uint32_t rows = M.count ? *M.count : M.rows, end = M.count ? (rows + 63) & ~63u : rows;
     const float s = F32 ? split_scale(*max_bits) : 1.0f;
-    for (uint32_t r = blockIdx.x; r < end; r += gridDim.x) {
-        const int64_t from = r < rows ? (int64_t)(token ? token[r] : r) * ld : 0;
-        for (uint32_t c = threadIdx.x; c < ld_out; c += 256) {
-            const bool in = r < rows && c < dim;
-            const size_t at = (size_t)r * ld_out + c;
-            if (F32) {
-                uint16_t a, b;
-                split_f32(in ? static_cast<const float*>(x)[from + c] : 0.0f, s, &a, &b);
-                hi[at] = a;
-                lo[at] = b;
-            } else {
-                hi[at] = in ? static_cast<const uint16_t*>(x)[from + c] : (uint16_t)0;
-            }
+    const uint32_t c = spread.unit() * 8, r0 = spread.row() * PACK_ROWS;
+    if (c >= ld_out) return;
+    constexpr int WORDS = F32 ? 2 : 1;
+    words4 v[PACK_ROWS][WORDS];
+#pragma unroll
+    for (uint32_t i = 0; i < PACK_ROWS; ++i) {
+        const uint32_t r = r0 + i;
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) v[i][w] = words4{};
+        if (r >= rows) continue;
+        const char* p = static_cast<const char*>(M.x) + ((int64_t)(M.token ? M.token[r] : r) * M.ld + c) * (F32 ? 4 : 2);
+        if (c + 8 <= M.dim) {
+#pragma unroll
+            for (int w = 0; w < WORDS; ++w)
+                v[i][w] = F32 ? *reinterpret_cast<const words4*>(p + 16 * w) : (words4)*reinterpret_cast<const words4_any*>(p);
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e)
+                if (c + e < M.dim) {
+                    if (F32) v[i][e / 4 % WORDS][e % 4] = reinterpret_cast<const uint32_t*>(p)[e];
+                    else v[i][0][e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[e] << (e % 2 * 16);
+                }
+        }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < PACK_ROWS; ++i) {
+        if (r0 + i >= end) break;
+        const size_t at = (size_t)(r0 + i) * ld_out + c;
+        if (F32) {
+            uint16_t a[8], b[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) split_f32(__uint_as_float(v[i][e / 4 % WORDS][e % 4]), s, &a[e], &b[e]);
+            *reinterpret_cast<uint4*>(hi + at) = *reinterpret_cast<const uint4*>(a);
+            *reinterpret_cast<uint4*>(lo + at) = *reinterpret_cast<const uint4*>(b);
+        } else {
+            *reinterpret_cast<words4*>(hi + at) = v[i][0];
         }
     }
 }
@@ -284,7 +417,7 @@ __device__ __forceinline__ void put_dz(float g, uint16_t* hi, uint16_t* lo) {
 
 template <class E, int BP, int BQ, int WP, int WQ, int MODE, bool F32, bool WIDE, bool SOFT>
 __global__ void __launch_bounds__(WP * WQ * 64) k_head_logits(Operand W, Operand H, uint32_t dim_padded, HeadPiece G, HeadRows R,
-                                                              HeadStats St, float t, const HeadScalars* __restrict__ S) {
+                                                              HeadStats St, Teacher T, const HeadScalars* __restrict__ S) {
     typedef Product<E, BP, BQ, WP, WQ, false, false> M;
     __shared__ __align__(1024) char lds[M::LDS];
     const uint32_t count = S->count;
@@ -292,13 +425,29 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_logits(Operand W, Operand
     tile_of(blockIdx.x, (G.n + BP - 1) / BP, H.extent / BQ, &tp, &tq);
     if (tq * BQ >= count) return;
     H.extent = count;
-    M mm;
-    mm.run(W, H, tp * BP, tq * BQ, 0, dim_padded, lds);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t p0 = tp * BP + M::p_of(wave), q0 = tq * BQ + M::q_of(wave);
+    // the teacher's entries in this wavefront's stretch of the vocabulary, for the 64 rows that its own are among: the first 64 of them
+    // a lane each, from before the product
+    constexpr bool PICK = SOFT && MODE != GRADIENT;
+    uint32_t found = 0, found_from = 0, found_to = 0;
+    const uint32_t* list = nullptr;
+    if (PICK && q0 < count) {
+        const uint32_t stretch = min((G.first + p0) / T.width, T.stretches - 1);
+        const uint32_t* start = T.start + (size_t)(q0 / 64) * (T.stretches + 1) + stretch;
+        list = T.found + (size_t)(q0 & ~63u) * T.top;
+        found_from = start[0];
+        found_to = start[1];
+        if (found_from + lane < found_to) found = list[found_from + lane];
+    }
+    M mm;
+    mm.run(W, H, tp * BP, tq * BQ, 0, dim_padded, lds);
     float sw = 1.0f, sh = 1.0f;
     if (F32) sw = split_scale(S->w_max), sh = split_scale(S->h_max);
-    const float t_inv = 1.0f / t;
+    const float t = T.t, t_inv = 1.0f / t;
+    typedef Rows32<4, BP / WP> Picked;
+    static_assert(M::WAVES * Picked::BYTES <= M::LDS, "a wavefront's rows");
+    char* picked_lds = lds + wave * Picked::BYTES;
 #pragma unroll
     for (int b = 0; b < M::FQ; ++b) {
         const uint32_t q = q0 + b * 32 + (lane & 31);
@@ -309,19 +458,19 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_logits(Operand W, Operand
 #pragma unroll
                 for (int r = 0; r < 16; ++r) mm.acc[a][b][r] = unsplit(mm.acc[a][b][r], sw, sh);
         }
+        if (p0 + BP / WP > G.n) {                          // the piece ends in here
+#pragma unroll
+            for (int a = 0; a < M::FP; ++a)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    mm.acc[a][b][r] = p0 + a * 32 + p_in_fragment(r, lane) < G.n ? mm.acc[a][b][r] : -INFINITY;
+        }
         float m = -INFINITY;
-        RowGradient g;
+        RowGradient g{0.0f, 0.0f, INFINITY, INFINITY, 1.0f};       // of rows that are not there: zeros
         if (MODE != GRADIENT) {
             const int32_t label = row_in ? R.label[q] : -1;
             const uint32_t label_at = label >= 0 ? (uint32_t)label - (G.first + p0) - 4 * (lane >> 5) : ~0u;
             float z_label = 0.0f;
-            if (p0 + BP / WP > G.n) {                      // the piece ends in here
-#pragma unroll
-                for (int a = 0; a < M::FP; ++a)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        mm.acc[a][b][r] = p0 + a * 32 + p_in_fragment(r, lane) < G.n ? mm.acc[a][b][r] : -INFINITY;
-            }
 #pragma unroll
             for (int a = 0; a < M::FP; ++a)
 #pragma unroll
@@ -353,10 +502,25 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_logits(Operand W, Operand
         } else if (row_in) {
             g = row_gradient(R, q, S->most, t, SOFT);
         }
+        if (PICK && found_from < found_to) {               // through LDS, where any lane can take any logit
+#pragma unroll
+            for (int a = 0; a < M::FP; ++a)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const f32x4 v = {mm.acc[a][b][c * 4], mm.acc[a][b][c * 4 + 1], mm.acc[a][b][c * 4 + 2], mm.acc[a][b][c * 4 + 3]};
+                    Picked::put(picked_lds, a * 32 + p_in_fragment(c * 4, lane), lane, &v);
+                }
+            const uint32_t stretch = (G.first + p0) / T.width * T.width, rows_from = (q0 & 63u) + b * 32;
+            for (uint32_t i = found_from + lane; i < found_to; i += 64) {
+                const uint32_t word = i < found_from + 64 ? found : list[i];
+                const uint32_t p = (word >> 16) + stretch - (G.first + p0), row = (word >> 10 & 63u) - rows_from;
+                if (p < (uint32_t)(BP / WP) && row < 32)
+                    T.z[(size_t)(q0 + b * 32 + row) * T.top + (word & 1023u)] = Picked::value(picked_lds, row, p);
+            }
+        }
         if (MODE == STATISTICS) continue;
-        typedef Rows32<2> Out;
-        static_assert(BP / WP == Out::ENTRIES && M::WAVES * Out::BYTES <= M::LDS, "a wavefront's rows");
-        char* mine = lds + wave * Out::BYTES;
+        typedef Rows32<2, BP / WP> Out;
+        char* mine = picked_lds;
         constexpr bool TWO = MODE == GRADIENT ? F32 : WIDE;
         uint64_t hi[M::FP][4], lo[M::FP][4];
 #pragma unroll
@@ -367,11 +531,9 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_logits(Operand W, Operand
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     uint16_t x = 0, y = 0;
-                    const uint32_t p = p0 + a * 32 + p_in_fragment(c * 4 + e, lane);
                     const float z = mm.acc[a][b][c * 4 + e];
                     if (MODE == GRADIENT) {
-                        const float d = SOFT ? g.softmaxes(z) : g.c1 * exp_of(z - g.lse);
-                        put_dz<E, F32>(row_in && p < G.n ? d : 0.0f, &x, &y);
+                        put_dz<E, F32>(SOFT ? g.softmaxes(z) : g.c1 * exp_of(z - g.lse), &x, &y);
                     } else {
                         keep_logit<WIDE>(z, m, &x, &y);
                     }
@@ -391,37 +553,16 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_logits(Operand W, Operand
     }
 }
 
-// The head's logits at the teacher's entries: a wavefront per entry.
-template <class V>
-__device__ __forceinline__ float element(const void* x, int64_t at) { return V::value(static_cast<const uint16_t*>(x)[at]); }
-struct F32Element {};
-template <>
-__device__ __forceinline__ float element<F32Element>(const void* x, int64_t at) { return static_cast<const float*>(x)[at]; }
-
-template <class V>
-__global__ void __launch_bounds__(256) k_head_picked(const void* __restrict__ h, int64_t ld_h, const void* __restrict__ w, int64_t ld_w,
-                                                     uint32_t dim, HeadRows R, Teacher T, const HeadScalars* __restrict__ S) {
-    const uint32_t lane = threadIdx.x & 63, count = S->count;
-    for (uint64_t at = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6); at < (uint64_t)count * T.top; at += (uint64_t)gridDim.x * 4) {
-        const uint32_t row = at / T.top, k = at % T.top, token = R.token[row];
-        const int32_t j = T.index[(size_t)token * T.top + k];
-        float sum = 0.0f;
-        if (j >= 0)
-            for (uint32_t c = lane; c < dim; c += 64) sum += element<V>(h, token * ld_h + c) * element<V>(w, j * ld_w + c);
-        for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-        if (lane == 0) T.z[at] = sum;
-    }
-}
-
 // ------------------------------------------------------------------ statistics and losses
 
-// 32 rows a workgroup, 8 threads a row; groups in a fixed order.
+// 16 rows a workgroup, 32 threads a row; groups in a fixed order.
 template <bool SOFT>
-__global__ void __launch_bounds__(256) k_head_join(HeadStats St, uint32_t groups, HeadRows R, Teacher T, float* __restrict__ loss,
+__global__ void __launch_bounds__(512) k_head_join(HeadStats St, uint32_t groups, HeadRows R, Teacher T, float* __restrict__ loss,
                                                    const HeadScalars* __restrict__ S) {
-    __shared__ float ms[8][32], ss[8][32], ts[8][32];
-    const uint32_t in = threadIdx.x & 31, part = threadIdx.x >> 5, row = blockIdx.x * 32 + in, count = S->count;
-    if (blockIdx.x * 32 >= count) return;
+    constexpr uint32_t ROWS = 16, PARTS = 32;
+    __shared__ float ms[PARTS][ROWS], ss[PARTS][ROWS], ts[PARTS][ROWS];
+    const uint32_t in = threadIdx.x % ROWS, part = threadIdx.x / ROWS, row = blockIdx.x * ROWS + in, count = S->count;
+    if (blockIdx.x * ROWS >= count) return;
     const float t_inv = SOFT ? 1.0f / T.t : 1.0f;
     float m = -INFINITY, s = 0.0f, st = 0.0f, picked = 0.0f;
     auto merge = [&](float m2, float s2, float t2) {
@@ -432,13 +573,24 @@ __global__ void __launch_bounds__(256) k_head_join(HeadStats St, uint32_t groups
         m = top;
     };
     if (row < count) {
-        for (uint32_t g = part; g < groups; g += 8) {
-            const size_t at = (size_t)g * St.ld + row;
-            merge(St.m[at], St.sum[at], SOFT ? St.sum_t[at] : 0.0f);
+        constexpr uint32_t AT_ONCE = 4;
+        for (uint32_t g0 = part; g0 < groups; g0 += PARTS * AT_ONCE) {
+            float gm[AT_ONCE], gs[AT_ONCE], gt[AT_ONCE];
+#pragma unroll
+            for (uint32_t v = 0; v < AT_ONCE; ++v) {
+                const uint32_t g = g0 + v * PARTS;
+                const size_t at = (size_t)min(g, groups - 1) * St.ld + row;
+                gm[v] = St.m[at];
+                gs[v] = St.sum[at];
+                gt[v] = SOFT ? St.sum_t[at] : 0.0f;
+            }
+#pragma unroll
+            for (uint32_t v = 0; v < AT_ONCE; ++v)
+                if (g0 + v * PARTS < groups) merge(gm[v], gs[v], gt[v]);
         }
         if (SOFT && R.soft[row] != 0.0f) {
             const size_t from = (size_t)R.token[row] * T.top, z = (size_t)row * T.top;
-            for (uint32_t k = part; k < T.top; k += 8)
+            for (uint32_t k = part; k < T.top; k += PARTS)
                 if (T.index[from + k] >= 0) picked += T.q[from + k] * T.z[z + k];
         }
     }
@@ -447,7 +599,7 @@ __global__ void __launch_bounds__(256) k_head_join(HeadStats St, uint32_t groups
     ts[part][in] = st;
     __syncthreads();
     if (part == 0)
-        for (int v = 1; v < 8; ++v) merge(ms[v][in], ss[v][in], ts[v][in]);
+        for (uint32_t v = 1; v < PARTS; ++v) merge(ms[v][in], ss[v][in], ts[v][in]);
     if (SOFT) {
         __syncthreads();
         ms[part][in] = picked;
@@ -455,7 +607,7 @@ __global__ void __launch_bounds__(256) k_head_join(HeadStats St, uint32_t groups
     }
     if (part || row >= count) return;
     if (SOFT)
-        for (int v = 1; v < 8; ++v) picked += ms[v][in];
+        for (uint32_t v = 1; v < PARTS; ++v) picked += ms[v][in];
     const uint32_t token = R.token[row];
     const float lse = m + logf(s);
     float l = 0.0f;
@@ -471,56 +623,96 @@ __global__ void __launch_bounds__(256) k_head_join(HeadStats St, uint32_t groups
 
 // ------------------------------------------------------------------ the logits' gradient
 
-// In place on a kept piece; eight entries a thread.
-template <class E, bool F32, bool WIDE, bool SOFT>
-__global__ void __launch_bounds__(256) k_head_dz(HeadPiece G, uint32_t group, HeadStats St, HeadRows R, float t,
-                                                 const HeadScalars* __restrict__ S) {
-    const uint32_t count = S->count, across = (G.ld + 2047) / 2048, row = blockIdx.x / across;
-    const uint32_t p = (blockIdx.x % across * 256 + threadIdx.x) * 8;
-    if (row >= ((count + 63) & ~63u) || p >= G.ld) return;
-    const size_t at = (size_t)row * G.ld + p;
-    uint16_t hi[8] = {}, lo[8] = {};
-    if (row < count) {
-        const RowGradient g = row_gradient(R, row, S->most, t, SOFT);
-        *reinterpret_cast<uint4*>(hi) = *reinterpret_cast<const uint4*>(G.hi + at);
-        if (WIDE) *reinterpret_cast<uint4*>(lo) = *reinterpret_cast<const uint4*>(G.lo + at);
-        const float m = St.m[(size_t)((G.first + p) / group) * St.ld + row];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float z = kept_logit<WIDE>(hi[e], lo[e], m);
-            float d = 0.0f;
-            if (p + e < G.n) d = SOFT ? g.softmaxes(z) : g.c1 * exp_of(z - g.lse);
-            put_dz<E, F32>(d, &hi[e], &lo[e]);
-        }
-    }
-    *reinterpret_cast<uint4*>(G.hi + at) = *reinterpret_cast<const uint4*>(hi);
-    if (F32) *reinterpret_cast<uint4*>(G.lo + at) = *reinterpret_cast<const uint4*>(lo);
+// Entry k of a row's targets (the teacher's, then the label): where it lies in the piece, and its dz, in binary32 from its logit.  False
+// where it lies elsewhere or another entry stands for it.
+template <bool SOFT>
+__device__ __forceinline__ bool target_dz(uint32_t k, const HeadPiece& G, uint32_t row, uint32_t token, int32_t label, const RowGradient& g,
+                                          const HeadRows& R, const Teacher& T, uint32_t* at, float* dz) {
+    const uint32_t top = SOFT ? T.top : 0;
+    const size_t entry = (size_t)token * top + k;
+    const bool teacher = SOFT && k < top;
+    const int32_t j = teacher ? T.index[entry] : label;
+    if (j < 0 || (uint32_t)j - G.first >= G.n) return false;
+    if (SOFT && !teacher && (T.any[token] & 2)) return false;          // an entry of the teacher's is the label: it stands for both
+    const float z = teacher ? T.z[(size_t)row * top + k] : R.z_label[row];
+    float d = SOFT ? g.softmaxes(z) : g.c1 * exp_of(z - g.lse);
+    if (teacher) d -= g.c2 * T.q[entry];
+    if (j == label) d -= g.c1;
+    *at = (uint32_t)j - G.first;
+    *dz = d;
+    return true;
 }
 
-// The label's and the teacher's entries of dz, in binary32 from their logits and rounded once.
+// In place on a kept piece: a workgroup takes 4096 entries of a row, twice eight a thread.  The label's entry is put right here, the
+// teacher's are by k_head_targets.
+constexpr uint32_t DZ_ACROSS = 4096;
+template <class E, bool F32, bool WIDE, bool SOFT>
+__global__ void __launch_bounds__(256) k_head_dz(HeadPiece G, uint32_t group, HeadStats St, HeadRows R, Teacher T,
+                                                 const HeadScalars* __restrict__ S) {
+    const uint32_t count = S->count, across = (G.ld + DZ_ACROSS - 1) / DZ_ACROSS, row = blockIdx.x / across;
+    const uint32_t first = blockIdx.x % across * DZ_ACROSS + threadIdx.x * 8;
+    if (row >= ((count + 63) & ~63u)) return;
+    constexpr int PARTS = DZ_ACROSS / 2048;
+    uint16_t hi[PARTS][8] = {}, lo[PARTS][8] = {};
+    if (row < count) {
+        float m[PARTS] = {};
+#pragma unroll
+        for (int v = 0; v < PARTS; ++v) {
+            const uint32_t p = first + v * 2048;
+            const size_t at = (size_t)row * G.ld + p;
+            if (p < G.ld) {
+                *reinterpret_cast<uint4*>(hi[v]) = *reinterpret_cast<const uint4*>(G.hi + at);
+                if (WIDE) *reinterpret_cast<uint4*>(lo[v]) = *reinterpret_cast<const uint4*>(G.lo + at);
+                else m[v] = St.m[(size_t)((G.first + p) / group) * St.ld + row];
+            }
+        }
+        const RowGradient g = row_gradient(R, row, S->most, T.t, SOFT);
+        const uint32_t label = SOFT ? ~0u : (uint32_t)R.label[row] - G.first;
+#pragma unroll
+        for (int v = 0; v < PARTS; ++v) {
+            const uint32_t p = first + v * 2048;
+            float d[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float z = kept_logit<WIDE>(hi[v][e], lo[v][e], m[v]);
+                d[e] = SOFT ? g.softmaxes(z) : g.c1 * exp_of(z - g.lse);
+                if (p + e >= G.n) d[e] = 0.0f;
+            }
+            if (!SOFT && label - p < 8 && label < G.n) {
+                const float is = g.c1 * exp_of(R.z_label[row] - g.lse) - g.c1;
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e)
+                    if (label - p == e) d[e] = is;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) put_dz<E, F32>(d[e], &hi[v][e], &lo[v][e]);
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < PARTS; ++v) {
+        const uint32_t p = first + v * 2048;
+        const size_t at = (size_t)row * G.ld + p;
+        if (p < G.ld) {
+            *reinterpret_cast<uint4*>(G.hi + at) = *reinterpret_cast<const uint4*>(hi[v]);
+            if (F32) *reinterpret_cast<uint4*>(G.lo + at) = *reinterpret_cast<const uint4*>(lo[v]);
+        }
+    }
+}
+
+// A piece's targets, over the gradient that stands there without them; a wavefront per row.
 template <class E, bool F32, bool SOFT>
-__global__ void __launch_bounds__(256) k_head_targets(HeadPiece G, HeadRows R, Teacher T, float t, const HeadScalars* __restrict__ S) {
-    const uint32_t top = SOFT ? T.top : 0, per = top + 1, count = S->count;
-    for (uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x; at < (uint64_t)count * per; at += (uint64_t)gridDim.x * 256) {
-        const uint32_t row = at / per, k = at % per;
-        const int32_t label = R.label[row];
-        const size_t from = SOFT ? (size_t)R.token[row] * top : 0;
-        const int32_t j = SOFT && k < top ? T.index[from + k] : label;
-        if (j < 0 || (uint32_t)j - G.first >= G.n) continue;
-        const RowGradient g = row_gradient(R, row, S->most, t, SOFT);
-        const float z = SOFT && k < top ? T.z[(size_t)row * top + k] : R.z_label[row];
-        float q = 0.0f;
-        bool listed = false;
-        for (uint32_t v = 0; v < top; ++v)
-            if (T.index[from + v] == j) q += T.q[from + v], listed = true;
-        if (k == top && listed) continue;                  // an entry of the teacher's is the label: it writes for both
-        float d = SOFT ? g.softmaxes(z) - g.c2 * q : g.c1 * exp_of(z - g.lse);
-        if (j == label) d -= g.c1;
+__global__ void __launch_bounds__(256) k_head_targets(HeadPiece G, HeadRows R, Teacher T, const HeadScalars* __restrict__ S) {
+    const uint32_t row = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= S->count) return;
+    const RowGradient g = row_gradient(R, row, S->most, T.t, SOFT);
+    for (uint32_t k = threadIdx.x & 63; k <= (SOFT ? T.top : 0u); k += 64) {
+        uint32_t at;
+        float d;
+        if (!target_dz<SOFT>(k, G, row, R.token[row], R.label[row], g, R, T, &at, &d)) continue;
         uint16_t hi, lo;
         put_dz<E, F32>(d, &hi, &lo);
-        const size_t to = (size_t)row * G.ld + ((uint32_t)j - G.first);
-        G.hi[to] = hi;
-        if (F32) G.lo[to] = lo;
+        G.hi[(size_t)row * G.ld + at] = hi;
+        if (F32) G.lo[(size_t)row * G.ld + at] = lo;
     }
 }
 
@@ -529,11 +721,11 @@ __global__ void __launch_bounds__(256) k_head_targets(HeadPiece G, HeadRows R, T
 // dH, partial sums: workgroups of split s take a stretch of the piece's vocabulary.  sums: [splits, rows, ld].
 template <class E, int BP, int BQ, int WP, int WQ>
 __global__ void __launch_bounds__(WP * WQ * 64) k_head_dh(Operand W, Operand G, uint32_t splits, uint32_t per_split,
-                                                          float* __restrict__ sums, uint32_t ld, bool add,
+                                                          float* __restrict__ sums, uint32_t rows, uint32_t ld, bool add,
                                                           const HeadScalars* __restrict__ S) {
     typedef Product<E, BP, BQ, WP, WQ, true, false> M;
     __shared__ __align__(1024) char lds[M::LDS];
-    const uint32_t count = S->count, rows = G.extent, np = (W.extent + BP - 1) / BP, nq = rows / BQ;
+    const uint32_t count = S->count, np = (W.extent + BP - 1) / BP, nq = G.extent / BQ;
     const uint32_t split = blockIdx.x / (np * nq);
     uint32_t tp, tq;
     tile_of(blockIdx.x - split * np * nq, np, nq, &tp, &tq);
@@ -569,28 +761,45 @@ __device__ __forceinline__ void put(void* out, int64_t at, float x) {
     else static_cast<uint16_t*>(out)[at] = OUT == OUT_BF16 ? Bf16::bits(x) : F16::bits(x);
 }
 
-// dH: the splits' sums in order, times what dz and W were scaled by, to the token's row; zeros for tokens that do not count.
+// dH: the splits' sums in order, times what dz and W were scaled by, to the token's row; zeros for tokens that do not count.  Four
+// entries a thread.
 template <int OUT, bool F32>
 __global__ void __launch_bounds__(256) k_head_dh_out(const float* __restrict__ sums, uint32_t splits, uint32_t rows, uint32_t ld,
-                                                     HeadRows R, uint32_t dim, float scale, void* __restrict__ dh, int64_t ld_dh,
-                                                     const HeadScalars* __restrict__ S) {
-    const uint32_t token = blockIdx.x;
+                                                     HeadRows R, Spread spread, uint32_t tokens, uint32_t dim, float scale, void* __restrict__ dh,
+                                                     int64_t ld_dh, const HeadScalars* __restrict__ S) {
+    const uint32_t token = spread.row(), c = spread.unit() * 4;
+    if (token >= tokens || c >= dim) return;
     const int32_t row = R.row[token];
-    const float factor = scale * S->most * (1.0f / DZ_SCALE), s = F32 ? 1.0f / split_scale(S->w_max) : 1.0f;
-    for (uint32_t c = threadIdx.x; c < dim; c += 256) {
-        float x = 0.0f;
-        if (row >= 0) {
-            for (uint32_t v = 0; v < splits; ++v) x += sums[((size_t)v * rows + row) * ld + c];
-            x = x * s * factor;
+    f32x4 x = {};
+    if (row >= 0) {
+        const float factor = scale * S->most * (1.0f / DZ_SCALE), s = F32 ? 1.0f / split_scale(S->w_max) : 1.0f;
+        const float* from = sums + (size_t)row * ld + c;
+        const size_t step = (size_t)rows * ld;
+        uint32_t v = 0;
+        for (; v + 4 <= splits; v += 4) {
+            f32x4 y[4];
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) y[i] = *reinterpret_cast<const f32x4*>(from + (v + i) * step);
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) x += y[i];
         }
-        put<OUT>(dh, token * ld_dh + c, x);
+        for (; v < splits; ++v) x += *reinterpret_cast<const f32x4*>(from + v * step);
+        x = x * s * factor;
+    }
+    const int64_t to = token * ld_dh + c;
+    if (c + 4 <= dim && OUT == OUT_F32) {
+        *reinterpret_cast<words4*>(static_cast<float*>(dh) + to) = __builtin_bit_cast(words4, x);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < dim) put<OUT>(dh, to + e, x[e]);
     }
 }
 
-// dW of a piece: rows of the vocabulary, summed over the rows of tokens.  wide_rows: every row of dw is 4-byte aligned.
+// dW of a piece: rows of the vocabulary, summed over the rows of tokens.
 template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool F32>
 __global__ void __launch_bounds__(WP * WQ * 64) k_head_dw(Operand H, Operand G, float scale, void* __restrict__ dw, int64_t ld_dw,
-                                                          bool wide_rows, uint32_t first, uint32_t dim, const HeadScalars* __restrict__ S) {
+                                                          uint32_t first, uint32_t dim, const HeadScalars* __restrict__ S) {
     typedef Product<E, BP, BQ, WP, WQ, true, true> M;
     __shared__ __align__(1024) char lds[M::LDS];
     const uint32_t count = S->count, n = G.extent;
@@ -603,8 +812,8 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_dw(Operand H, Operand G, 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t p0 = tp * BP + M::p_of(wave), q0 = tq * BQ + M::q_of(wave);
     const float factor = scale * S->most * (1.0f / DZ_SCALE), s = F32 ? 1.0f / split_scale(S->h_max) : 1.0f;
-    typedef Rows32<OUT == OUT_F32 ? 4 : 2> Out;
-    static_assert(BP / WP == Out::ENTRIES && M::WAVES * Out::BYTES <= M::LDS, "a wavefront's rows");
+    typedef Rows32<OUT == OUT_F32 ? 4 : 2, BP / WP> Out;
+    static_assert(M::WAVES * Out::BYTES <= M::LDS, "a wavefront's rows");
     char* mine = lds + wave * Out::BYTES;
     constexpr uint32_t SIZE = OUT == OUT_F32 ? 4 : 2;
 #pragma unroll
@@ -622,14 +831,12 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_dw(Operand H, Operand G, 
                     for (int e = 0; e < 4; ++e) four |= (uint64_t)(OUT == OUT_BF16 ? Bf16::bits(v[e]) : F16::bits(v[e])) << (16 * e);
                 Out::put(mine, a * 32 + p_in_fragment(c * 4, lane), lane, OUT == OUT_F32 ? (const void*)&v : (const void*)&four);
             }
-        // 128-bit stores need no more than 4-byte alignment
         Out::each(mine, lane, [&](uint32_t row, uint32_t p, uint4 v) {
             const uint32_t q = q0 + b * 32 + row;
             if (q >= n || p0 + p >= dim) return;
             char* to = static_cast<char*>(dw) + ((int64_t)(first + q) * ld_dw + p0 + p) * SIZE;
-            if (p0 + p + Out::PER_CHUNK <= dim && (OUT == OUT_F32 || wide_rows)) {
-                typedef uint32_t quad_any __attribute__((ext_vector_type(4), aligned(4)));
-                *reinterpret_cast<quad_any*>(to) = quad_any{v.x, v.y, v.z, v.w};
+            if (p0 + p + Out::PER_CHUNK <= dim) {
+                *reinterpret_cast<words4_any*>(to) = words4_any{v.x, v.y, v.z, v.w};
             } else {
                 const uint32_t word[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll

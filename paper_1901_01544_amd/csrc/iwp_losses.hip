@@ -13,9 +13,38 @@ using namespace iwp;
 
 namespace {
 
-constexpr uint32_t TILE_ROWS = 256, TILE_VOCAB = 256;
-constexpr uint32_t GROUP = 128;                    // vocabulary entries that share a largest logit and a sum
+constexpr uint32_t TILE_VOCAB = 256;                 // pieces of the vocabulary start and end at multiples of the largest tile
 constexpr uint32_t CUS = 256;
+
+// Tiles of the products.  GROUP: vocabulary entries of a wavefront, which share a largest logit and a sum; RESIDENT: workgroups that a
+// compute unit holds at a time.
+struct Big { static constexpr int BP = 256, BQ = 256, WP = 2, WQ = 4, THREADS = 512, GROUP = BP / WP, RESIDENT = 1; };
+struct Mid { static constexpr int BP = 128, BQ = 128, WP = 2, WQ = 2, THREADS = 256, GROUP = BP / WP; };
+struct Few { static constexpr int BP = 64, BQ = 64, WP = 2, WQ = 2, THREADS = 256, GROUP = BP / WP, RESIDENT = 4; };
+enum TileKind { BIG, MID, FEW };
+
+#ifndef BIG_FROM
+#define BIG_FROM 160
+#define MID_FROM 160
+#endif
+template <class T>
+uint32_t tiles_of(uint32_t np, uint32_t nq) { return (np + T::BP - 1) / T::BP * ((nq + T::BQ - 1) / T::BQ); }
+
+// The largest tile that still gives the chip's compute units something to do.
+TileKind tile_for(uint32_t np, uint32_t nq) {
+    if (tiles_of<Big>(np, nq) >= BIG_FROM) return BIG;
+    return tiles_of<Mid>(np, nq) >= MID_FROM ? MID : FEW;
+}
+
+// f(tile) with the tile's type
+template <class F>
+int with_tile(TileKind kind, F f) {
+    switch (kind) {
+        case BIG: return f(Big{});
+        case MID: return f(Mid{});
+        default: return f(Few{});
+    }
+}
 
 struct Carver {            // hands out 256-byte aligned parts; at == nullptr: only adds up
     char* at;
@@ -38,7 +67,8 @@ struct HeadPlan {
     uint32_t tokens, dim, vocab, dtype, top, piece, pieces;
     uint32_t rows;         // tokens, rounded up to a tile
     uint32_t dim_padded;   // dim, rounded up to the LDS tile
-    uint32_t ld_logits, ld_sums, splits, per_split, groups;
+    uint32_t ld_logits, ld_sums, splits, per_split, group, groups;
+    TileKind logits_tile, dh_tile;
     bool f32, wide, copy_w;
 
     HeadScalars* scalars;
@@ -50,6 +80,14 @@ struct HeadPlan {
     size_t bytes;
 };
 
+Spread spread(uint32_t units) {
+    Spread s{0, 1};
+    while (s.shift < 8 && (1u << s.shift) < units) ++s.shift;
+    s.across = (units + (1u << s.shift) - 1) >> s.shift;
+    return s;
+}
+uint32_t blocks_of(const Spread& s, uint32_t rows) { return (rows + (256u >> s.shift) - 1) / (256u >> s.shift) * s.across; }
+
 bool readable(const void* w, int64_t ld_w, uint32_t dim, uint32_t dtype) {
     return dtype != IWP_F32 && aligned(w, 16) && ld_w % 8 == 0 && dim % 8 == 0;
 }
@@ -60,19 +98,25 @@ HeadPlan head_plan(uint32_t tokens, uint32_t dim, uint32_t vocab, uint32_t dtype
                    void* workspace) {
     HeadPlan p{};
     p.tokens = tokens; p.dim = dim; p.vocab = vocab; p.dtype = dtype; p.top = top; p.copy_w = copy_w;
+    p.T.t = 1.0f;
     p.f32 = dtype == IWP_F32;
     p.wide = dtype != IWP_BF16;
     p.piece = piece == 0 || piece >= vocab ? vocab : std::min(vocab, round_up(piece, TILE_VOCAB));
     p.pieces = (vocab + p.piece - 1) / p.piece;
-    p.rows = round_up(std::max(tokens, 1u), TILE_ROWS);
+    p.rows = round_up(std::max(tokens, 1u), tokens <= Few::BQ ? (uint32_t)Few::BQ : (uint32_t)Big::BQ);
     p.dim_padded = round_up(dim, BK);
     p.ld_logits = round_up(p.piece, TILE_VOCAB);
     p.ld_sums = copy_w ? p.dim_padded : dim;
-    p.groups = (uint32_t)(((uint64_t)p.pieces * p.ld_logits + GROUP - 1) / GROUP);
-    // dH has few tiles and a long sum: its vocabulary is split until every compute unit has a tile, at least 8 LDS tiles each
-    const uint32_t tiles = (p.rows / TILE_ROWS) * ((dim + 255) / 256), steps = (p.piece + BK - 1) / BK;
-    p.splits = std::max(1u, std::min({(CUS + tiles - 1) / tiles, steps / 8, MAX_SPLITS}));
-    p.per_split = round_up((steps + p.splits - 1) / p.splits, 1u) * BK;
+    p.logits_tile = p.rows < Big::BQ ? FEW : tile_for(p.piece, p.tokens);   // a tile's rows are all written
+    p.group = p.logits_tile == BIG ? Big::GROUP : p.logits_tile == MID ? Mid::GROUP : Few::GROUP;
+    p.groups = (uint32_t)(((uint64_t)p.pieces * p.ld_logits + p.group - 1) / p.group);
+    // dH has few tiles and a long sum: its vocabulary is split until the compute units are full, at least 8 LDS tiles each
+    const uint32_t steps = (p.piece + BK - 1) / BK;
+    p.dh_tile = tokens <= Few::BQ ? FEW : BIG;
+    const uint32_t tiles = std::max(1u, p.dh_tile == FEW ? tiles_of<Few>(dim, tokens) : tiles_of<Big>(dim, tokens));
+    const uint32_t room = CUS * (p.dh_tile == FEW ? Few::RESIDENT : Big::RESIDENT);
+    p.splits = std::max(1u, std::min({(room + tiles - 1) / tiles, steps / 8, MAX_SPLITS}));
+    p.per_split = (steps + p.splits - 1) / p.splits * BK;
 
     Carver c{static_cast<char*>(workspace)};
     c.take(p.scalars, 1);
@@ -95,6 +139,11 @@ HeadPlan head_plan(uint32_t tokens, uint32_t dim, uint32_t vocab, uint32_t dtype
         c.take(p.T.entropy, tokens);
         c.take(p.T.any, tokens);
         p.T.top = top;
+        p.T.width = TILE_VOCAB;
+        while ((vocab + p.T.width - 1) / p.T.width > STRETCHES) p.T.width *= 2;
+        p.T.stretches = (vocab + p.T.width - 1) / p.T.width;
+        c.take(p.T.start, (size_t)((tokens + 63) / 64) * (p.T.stretches + 1));
+        c.take(p.T.found, (size_t)((tokens + 63) / 64) * 64 * top);
     }
     c.take(p.h_hi, (size_t)p.rows * p.dim_padded);
     if (p.f32) c.take(p.h_lo, (size_t)p.rows * p.dim_padded);
@@ -125,52 +174,57 @@ struct HeadCall {
     hipStream_t s;
 };
 
-struct KindF32 { typedef F16 E; typedef F32Element V; static constexpr bool F32 = true, WIDE = true; static constexpr int OUT = OUT_F32; };
-struct KindBf16 { typedef Bf16 E; typedef Bf16 V; static constexpr bool F32 = false, WIDE = false; static constexpr int OUT = OUT_BF16; };
-struct KindF16 { typedef F16 E; typedef F16 V; static constexpr bool F32 = false, WIDE = true; static constexpr int OUT = OUT_F16; };
-
-struct Big { static constexpr int BP = 256, BQ = 256, WP = 2, WQ = 4, THREADS = 512; };
+struct KindF32 { typedef F16 E; static constexpr bool F32 = true, WIDE = true; static constexpr int OUT = OUT_F32; };
+struct KindBf16 { typedef Bf16 E; static constexpr bool F32 = false, WIDE = false; static constexpr int OUT = OUT_BF16; };
+struct KindF16 { typedef F16 E; static constexpr bool F32 = false, WIDE = true; static constexpr int OUT = OUT_F16; };
 
 template <class K, class T, int MODE, bool SOFT>
-int launch_logits(const HeadPlan& p, const HeadCall& c, const Operand& W, const Operand& H, const HeadPiece& G) {
-    static_assert(T::BP / T::WP == GROUP, "a wavefront has a group");
-    const uint32_t tiles = (G.n + T::BP - 1) / T::BP * (p.rows / T::BQ);
+int launch_logits(const HeadPlan& p, const HeadCall& c, const Operand& W, Operand H, const HeadPiece& G) {
+    H.extent = round_up(std::max(p.tokens, 1u), (uint32_t)T::BQ);
     auto kernel = k_head_logits<typename K::E, T::BP, T::BQ, T::WP, T::WQ, MODE, K::F32, K::WIDE, SOFT>;
-    IWP_LAUNCH_BLOCK("k_head_logits", kernel, tiles, T::THREADS, c.s, W, H, p.dim_padded, G, p.R, p.St, c.temperature, p.scalars);
+    IWP_LAUNCH_BLOCK("k_head_logits", kernel, tiles_of<T>(G.n, H.extent), T::THREADS, c.s, W, H, p.dim_padded, G, p.R, p.St, p.T, p.scalars);
     return IWP_OK;
 }
 
-template <class K, class T, int OUT>
+template <class K, int OUT>
 int launch_dw(const HeadPlan& p, const HeadCall& c, const Operand& H, const Operand& G, uint32_t first) {
-    const uint32_t tiles = (p.dim + T::BP - 1) / T::BP * ((G.extent + T::BQ - 1) / T::BQ);
-    auto kernel = k_head_dw<typename K::E, T::BP, T::BQ, T::WP, T::WQ, OUT, K::F32>;
-    IWP_LAUNCH_BLOCK("k_head_dw", kernel, tiles, T::THREADS, c.s, H, G, c.scale, c.dw, c.ld_dw,
-                     aligned(c.dw, 4) && c.ld_dw % 2 == 0, first, p.dim, p.scalars);
+    return with_tile(tile_for(p.dim, G.extent), [&](auto tile) {
+        typedef decltype(tile) T;
+        auto kernel = k_head_dw<typename K::E, T::BP, T::BQ, T::WP, T::WQ, OUT, K::F32>;
+        IWP_LAUNCH_BLOCK("k_head_dw", kernel, tiles_of<T>(p.dim, G.extent), T::THREADS, c.s, H, G, c.scale, c.dw, c.ld_dw, first, p.dim, p.scalars);
+        return (int)IWP_OK;
+    });
+}
+
+template <class K, class T>
+int launch_dh(const HeadPlan& p, const HeadCall& c, const Operand& W, Operand G, bool add) {
+    G.extent = round_up(p.tokens, (uint32_t)T::BQ);
+    auto kernel = k_head_dh<typename K::E, T::BP, T::BQ, T::WP, T::WQ>;
+    IWP_LAUNCH_BLOCK("k_head_dh", kernel, tiles_of<T>(W.extent, G.extent) * p.splits, T::THREADS, c.s, W, G, p.splits, p.per_split, p.sums,
+                     p.rows, p.ld_sums, add, p.scalars);
     return IWP_OK;
 }
 
 template <class K, bool SOFT>
 int head(const HeadPlan& p, const HeadCall& c) {
-    typedef Big T;
     const uint32_t tokens = std::max(p.tokens, 1u);        // grids: without tokens, the weight's gradient is still written
-    Teacher teacher = p.T;
-    teacher.t = c.temperature;
-    if (SOFT) IWP_LAUNCH_BLOCK("k_head_teacher", k_head_teacher, (tokens + 3) / 4, 256, c.s, c.top_index, c.top_logit, p.tokens,
-                               p.vocab, teacher);
+    if (SOFT) IWP_LAUNCH_BLOCK("k_head_teacher", k_head_teacher, (tokens + 3) / 4, 256, c.s, c.top_index, c.top_logit, c.target, p.tokens,
+                               p.vocab, p.T);
     IWP_LAUNCH_BLOCK("k_head_rows", k_head_rows, 1, 1024, c.s, c.target, c.weight, SOFT ? p.T.any : nullptr, p.tokens, p.vocab, c.hard,
                      c.soft, c.temperature, p.R, c.loss, p.scalars);
-    const uint32_t* count = &p.scalars->count;
+    if (SOFT) IWP_LAUNCH_BLOCK("k_head_sort", k_head_sort, (tokens + 63) / 64, 1024, c.s, p.R, p.T, p.scalars);
+    const HeadMatrix h{c.h, c.ld_h, p.tokens, p.dim, p.R.token, &p.scalars->count}, w{c.w, c.ld_w, p.vocab, p.dim, nullptr, nullptr};
     if (K::F32) {
-        IWP_LAUNCH_BLOCK("k_head_max", k_head_max, std::min(tokens, 1024u), 256, c.s, static_cast<const float*>(c.h), c.ld_h, 0u, p.dim,
-                         p.R.token, count, &p.scalars->h_max);
-        IWP_LAUNCH_BLOCK("k_head_max", k_head_max, std::min(p.vocab, 2048u), 256, c.s, static_cast<const float*>(c.w), c.ld_w, p.vocab, p.dim,
-                         (const uint32_t*)nullptr, (const uint32_t*)nullptr, &p.scalars->w_max);
+        auto blocks = [&](uint32_t rows, uint32_t most) { return std::max(1u, std::min((rows + 15) / 16 * ((p.dim + 1023) / 1024), most)); };
+        const uint32_t hb = blocks(p.tokens, 64), wb = blocks(p.vocab, 256);
+        IWP_LAUNCH_BLOCK("k_head_max", k_head_max, hb + wb, 1024, c.s, h, w, hb, p.scalars);
     }
-    IWP_LAUNCH_BLOCK("k_head_pack", k_head_pack<K::F32>, std::min(p.rows, 4096u), 256, c.s, c.h, c.ld_h, 0u, p.dim, p.R.token, count,
-                     &p.scalars->h_max, p.h_hi, p.h_lo, p.dim_padded);
+    const Spread packed = spread(p.dim_padded / 8);
+    IWP_LAUNCH_BLOCK("k_head_pack", k_head_pack<K::F32>, blocks_of(packed, (p.rows + PACK_ROWS - 1) / PACK_ROWS), 256, c.s, h, packed, &p.scalars->h_max, p.h_hi, p.h_lo,
+                     p.dim_padded);
     if (p.copy_w)
-        IWP_LAUNCH_BLOCK("k_head_pack", k_head_pack<K::F32>, std::min(p.vocab, 8192u), 256, c.s, c.w, c.ld_w, p.vocab, p.dim,
-                         (const uint32_t*)nullptr, (const uint32_t*)nullptr, &p.scalars->w_max, p.w_hi, p.w_lo, p.dim_padded);
+        IWP_LAUNCH_BLOCK("k_head_pack", k_head_pack<K::F32>, blocks_of(packed, (p.vocab + PACK_ROWS - 1) / PACK_ROWS), 256, c.s, w, packed, &p.scalars->w_max, p.w_hi, p.w_lo,
+                         p.dim_padded);
     const uint16_t* w_hi = p.copy_w ? p.w_hi : static_cast<const uint16_t*>(c.w);
     const size_t ld_w = p.copy_w ? p.dim_padded : (size_t)c.ld_w;
     const uint32_t dim_w = p.copy_w ? p.dim_padded : p.dim;
@@ -186,49 +240,51 @@ int head(const HeadPlan& p, const HeadCall& c) {
     int rc;
     for (uint32_t i = 0; i < p.pieces; ++i) {
         const HeadPiece G = piece(i);
-        rc = i + 1 == p.pieces && gradients ? launch_logits<K, T, STATISTICS_KEPT, SOFT>(p, c, weight(G), H, G)
-                                            : launch_logits<K, T, STATISTICS, SOFT>(p, c, weight(G), H, G);
+        rc = with_tile(p.logits_tile, [&](auto tile) {
+            typedef decltype(tile) T;
+            return i + 1 == p.pieces && gradients ? launch_logits<K, T, STATISTICS_KEPT, SOFT>(p, c, weight(G), H, G)
+                                                  : launch_logits<K, T, STATISTICS, SOFT>(p, c, weight(G), H, G);
+        });
         if (rc) return rc;
     }
-    if (SOFT)
-        IWP_LAUNCH_BLOCK("k_head_picked", k_head_picked<typename K::V>, (uint32_t)std::min<uint64_t>(((uint64_t)tokens * p.top + 3) / 4, 65536u),
-                         256, c.s, c.h, c.ld_h, c.w, c.ld_w, p.dim, p.R, teacher, p.scalars);
-    const uint32_t groups = (p.vocab + GROUP - 1) / GROUP;
-    IWP_LAUNCH_BLOCK("k_head_join", k_head_join<SOFT>, (tokens + 31) / 32, 256, c.s, p.St, groups, p.R, teacher, c.loss, p.scalars);
+    const uint32_t groups = (p.vocab + p.group - 1) / p.group;
+    IWP_LAUNCH_BLOCK("k_head_join", k_head_join<SOFT>, (tokens + 15) / 16, 512, c.s, p.St, groups, p.R, p.T, c.loss, p.scalars);
     if (!gradients) return IWP_OK;
     for (uint32_t i = p.pieces; i-- > 0;) {
         const HeadPiece G = piece(i);
         const bool kept = i + 1 == p.pieces;
         if (kept) {
             auto kernel = k_head_dz<typename K::E, K::F32, K::WIDE, SOFT>;
-            IWP_LAUNCH_BLOCK("k_head_dz", kernel, (p.ld_logits + 2047) / 2048 * p.rows, 256, c.s, G, GROUP, p.St, p.R,
-                             c.temperature, p.scalars);
-        } else if ((rc = launch_logits<K, T, GRADIENT, SOFT>(p, c, weight(G), H, G))) {
-            return rc;
+            IWP_LAUNCH_BLOCK("k_head_dz", kernel, (p.ld_logits + DZ_ACROSS - 1) / DZ_ACROSS * p.rows, 256, c.s, G, p.group, p.St, p.R, p.T,
+                             p.scalars);
+        } else {
+            rc = p.rows < Big::BQ ? launch_logits<K, Few, GRADIENT, SOFT>(p, c, weight(G), H, G)
+                                  : launch_logits<K, Big, GRADIENT, SOFT>(p, c, weight(G), H, G);
+            if (rc) return rc;
         }
-        auto targets = k_head_targets<typename K::E, K::F32, SOFT>;
-        IWP_LAUNCH_BLOCK("k_head_targets", targets, (uint32_t)std::min<uint64_t>(((uint64_t)tokens * (p.top + 1) + 255) / 256, 65536u), 256,
-                         c.s, G, p.R, teacher, c.temperature, p.scalars);
+        if (SOFT || !kept) {
+            auto targets = k_head_targets<typename K::E, K::F32, SOFT>;
+            IWP_LAUNCH_BLOCK("k_head_targets", targets, (tokens + 3) / 4, 256, c.s, G, p.R, p.T, p.scalars);
+        }
         const uint16_t* g_lo = K::F32 ? p.g_lo : nullptr;
-        if (c.dh) {
+        if (c.dh && p.tokens) {
             Operand W = weight(G);
             W.extent = dim_w;
             W.summed = G.n;
-            const Operand dz{p.g_hi, g_lo, p.ld_logits, p.rows, p.ld_logits};
-            const uint32_t tiles = (dim_w + T::BP - 1) / T::BP * (p.rows / T::BQ);
-            auto kernel = k_head_dh<typename K::E, T::BP, T::BQ, T::WP, T::WQ>;
-            IWP_LAUNCH_BLOCK("k_head_dh", kernel, tiles * p.splits, T::THREADS, c.s, W, dz, p.splits, p.per_split, p.sums, p.ld_sums, !kept,
-                             p.scalars);
+            const Operand dz{p.g_hi, g_lo, p.ld_logits, 0u, p.ld_logits};
+            rc = p.dh_tile == FEW ? launch_dh<K, Few>(p, c, W, dz, !kept) : launch_dh<K, Big>(p, c, W, dz, !kept);
+            if (rc) return rc;
         }
         if (c.dw) {
             const Operand Hc{p.h_hi, p.h_lo, p.dim_padded, p.dim_padded, 0u}, dz{p.g_hi, g_lo, p.ld_logits, G.n, 0u};
-            rc = c.dw_dtype == IWP_F32 ? launch_dw<K, T, OUT_F32>(p, c, Hc, dz, G.first) : launch_dw<K, T, K::OUT>(p, c, Hc, dz, G.first);
+            rc = c.dw_dtype == IWP_F32 ? launch_dw<K, OUT_F32>(p, c, Hc, dz, G.first) : launch_dw<K, K::OUT>(p, c, Hc, dz, G.first);
             if (rc) return rc;
         }
     }
+    const Spread out = spread((p.dim + 3) / 4);
     if (c.dh && p.tokens)
-        IWP_LAUNCH_BLOCK("k_head_dh_out", (k_head_dh_out<K::OUT, K::F32>), tokens, 256, c.s, p.sums, p.splits, p.rows, p.ld_sums, p.R, p.dim,
-                         c.scale, c.dh, c.ld_dh, p.scalars);
+        IWP_LAUNCH_BLOCK("k_head_dh_out", (k_head_dh_out<K::OUT, K::F32>), blocks_of(out, p.tokens), 256, c.s, p.sums, p.splits, p.rows,
+                         p.ld_sums, p.R, out, p.tokens, p.dim, c.scale, c.dh, c.ld_dh, p.scalars);
     return IWP_OK;
 }
 
@@ -247,7 +303,8 @@ int head_call(const HeadCall& c, uint32_t tokens, uint32_t dim, uint32_t vocab, 
         !aligned(c.target, 4) || !aligned(c.weight, 4) || !aligned(c.top_index, 4) || !aligned(c.top_logit, 4) || !aligned(workspace, 256))
         return IWP_EALIGN;
     if (tokens == 0 && !c.dw) return IWP_OK;
-    const HeadPlan p = head_plan(tokens, dim, vocab, dtype, !readable(c.w, c.ld_w, dim, dtype), top, piece, workspace);
+    HeadPlan p = head_plan(tokens, dim, vocab, dtype, !readable(c.w, c.ld_w, dim, dtype), top, piece, workspace);
+    p.T.t = c.temperature;
     if (!workspace || workspace_bytes < p.bytes) return IWP_EWORKSPACE;
     if (top) {
         if (dtype == IWP_F32) return head<KindF32, true>(p, c);

@@ -51,8 +51,9 @@ struct Operand {
 
 // 16 bytes per lane from `base` + the lane's offset straight to LDS, lane after lane from `lds` (uniform) on.  In assembly,
 // because the compiler waits for such loads before any transposing read, of whichever tile; wait_for_loads() waits for them.
+// (m0 is no register that the compiler keeps anything in: it sets it where an instruction of its own needs it.)
 __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
 }
 // Until at most LEFT of this wavefront's loads are on their way and all of its LDS reads are done.
 template <int LEFT>
@@ -270,18 +271,24 @@ struct Product {
 // Register r of a fragment: entry of P inside the fragment's 32 (the entry of Q is lane & 31).
 __device__ __forceinline__ uint32_t p_in_fragment(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
 
-// A wavefront's way from accumulators to memory: 32 rows (entries of Q) of 128 entries of P, through LDS, so that a store instruction
-// writes whole rows of 256 bytes and more.  As the matrix instructions leave them, a lane holds four entries of a row and neighbouring
+// A wavefront's way from accumulators to memory: 32 rows (entries of Q) of its entries of P, through LDS, so that a store instruction
+// writes whole stretches of rows.  As the matrix instructions leave them, a lane holds four entries of a row and neighbouring
 // lanes neighbouring rows.  Chunks of 16 bytes are turned by the row, which keeps both sides off each other's banks.
-template <int SIZE>        // bytes per entry: 2 or 4
+template <int SIZE, int ENTRIES>                   // bytes per entry: 2 or 4
 struct Rows32 {
-    static constexpr int ENTRIES = 128, CHUNKS = ENTRIES * SIZE / 16, BYTES = 32 * ENTRIES * SIZE, PER_CHUNK = 16 / SIZE;
-    static __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t chunk) { return (row * CHUNKS + (chunk ^ (row & 15u))) * 16; }
+    static constexpr int CHUNKS = ENTRIES * SIZE / 16, BYTES = 32 * ENTRIES * SIZE, PER_CHUNK = 16 / SIZE;
+    static constexpr uint32_t TURNS = CHUNKS < 16 ? CHUNKS : 16;
+    static __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t chunk) {
+        return (row * CHUNKS + (chunk ^ (row & (TURNS - 1)))) * 16;
+    }
     // four entries from p on (a multiple of 4) of this lane's row
     static __device__ __forceinline__ void put(char* lds, uint32_t p, int lane, const void* four) {
         char* to = lds + place(lane & 31, p / PER_CHUNK) + (p % PER_CHUNK) * SIZE;
         if (SIZE == 2) *reinterpret_cast<uint64_t*>(to) = *static_cast<const uint64_t*>(four);
         else *reinterpret_cast<f32x4*>(to) = *static_cast<const f32x4*>(four);
+    }
+    static __device__ __forceinline__ float value(const char* lds, uint32_t row, uint32_t p) {      // of 4 bytes
+        return *reinterpret_cast<const float*>(lds + place(row, p / 4) + (p % 4) * 4);
     }
     // store(row, first entry, 16 bytes) for every chunk
     template <class F>
