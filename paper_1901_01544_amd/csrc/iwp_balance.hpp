@@ -22,85 +22,226 @@ struct BalanceSums {
     uint32_t* tokens_all;
 };
 
-template <int IN>
-__device__ __forceinline__ float router_logit(const void* x, int64_t at) {
-    if (IN == OUT_F32) return static_cast<const float*>(x)[at];
-    const uint16_t b = static_cast<const uint16_t*>(x)[at];
-    return IN == OUT_BF16 ? Bf16::value(b) : F16::value(b);
-}
-
 // exp(d) 2^40 for d <= 0, a normal number down to exp(d) of 2^-166: the gradient, which is proportional to it, is rounded once.
 __device__ __forceinline__ float exp_raised(float d) {
     const float t = fmaxf(d * LOG2E, -300.0f), n = rintf(t);
     return ldexpf(exp2_fast(t - n), (int)n + 40);
 }
 
-// One token: its exponentials in place of its logits (lane + 64 v), what they take to be probabilities, its L; false if it does not
-// count.
-template <int NV>
-__device__ __forceinline__ bool token_softmax(float (&x)[NV], float* by, float* log_sum) {
-    float m = -INFINITY;
-    bool nan = false;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        nan |= x[v] != x[v];
-        m = fmaxf(m, x[v]);
+// A token's experts over `lanes` lanes (a power of two), CHUNKS times 16 bytes each: chunk c of lane l starts at expert
+// (c lanes + l) WIDTH.  A wavefront has 64 / lanes tokens at a time.
+template <int IN, int CHUNKS>
+struct TokenLanes {
+    static constexpr int WIDTH = IN == OUT_F32 ? 4 : 8, N = CHUNKS * WIDTH;
+    uint32_t experts, lanes, lane, of;                 // of: which of the wavefront's tokens
+    __device__ __forceinline__ TokenLanes(uint32_t experts, uint32_t lanes) : experts(experts), lanes(lanes) {
+        lane = threadIdx.x & (lanes - 1);
+        of = (threadIdx.x & 63) / lanes;
     }
-    for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    if (__ballot(nan)) m = NAN;
-    if (m == -INFINITY) return false;
-    float s = 0.0f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        x[v] = exp_raised(x[v] - m);
-        s += x[v];
-    }
-    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
-    *by = 1.0f / s;
-    *log_sum = m + logf(s * 0x1p-40f);
-    return true;
-}
+    __device__ __forceinline__ uint32_t tokens() const { return 64 / lanes; }
+    __device__ __forceinline__ uint32_t first(int c) const { return (c * lanes + lane) * WIDTH; }
+    __device__ __forceinline__ uint32_t expert(int i) const { return first(i / WIDTH) + i % WIDTH; }
 
-template <int IN, int NV>
-__device__ __forceinline__ void token_logits(const void* x, int64_t row, uint32_t experts, int lane, float (&out)[NV]) {
+    __device__ __forceinline__ void load(const void* x, int64_t at, words4 (&v)[CHUNKS]) const {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) out[v] = lane + 64 * v < (int)experts ? router_logit<IN>(x, row + lane + 64 * v) : -INFINITY;
-}
-
-template <int IN, int NV>
-__global__ void __launch_bounds__(256) k_balance_rows(const void* __restrict__ x, int64_t ld, uint32_t tokens, uint32_t experts,
-                                                      const int32_t* __restrict__ chosen, uint32_t slots,
-                                                      const uint8_t* __restrict__ keep, BalanceSums B) {
-    __shared__ uint32_t of_expert[IWP_MAX_EXPERTS];
-    __shared__ float sums[4][64 * NV];
-    __shared__ float squares[4];
-    __shared__ uint32_t counted[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (uint32_t e = threadIdx.x; e < experts; e += 256) of_expert[e] = 0;
-    __syncthreads();
-    float p[NV] = {}, square = 0.0f;
-    uint32_t n = 0;
-    for (uint32_t i = blockIdx.x * 4 + wave; i < tokens; i += gridDim.x * 4) {
-        if (keep && !keep[i]) continue;
-        float y[NV], by, log_sum;
-        token_logits<IN, NV>(x, (int64_t)i * ld, experts, lane, y);
-        if (!token_softmax<NV>(y, &by, &log_sum)) continue;
+        for (int c = 0; c < CHUNKS; ++c) {
+            const uint32_t e0 = first(c);
+            if (IN == OUT_F32) {
+                const float* p = static_cast<const float*>(x) + at + e0;
+                if (e0 + WIDTH <= experts) {
+                    v[c] = *reinterpret_cast<const words4*>(p);
+                } else {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) p[v] += y[v] * by;
-        square += log_sum * log_sum;
-        ++n;
-        for (uint32_t k = lane; k < slots; k += 64) {
-            const uint32_t e = chosen[(size_t)i * slots + k];
-            if (e < experts) atomicAdd(&of_expert[e], 1u);
+                    for (uint32_t e = 0; e < 4; ++e) v[c][e] = e0 + e < experts ? __float_as_uint(p[e]) : 0xff800000u;
+                }
+            } else {
+                const uint16_t* p = static_cast<const uint16_t*>(x) + at + e0;
+                const uint32_t none = IN == OUT_BF16 ? 0xff80u : 0xfc00u;              // -inf
+                if (e0 + WIDTH <= experts) {
+                    v[c] = (words4)*reinterpret_cast<const words4_any*>(p);
+                } else {
+#pragma unroll
+                    for (uint32_t e = 0; e < 8; e += 2)
+                        v[c][e / 2] = (e0 + e < experts ? p[e] : none) | (e0 + e + 1 < experts ? p[e + 1] : none) << 16;
+                }
+            }
         }
     }
+    static __device__ __forceinline__ void unpack(const words4 (&v)[CHUNKS], float (&y)[N]) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) sums[wave][lane + 64 * v] = p[v];
-    if (lane == 0) squares[wave] = square, counted[wave] = n;
+        for (int i = 0; i < N; ++i) {
+            if (IN == OUT_F32) y[i] = __uint_as_float(v[i / 4 % CHUNKS][i % 4]);
+            else {
+                const uint16_t b = (uint16_t)(v[i / 8 % CHUNKS][i % 8 / 2] >> (i % 2 * 16));
+                y[i] = IN == OUT_BF16 ? Bf16::value(b) : F16::value(b);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(void* out, int64_t at, const float (&y)[N]) const {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const uint32_t e0 = first(c);
+            words4 v;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                if (IN == OUT_F32) v[w] = __float_as_uint(y[c * WIDTH % N + w]);
+                else {
+                    const float a = y[(c * WIDTH + 2 * w) % N], b = y[(c * WIDTH + 2 * w + 1) % N];
+                    v[w] = IN == OUT_BF16 ? Bf16::bits(a) | (uint32_t)Bf16::bits(b) << 16 : F16::bits(a) | (uint32_t)F16::bits(b) << 16;
+                }
+            }
+            if (e0 + WIDTH <= experts) {
+                if (IN == OUT_F32) *reinterpret_cast<words4*>(static_cast<float*>(out) + at + e0) = v;
+                else *reinterpret_cast<words4_any*>(static_cast<uint16_t*>(out) + at + e0) = v;
+            } else {
+#pragma unroll
+                for (int e = 0; e < WIDTH; ++e)
+                    if (e0 + e < experts) put<IN>(out, at + e0 + e, y[c * WIDTH + e]);
+            }
+        }
+    }
+    __device__ __forceinline__ float sum(float s) const {
+        for (uint32_t o = lanes / 2; o; o >>= 1) s += __shfl_xor(s, o);
+        return s;
+    }
+    // A token's exponentials in place of its logits, what they take to be probabilities, its L; false where all logits are -inf.
+    __device__ __forceinline__ bool softmax(float (&x)[N], float* by, float* log_sum) const {
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < N; ++i) m = x[i] != x[i] ? INFINITY : fmaxf(m, x[i]);    // NaN as infinity: the whole token is NaN
+        for (uint32_t o = lanes / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+        float s = 0.0f;
+        const float from = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            x[i] = exp_raised(x[i] - from);
+            s += x[i];
+        }
+        s = sum(s);
+        *by = 1.0f / s;
+        *log_sum = m + logf(s * 0x1p-40f);
+        return m != -INFINITY;
+    }
+};
+
+struct Router {
+    const void* x;
+    int64_t ld;
+    uint32_t tokens, experts, lanes, slots;
+    const int32_t* chosen;
+    const uint8_t* keep;
+};
+struct BalanceGradient {
+    float balance, z;
+    void* dx;
+    int64_t ld;
+};
+
+// Sums over the tokens that wavefront `wave` of `waves` takes.
+template <int IN, int CHUNKS>
+__device__ __forceinline__ void balance_sums(const Router& r, uint32_t wave, uint32_t waves, uint32_t* of_expert,
+                                             float (&p)[TokenLanes<IN, CHUNKS>::N], float* square, uint32_t* n) {
+    typedef TokenLanes<IN, CHUNKS> L;
+    const L l(r.experts, r.lanes);
+    const uint32_t at_once = l.tokens(), stride = waves * at_once;
+    words4 next[CHUNKS] = {};
+    bool next_in = false;
+    uint32_t i = wave * at_once + l.of;
+    auto request = [&](uint32_t i) {
+        next_in = i < r.tokens && !(r.keep && !r.keep[i]);
+        if (next_in) l.load(r.x, (int64_t)i * r.ld, next);
+    };
+    request(i);
+    for (uint32_t base = wave * at_once; base < r.tokens; base += stride, i += stride) {
+        words4 now[CHUNKS];
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) now[c] = next[c];
+        bool in = next_in;
+        request(i + stride);
+        float y[L::N], by, log_sum;
+        L::unpack(now, y);
+        in = l.softmax(y, &by, &log_sum) && in;
+        if (!in) continue;
+#pragma unroll
+        for (int v = 0; v < L::N; ++v) p[v] += y[v] * by;
+        if (l.lane == 0) {
+            *square += log_sum * log_sum;
+            ++*n;
+        }
+        for (uint32_t k = l.lane; k < r.slots; k += r.lanes) {
+            const uint32_t e = r.chosen[(size_t)i * r.slots + k];
+            if (e < r.experts) atomicAdd(&of_expert[e], 1u);
+        }
+    }
+    // over the wavefront's tokens
+    for (uint32_t o = r.lanes; o < 64; o <<= 1) {
+#pragma unroll
+        for (int v = 0; v < L::N; ++v) p[v] += __shfl_xor(p[v], o);
+        *square += __shfl_xor(*square, o);
+        *n += __shfl_xor(*n, o);
+    }
+}
+
+// The gradient of the tokens that wavefront `wave` of `waves` takes.
+template <int IN, int CHUNKS, class Share>
+__device__ __forceinline__ void balance_gradient(const Router& r, const BalanceGradient& g, uint32_t wave, uint32_t waves, float by_n, Share share_of) {
+    typedef TokenLanes<IN, CHUNKS> L;
+    const L l(r.experts, r.lanes);
+    const uint32_t at_once = l.tokens(), stride = waves * at_once;
+    float share[L::N];
+#pragma unroll
+    for (int v = 0; v < L::N; ++v) share[v] = l.expert(v) < r.experts ? share_of(l.expert(v)) : 0.0f;
+    const float cb = g.balance * (float)r.experts * by_n, cz = 2.0f * g.z * by_n;
+    words4 next[CHUNKS] = {};
+    bool next_in = false;
+    uint32_t i = wave * at_once + l.of;
+    auto request = [&](uint32_t i) {
+        next_in = i < r.tokens && !(r.keep && !r.keep[i]);
+        if (next_in) l.load(r.x, (int64_t)i * r.ld, next);
+    };
+    request(i);
+    for (uint32_t base = wave * at_once; base < r.tokens; base += stride, i += stride) {
+        words4 now[CHUNKS];
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) now[c] = next[c];
+        bool in = next_in;
+        request(i + stride);
+        float y[L::N], by, log_sum, inner = 0.0f;
+        L::unpack(now, y);
+        in = l.softmax(y, &by, &log_sum) && in;
+#pragma unroll
+        for (int v = 0; v < L::N; ++v) inner += y[v] * share[v];
+        inner = l.sum(inner) * by;
+#pragma unroll
+        for (int v = 0; v < L::N; ++v) y[v] = in ? y[v] * (by * (cb * (share[v] - inner) + cz * log_sum)) : 0.0f;
+        if (i < r.tokens) l.store(g.dx, (int64_t)i * g.ld, y);
+    }
+}
+
+template <int IN, int CHUNKS>
+__global__ void __launch_bounds__(256) k_balance_rows(Router r, BalanceSums B) {
+    typedef TokenLanes<IN, CHUNKS> L;
+    __shared__ uint32_t of_expert[IWP_MAX_EXPERTS];
+    __shared__ float sums[4][IWP_MAX_EXPERTS];
+    __shared__ float squares[4];
+    __shared__ uint32_t counted[4];
+    const uint32_t wave = threadIdx.x >> 6;
+    for (uint32_t e = threadIdx.x; e < r.experts; e += 256) of_expert[e] = 0;
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < experts; e += 256) {
-        B.p[(size_t)blockIdx.x * experts + e] = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
-        B.slots[(size_t)blockIdx.x * experts + e] = of_expert[e];
+    float p[L::N] = {}, square = 0.0f;
+    uint32_t n = 0;
+    balance_sums<IN, CHUNKS>(r, blockIdx.x * 4 + wave, gridDim.x * 4, of_expert, p, &square, &n);
+    const L l(r.experts, r.lanes);
+    if (l.of == 0) {
+#pragma unroll
+        for (int v = 0; v < L::N; ++v)
+            if (l.expert(v) < r.experts) sums[wave][l.expert(v)] = p[v];
+    }
+    if ((threadIdx.x & 63) == 0) squares[wave] = square, counted[wave] = n;
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < r.experts; e += 256) {
+        B.p[(size_t)blockIdx.x * r.experts + e] = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
+        B.slots[(size_t)blockIdx.x * r.experts + e] = of_expert[e];
     }
     if (threadIdx.x == 0) {
         B.square[blockIdx.x] = (squares[0] + squares[1]) + (squares[2] + squares[3]);
@@ -114,6 +255,7 @@ __global__ void __launch_bounds__(256) k_balance_join(BalanceSums B, uint32_t gr
     if (e > experts) return;
     float s = 0.0f;
     uint32_t n = 0;
+#pragma unroll 4
     for (uint32_t g = lane; g < groups; g += 64) {
         s += e < experts ? B.p[(size_t)g * experts + e] : B.square[g];
         n += e < experts ? B.slots[(size_t)g * experts + e] : B.tokens[g];
@@ -127,50 +269,73 @@ __global__ void __launch_bounds__(256) k_balance_join(BalanceSums B, uint32_t gr
     else *B.square_all = s, *B.tokens_all = n;
 }
 
-// The gradient, a wavefront per token; the first workgroup also has the losses.
-template <int IN, int NV>
-__global__ void __launch_bounds__(256) k_balance_grad(const void* __restrict__ x, int64_t ld, uint32_t tokens, uint32_t experts,
-                                                      uint32_t slots, const uint8_t* __restrict__ keep, float balance, float z,
-                                                      BalanceSums B, const int32_t* __restrict__ counts, float* __restrict__ loss,
-                                                      void* __restrict__ dx, int64_t ld_dx) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// The first wavefront of a launch: loss[0] from the experts' slots and sums, loss[1].
+template <class Slots, class Sum>
+__device__ __forceinline__ void balance_loss(uint32_t experts, uint32_t slots, uint32_t n, float square, Slots slots_of, Sum p_of, float* loss) {
+    const uint32_t lane = threadIdx.x & 63;
+    const float by_n = n ? 1.0f / (float)n : 0.0f;
+    float s = 0.0f;
+    for (uint32_t e = lane; e < experts; e += 64) s += (float)slots_of(e) / (float)slots * by_n * (p_of(e) * by_n);
+    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+    if (lane == 0) {
+        loss[0] = (float)experts * s;
+        loss[1] = square * by_n;
+    }
+}
+
+// The gradient; the first wavefront also has the losses.
+template <int IN, int CHUNKS>
+__global__ void __launch_bounds__(256) k_balance_grad(Router r, BalanceGradient g, BalanceSums B, const int32_t* __restrict__ counts,
+                                                      float* __restrict__ loss) {
     const uint32_t n = *B.tokens_all;
     const float by_n = n ? 1.0f / (float)n : 0.0f;
-    float share[NV];
+    if (blockIdx.x == 0 && threadIdx.x < 64)
+        balance_loss(r.experts, r.slots, n, *B.square_all, [&](uint32_t e) { return counts[e]; }, [&](uint32_t e) { return B.p_all[e]; }, loss);
+    if (g.dx)
+        balance_gradient<IN, CHUNKS>(r, g, blockIdx.x * 4 + (threadIdx.x >> 6), gridDim.x * 4, by_n,
+                                     [&](uint32_t e) { return (float)counts[e] / (float)r.slots * by_n; });
+}
+
+// All of it in one workgroup, for small batches.
+constexpr uint32_t BALANCE_ONE_WAVES = 16;
+template <int IN, int CHUNKS>
+__global__ void __launch_bounds__(BALANCE_ONE_WAVES * 64) k_balance_one(Router r, BalanceGradient g, int32_t* __restrict__ counts,
+                                                                        float* __restrict__ loss) {
+    typedef TokenLanes<IN, CHUNKS> L;
+    constexpr uint32_t THREADS = BALANCE_ONE_WAVES * 64;
+    __shared__ uint32_t of_expert[IWP_MAX_EXPERTS];
+    __shared__ float sums[BALANCE_ONE_WAVES][IWP_MAX_EXPERTS];
+    __shared__ float squares[BALANCE_ONE_WAVES];
+    __shared__ uint32_t counted[BALANCE_ONE_WAVES];
+    const uint32_t wave = threadIdx.x >> 6;
+    for (uint32_t e = threadIdx.x; e < r.experts; e += THREADS) of_expert[e] = 0;
+    __syncthreads();
+    float p[L::N] = {}, square = 0.0f;
+    uint32_t n = 0;
+    balance_sums<IN, CHUNKS>(r, wave, BALANCE_ONE_WAVES, of_expert, p, &square, &n);
+    const L l(r.experts, r.lanes);
+    if (l.of == 0) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-        share[v] = lane + 64 * v < (int)experts && n ? (float)counts[lane + 64 * v] / ((float)n * (float)slots) : 0.0f;
-    if (blockIdx.x == 0 && wave == 0) {
-        float s = 0.0f;
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-            if (lane + 64 * v < (int)experts) s += share[v] * (B.p_all[lane + 64 * v] * by_n);
-        for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
-        if (lane == 0) {
-            loss[0] = (float)experts * s;
-            loss[1] = *B.square_all * by_n;
-        }
+        for (int v = 0; v < L::N; ++v)
+            if (l.expert(v) < r.experts) sums[wave][l.expert(v)] = p[v];
     }
-    if (!dx) return;
-    const float cb = balance * (float)experts * by_n, cz = 2.0f * z * by_n;
-    for (uint32_t i = blockIdx.x * 4 + wave; i < tokens; i += gridDim.x * 4) {
-        float y[NV], by = 0.0f, log_sum = 0.0f, inner = 0.0f;
-        bool in = !(keep && !keep[i]);
-        if (in) {
-            token_logits<IN, NV>(x, (int64_t)i * ld, experts, lane, y);
-            in = token_softmax<NV>(y, &by, &log_sum);
-        }
-        if (in) {
-#pragma unroll
-            for (int v = 0; v < NV; ++v) inner += y[v] * share[v];
-            for (int o = 32; o; o >>= 1) inner += __shfl_xor(inner, o);
-            inner *= by;
-        }
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-            if (lane + 64 * v < (int)experts)
-                put<IN>(dx, (int64_t)i * ld_dx + lane + 64 * v, in ? y[v] * (by * (cb * (share[v] - inner) + cz * log_sum)) : 0.0f);
+    if ((threadIdx.x & 63) == 0) squares[wave] = square, counted[wave] = n;
+    __syncthreads();
+    n = 0;
+    square = 0.0f;
+    for (uint32_t v = 0; v < BALANCE_ONE_WAVES; ++v) n += counted[v], square += squares[v];
+    for (uint32_t e = threadIdx.x; e < r.experts; e += THREADS) counts[e] = (int32_t)of_expert[e];
+    if (threadIdx.x < 64) {
+        balance_loss(r.experts, r.slots, n, square, [&](uint32_t e) { return of_expert[e]; },
+                     [&](uint32_t e) {
+                         float s = 0.0f;
+                         for (uint32_t v = 0; v < BALANCE_ONE_WAVES; ++v) s += sums[v][e];
+                         return s;
+                     }, loss);
     }
+    const float by_n = n ? 1.0f / (float)n : 0.0f;
+    if (g.dx)
+        balance_gradient<IN, CHUNKS>(r, g, wave, BALANCE_ONE_WAVES, by_n, [&](uint32_t e) { return (float)of_expert[e] / (float)r.slots * by_n; });
 }
 
 }  // namespace iwp

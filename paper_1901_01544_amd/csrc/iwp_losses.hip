@@ -315,6 +315,9 @@ int head_call(const HeadCall& c, uint32_t tokens, uint32_t dim, uint32_t vocab, 
 }
 
 constexpr uint32_t BALANCE_GROUPS = 512;
+#ifndef BALANCE_ONE
+#define BALANCE_ONE 16384
+#endif
 
 uint32_t balance_groups(uint32_t tokens) { return std::max(1u, std::min(BALANCE_GROUPS, (tokens + 3) / 4)); }
 
@@ -330,26 +333,33 @@ size_t balance_carve(BalanceSums* B, uint32_t groups, uint32_t experts, void* wo
     return c.used;
 }
 
-template <int IN, int NV>
-int balance_run(const void* x, int64_t ld_x, uint32_t tokens, uint32_t experts, const int32_t* chosen, uint32_t slots, const uint8_t* keep,
-                float balance, float z, float* loss, int32_t* counts, void* dx, int64_t ld_dx, const BalanceSums& B, uint32_t groups,
-                hipStream_t s) {
-    auto rows = k_balance_rows<IN, NV>;
-    auto grad = k_balance_grad<IN, NV>;
-    IWP_LAUNCH_BLOCK("k_balance_rows", rows, groups, 256, s, x, ld_x, tokens, experts, chosen, slots, keep, B);
-    IWP_LAUNCH_BLOCK("k_balance_join", k_balance_join, experts / 4 + 1, 256, s, B, groups, experts, counts);
-    IWP_LAUNCH_BLOCK("k_balance_grad", grad, dx ? std::max(1u, std::min((tokens + 3) / 4, 2048u)) : 1u, 256, s, x, ld_x, tokens, experts, slots,
-                     keep, balance, z, B, counts, loss, dx, ld_dx);
+template <int IN, int CHUNKS>
+int balance_run(const Router& r, const BalanceGradient& g, float* loss, int32_t* counts, const BalanceSums& B, uint32_t groups, hipStream_t s) {
+    auto one = k_balance_one<IN, CHUNKS>;
+    auto rows = k_balance_rows<IN, CHUNKS>;
+    auto grad = k_balance_grad<IN, CHUNKS>;
+    if ((uint64_t)r.tokens * r.experts <= BALANCE_ONE) {
+        IWP_LAUNCH_BLOCK("k_balance_one", one, 1, BALANCE_ONE_WAVES * 64, s, r, g, counts, loss);
+        return IWP_OK;
+    }
+    const uint32_t at_once = 4 * (64 / r.lanes), blocks = std::max(1u, (r.tokens + at_once - 1) / at_once);
+    groups = std::min(groups, blocks);
+    IWP_LAUNCH_BLOCK("k_balance_rows", rows, groups, 256, s, r, B);
+    IWP_LAUNCH_BLOCK("k_balance_join", k_balance_join, r.experts / 4 + 1, 256, s, B, groups, r.experts, counts);
+    IWP_LAUNCH_BLOCK("k_balance_grad", grad, g.dx ? std::min(blocks, 2048u) : 1u, 256, s, r, g, B, counts, loss);
     return IWP_OK;
 }
 
-template <int IN, class... A>
-int balance_typed(uint32_t experts, A... a) {
-    if (experts <= 64) return balance_run<IN, 1>(a...);
-    if (experts <= 128) return balance_run<IN, 2>(a...);
-    if (experts <= 256) return balance_run<IN, 4>(a...);
-    if (experts <= 512) return balance_run<IN, 8>(a...);
-    return balance_run<IN, 16>(a...);
+// 16 bytes a lane up to 16 lanes a token, then two and four times as many bytes before more lanes: a token's sums take a step less
+// for every halving of its lanes.
+template <int IN>
+int balance_typed(Router r, const BalanceGradient& g, float* loss, int32_t* counts, const BalanceSums& B, uint32_t groups, hipStream_t s) {
+    const uint32_t units = (r.experts + TokenLanes<IN, 1>::WIDTH - 1) / TokenLanes<IN, 1>::WIDTH;
+    const uint32_t chunks = units <= 16 ? 1 : units <= 32 ? 2 : 4;
+    r.lanes = 1;
+    while (r.lanes * chunks < units) r.lanes *= 2;
+    if (chunks == 1) return balance_run<IN, 1>(r, g, loss, counts, B, groups, s);
+    return chunks == 2 ? balance_run<IN, 2>(r, g, loss, counts, B, groups, s) : balance_run<IN, 4>(r, g, loss, counts, B, groups, s);
 }
 
 }  // namespace
@@ -401,11 +411,10 @@ int iwp_balance(const void* x, int64_t ld_x, uint32_t tokens, uint32_t experts, 
     const uint32_t groups = balance_groups(tokens);
     if (!workspace || workspace_bytes < balance_carve(&B, groups, experts, workspace)) return IWP_EWORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    if (dtype == IWP_F32)
-        return balance_typed<OUT_F32>(experts, x, ld_x, tokens, experts, chosen, slots, keep, balance, z, loss, counts, dx, ld_dx, B, groups, s);
-    if (dtype == IWP_BF16)
-        return balance_typed<OUT_BF16>(experts, x, ld_x, tokens, experts, chosen, slots, keep, balance, z, loss, counts, dx, ld_dx, B, groups, s);
-    return balance_typed<OUT_F16>(experts, x, ld_x, tokens, experts, chosen, slots, keep, balance, z, loss, counts, dx, ld_dx, B, groups, s);
+    const Router r{x, ld_x, tokens, experts, 0, slots, chosen, keep};
+    const BalanceGradient g{balance, z, dx, ld_dx};
+    if (dtype == IWP_F32) return balance_typed<OUT_F32>(r, g, loss, counts, B, groups, s);
+    return dtype == IWP_BF16 ? balance_typed<OUT_BF16>(r, g, loss, counts, B, groups, s) : balance_typed<OUT_F16>(r, g, loss, counts, B, groups, s);
 }
 
 }  // extern "C"
