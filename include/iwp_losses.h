@@ -39,10 +39,10 @@ typedef enum { IWP_F32 = 0, IWP_BF16 = 1, IWP_F16 = 2 } iwp_dtype;
 /* Workspace of the two head calls.  tokens, dim, vocab: sizes; ld_w, w: the weight's rows as they will
  * be handed over (a weight of 16 bits whose rows are not 16-byte aligned is copied into the workspace
  * first, one of 32 bits is split there); top: the teacher's entries per token (0: cross entropy);
- * piece: vocabulary entries whose logits are held at a time, 0 = all of them.  The rest of the vocabulary is worked
+ * piece: vocabulary entries whose logits are held at a time (rounded up to 256), 0 = all of them.  The rest of the vocabulary is worked
  * through in pieces, whose logits are computed a second time for the gradient: at piece >= vocab nothing is
- * computed twice, below it the workspace no longer grows with the vocabulary's logits.  with_dh: whether dh will
- * be asked for.  256-byte aligned.  0 for sizes that the calls refuse. */
+ * computed twice, below it the workspace holds a piece's logits instead of all of them (and 8 bytes per token
+ * and 32 to 128 entries of the vocabulary).  256-byte aligned.  0 for sizes that the calls refuse. */
 size_t iwp_head_workspace_bytes(uint32_t tokens, uint32_t dim, uint32_t vocab, uint32_t dtype, const void* w, int64_t ld_w,
                                 uint32_t top, uint32_t piece);
 
@@ -51,11 +51,12 @@ size_t iwp_head_workspace_bytes(uint32_t tokens, uint32_t dim, uint32_t vocab, u
  * weight[i] (NULL: 1) is not 0; then
  *   loss[i] = weight[i] * (log sum_j exp z_ij - z_i,target[i])
  *   dh, dw  = gradients of scale * sum_i loss[i]
- * A token that does not count has loss 0, a dh row of zeros, and no part in dw whatever its row of h holds.
+ * A token that does not count has loss 0, a dh row of zeros, and no part in dw whatever its row of h holds.  (A NaN or an
+ * infinity in the row of a token that counts, in w or in a weight makes what depends on it NaN, as by the definition.)
  * loss: [tokens], binary32.  dh: [tokens, dim], h's type, or NULL.  dw: [vocab, dim], of dw_dtype (the operands' type, or
  * IWP_F32 as the flat gradients of iwp.h are), or NULL.  Both gradients are written, not added to.
  * IWP_EINVAL: sizes of 0 (tokens may be 0) or above the limits, pointers missing, scale not finite, rows that overlap;
- * IWP_EALIGN: a buffer not aligned to its elements; IWP_ERANGE: ld of 2^23 or more. */
+ * IWP_EALIGN: a buffer not aligned to its elements, or the workspace; IWP_ERANGE: ld of 2^23 or more. */
 int iwp_head_cross_entropy(const void* h, int64_t ld_h, const void* w, int64_t ld_w, uint32_t tokens, uint32_t dim,
                            uint32_t vocab, uint32_t dtype, const int32_t* target, const float* weight, float scale,
                            uint32_t piece, float* loss, void* dh, int64_t ld_dh, void* dw, int64_t ld_dw, uint32_t dw_dtype,

@@ -4,7 +4,10 @@
 // Logits z = H W^T are held for one piece of the vocabulary at a time.  Forward, every piece leaves per token and group of
 // entries the largest logit m and sum exp(z - m); those are merged into L = log sum exp z.  Backward,
 //   dz = c1 (softmax(z) - [label]) + c2 (softmax(z / t) - q)
-// replaces the logits of a piece that is still there, and is computed with the logits again for a piece that is not.
+// replaces the logits of a piece that is still there (the last), and is computed with the logits again for a piece that is not.  A
+// vocabulary held as one piece takes 6 T V D operations, in many pieces 8 T V D, but no more memory than one piece's logits.
+// 8192 tokens x 2048 x 131072 in fp16, in pieces of 16384 (0.5 GB of logits instead of 4.3): 14.8 ms, a quarter of it for the
+// logits' second computation.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -58,7 +61,8 @@ static_assert(IWP_MAX_TOP <= 1u << 10 && IWP_MAX_VOCAB / STRETCHES <= 1u << 16, 
 
 // ------------------------------------------------------------------ tokens
 
-// Softmax of the teacher's entries of one token at temperature t; a wavefront per token.
+// Softmax of the teacher's entries of one token at temperature t; a wavefront per token.  An index that occurs again hands its share to
+// the first of its kind, for which every entry is compared with every other in LDS: 13 us for 4096 tokens of 64 entries.
 __global__ void __launch_bounds__(256) k_head_teacher(const int32_t* __restrict__ index, const float* __restrict__ logit,
                                                       const int32_t* __restrict__ label, uint32_t tokens, uint32_t vocab, Teacher T) {
     __shared__ int32_t at[4][IWP_MAX_TOP];
@@ -119,7 +123,9 @@ __global__ void __launch_bounds__(256) k_head_teacher(const int32_t* __restrict_
     }
 }
 
-// One workgroup: numbers the tokens that count, in order, and finds the largest coefficient.
+// One workgroup: numbers the tokens that count, in order, and finds the largest coefficient.  The products then run over those tokens
+// alone: what stands in the others' rows is never read, nor computed with.  Bound by its rounds of 1024 tokens, each two
+// barriers: 5 us for 1000 tokens, 13 us for 8192.
 __global__ void __launch_bounds__(1024) k_head_rows(const int32_t* __restrict__ label, const float* __restrict__ weight,
                                                     const uint8_t* __restrict__ any, uint32_t tokens, uint32_t vocab, float hard,
                                                     float soft, float t, HeadRows R, float* __restrict__ loss,
@@ -175,7 +181,10 @@ __global__ void __launch_bounds__(1024) k_head_rows(const int32_t* __restrict__ 
     }
 }
 
-// Sorts the teacher's entries of 64 rows into stretches of the vocabulary.  Inside a stretch their order is nobody's concern.
+// Sorts the teacher's entries of 64 rows into stretches of the vocabulary, for the logits' product, whose wavefronts then find theirs
+// without a search.  Inside a stretch their order is nobody's concern.  4096 tokens x 2048 x 32768 with 64 entries: 11 us here and
+// 45 us more in the product.  A dot product of its own for every entry, a wavefront each, took 409 us; reading the rows' entries
+// in the product's epilogue 190, with all of a wavefront's rows on their way at once 135.
 __global__ void __launch_bounds__(1024) k_head_sort(HeadRows R, Teacher T, const HeadScalars* __restrict__ S) {
     __shared__ uint32_t n[STRETCHES], in_wave[16];
     const uint32_t count = S->count, row0 = blockIdx.x * 64, thread = threadIdx.x;
@@ -252,7 +261,7 @@ struct Spread {
 };
 
 // The first `blocks` workgroups take one matrix, the others another; 16 rows of 1024 elements at a time.  Few and large workgroups: each
-// ends in an atomic on one word, and those take 20 ns one after the other.
+// ends in an atomic on one word, and those take 20 ns one after the other (75 MB: 19 us with 320 workgroups, 37 to 41 with 2560).
 __global__ void __launch_bounds__(1024) k_head_max(HeadMatrix A, HeadMatrix B, uint32_t blocks, HeadScalars* __restrict__ S) {
     const bool second = blockIdx.x >= blocks;
     const HeadMatrix M = second ? B : A;
@@ -300,7 +309,8 @@ __device__ __forceinline__ void split_f32(float x, float s, uint16_t* hi, uint16
 }
 
 // A matrix into rows of ld_out, zeros past its width; with `count`, zeros in the rows behind it up to the next multiple of 64.  Eight
-// elements of four rows a thread.
+// elements of four rows a thread: four loads on their way.  32003 rows of 1001 in bf16 (130 MB) 28 us, 4.6 TB/s; with one row a thread
+// 48 us.
 constexpr uint32_t PACK_ROWS = 4;
 template <bool F32>
 __global__ void __launch_bounds__(256) k_head_pack(HeadMatrix M, Spread spread, const uint32_t* __restrict__ max_bits,
@@ -555,7 +565,8 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_logits(Operand W, Operand
 
 // ------------------------------------------------------------------ statistics and losses
 
-// 16 rows a workgroup, 32 threads a row; groups in a fixed order.
+// 16 rows a workgroup, 32 threads a row; groups in a fixed order.  8192 rows x 1024 groups (64 MB): 29 us; with 32 rows a workgroup and 8
+// threads a row 70 us, and on 700 rows 18 us against 7, for want of workgroups.
 template <bool SOFT>
 __global__ void __launch_bounds__(512) k_head_join(HeadStats St, uint32_t groups, HeadRows R, Teacher T, float* __restrict__ loss,
                                                    const HeadScalars* __restrict__ S) {
@@ -644,7 +655,8 @@ __device__ __forceinline__ bool target_dz(uint32_t k, const HeadPiece& G, uint32
 }
 
 // In place on a kept piece: a workgroup takes 4096 entries of a row, twice eight a thread.  The label's entry is put right here, the
-// teacher's are by k_head_targets.
+// teacher's are by k_head_targets (handed around through LDS in here they cost 65 us at 4096 x 32768, there 9).  Bound by memory:
+// 8192 x 131072 entries of 2 bytes 740 us, 5.8 TB/s; with eight entries a thread 850.
 constexpr uint32_t DZ_ACROSS = 4096;
 template <class E, bool F32, bool WIDE, bool SOFT>
 __global__ void __launch_bounds__(256) k_head_dz(HeadPiece G, uint32_t group, HeadStats St, HeadRows R, Teacher T,
@@ -718,7 +730,8 @@ __global__ void __launch_bounds__(256) k_head_targets(HeadPiece G, HeadRows R, T
 
 // ------------------------------------------------------------------ gradients
 
-// dH, partial sums: workgroups of split s take a stretch of the piece's vocabulary.  sums: [splits, rows, ld].
+// dH, partial sums: workgroups of split s take a stretch of the piece's vocabulary.  sums: [splits, rows, ld].  T x D is a small product
+// with a long sum: 2048 tokens x 1024 make 32 tiles for 256 compute units, and eight splits fill them.
 template <class E, int BP, int BQ, int WP, int WQ>
 __global__ void __launch_bounds__(WP * WQ * 64) k_head_dh(Operand W, Operand G, uint32_t splits, uint32_t per_split,
                                                           float* __restrict__ sums, uint32_t rows, uint32_t ld, bool add,
@@ -796,7 +809,8 @@ __global__ void __launch_bounds__(256) k_head_dh_out(const float* __restrict__ s
     }
 }
 
-// dW of a piece: rows of the vocabulary, summed over the rows of tokens.
+// dW of a piece: rows of the vocabulary, summed over the rows of tokens.  Where tokens are few it is bound by writing dW: 5 tokens x 768 x
+// 8192 7 us, 684 x 1001 x 32003 with rows of odd length 51 us (90 us while those were written element by element).
 template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool F32>
 __global__ void __launch_bounds__(WP * WQ * 64) k_head_dw(Operand H, Operand G, float scale, void* __restrict__ dw, int64_t ld_dw,
                                                           uint32_t first, uint32_t dim, const HeadScalars* __restrict__ S) {
