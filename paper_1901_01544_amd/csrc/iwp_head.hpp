@@ -18,7 +18,7 @@
 
 namespace iwp {
 
-constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
+constexpr float LOG2E = 1.44269504088896340736f;
 // The gradient's coefficients are divided by the largest of any token, so an entry of dz is at most 1 in size.  Times 2^14, fp16
 // has room for entries down to 2^-38 of that, and none overflows; bf16 and the halves of binary32 do not mind.
 constexpr float DZ_SCALE = 16384.0f;
