@@ -19,17 +19,21 @@
 namespace iwp {
 
 constexpr float LOG2E = 1.44269504088896340736f;
-// The gradient's coefficients are divided by the largest of any token, so an entry of dz is at most 1 in size.  Times 2^14, fp16
-// has room for entries down to 2^-38 of that, and none overflows; bf16 and the halves of binary32 do not mind.
-constexpr float DZ_SCALE = 16384.0f;
+// A row of dz is held relative to its own token's coefficients: divided by 2^e, the power of two at or below |c1| + |c2|, an entry is less
+// than 2 in size.  Times 2^14, fp16 has room for entries down to 2^-38 of the coefficients, the halves of binary32 down to 2^-49, and none
+// overflows.  dH's rows take 2^e back one by one.  dW sums over the tokens: its product takes hidden states times 2^(e - the largest
+// e), a copy of them that is made where the tokens' powers differ.
+constexpr int DZ_BITS = 14;
+constexpr int32_t NO_EXPONENT = 1 << 20;           // of coefficients that are 0, infinite or NaN: not scaled, and no other token's concern
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
 
 struct HeadScalars {
     uint32_t count;        // tokens that count
-    float most;            // largest |c1| + |c2| of any token, without `scale`
-    uint32_t h_max, w_max; // bits of the largest finite |h|, |w| (binary32 operands only)
+    int32_t most;          // largest exponent of any token's coefficients, without `scale`
+    uint32_t alike;        // 1: all tokens have that one
+    uint32_t h_max, w_max; // bits of the largest finite |h|, |w| (of binary32 operands; h: also of fp16 ones that are scaled)
 };
 
 struct HeadRows {          // the tokens that count, in order
@@ -38,6 +42,7 @@ struct HeadRows {          // the tokens that count, in order
     int32_t* label;        // its label, or -1
     float* hard;           // weight * hard where there is a label, else 0
     float* soft;           // weight * soft * t^2 where there are teacher's entries, else 0
+    int32_t* exponent;     // of the power of two that its dz is relative to, or NO_EXPONENT
     float* z_label;
     float *lse, *lse_t;    // log sum exp of z, of z / t
 };
@@ -123,7 +128,7 @@ __global__ void __launch_bounds__(256) k_head_teacher(const int32_t* __restrict_
     }
 }
 
-// One workgroup: numbers the tokens that count, in order, and finds the largest coefficient.  The products then run over those tokens
+// One workgroup: numbers the tokens that count, in order, and finds the powers of two of their coefficients.  The products then run over those tokens
 // alone: what stands in the others' rows is never read, nor computed with.  Bound by its rounds of 1024 tokens, each two
 // barriers: 5 us for 1000 tokens, 13 us for 8192.
 __global__ void __launch_bounds__(1024) k_head_rows(const int32_t* __restrict__ label, const float* __restrict__ weight,
@@ -131,10 +136,10 @@ __global__ void __launch_bounds__(1024) k_head_rows(const int32_t* __restrict__ 
                                                     float soft, float t, HeadRows R, float* __restrict__ loss,
                                                     HeadScalars* __restrict__ S) {
     __shared__ uint32_t in_wave[16];
-    __shared__ float most_of[16];
+    __shared__ int32_t most_of[16], least_of[16];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t count = 0;
-    float most = 0.0f;
+    int32_t most = -NO_EXPONENT, least = NO_EXPONENT;
     for (uint32_t base = 0; base < tokens; base += 1024) {
         const uint32_t i = base + threadIdx.x;
         float ch = 0.0f, cs = 0.0f;
@@ -162,7 +167,15 @@ __global__ void __launch_bounds__(1024) k_head_rows(const int32_t* __restrict__ 
             R.label[at] = y;
             R.hard[at] = ch;
             R.soft[at] = cs;
-            most = fmaxf(most, fabsf(ch) + fabsf(cs) / t);
+            const float c1 = fabsf(ch), c2 = fabsf(cs) / t;
+            int32_t e = NO_EXPONENT;
+            if (c1 < INFINITY && c2 < INFINITY && (c1 != 0.0f || c2 != 0.0f)) {
+                e = ilogbf(fmaxf(c1, c2));
+                if (c1 + c2 >= ldexpf(1.0f, e + 1)) ++e;       // the sum may be infinite: so is 2^128
+                most = max(most, e);
+                least = min(least, e);
+            }
+            R.exponent[at] = e;
         } else if (i < tokens) {
             loss[i] = 0.0f;
         }
@@ -170,13 +183,17 @@ __global__ void __launch_bounds__(1024) k_head_rows(const int32_t* __restrict__ 
         count += all;
         __syncthreads();
     }
-    for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-    if (lane == 0) most_of[wave] = most;
+    for (int o = 32; o; o >>= 1) {
+        most = max(most, __shfl_xor(most, o));
+        least = min(least, __shfl_xor(least, o));
+    }
+    if (lane == 0) most_of[wave] = most, least_of[wave] = least;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int v = 1; v < 16; ++v) most = fmaxf(most, most_of[v]);
+        for (int v = 1; v < 16; ++v) most = max(most, most_of[v]), least = min(least, least_of[v]);
         S->count = count;
-        S->most = most;
+        S->alike = most <= least;
+        S->most = most == -NO_EXPONENT ? 0 : most;
         S->h_max = S->w_max = 0;
     }
 }
@@ -249,9 +266,10 @@ struct HeadMatrix {        // rows of a caller's matrix; those of `token` alone 
     const uint32_t* count;
 };
 
-// 128-bit accesses at an element's own alignment
+// 128-bit and 64-bit accesses at an element's own alignment
 typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t words4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint16_t halves4_any __attribute__((ext_vector_type(4), aligned(2)));
 
 // How a kernel's 256 threads lie over rows of `chunks` units: 2^shift threads to a row, the rest of the row by further workgroups.
 struct Spread {
@@ -262,7 +280,10 @@ struct Spread {
 
 // The first `blocks` workgroups take one matrix, the others another; 16 rows of 1024 elements at a time.  Few and large workgroups: each
 // ends in an atomic on one word, and those take 20 ns one after the other (75 MB: 19 us with 320 workgroups, 37 to 41 with 2560).
+// Operands of fp16: one matrix, and only where its rows are about to be scaled.
+template <bool F32>
 __global__ void __launch_bounds__(1024) k_head_max(HeadMatrix A, HeadMatrix B, uint32_t blocks, HeadScalars* __restrict__ S) {
+    if (!F32 && S->alike) return;
     const bool second = blockIdx.x >= blocks;
     const HeadMatrix M = second ? B : A;
     const uint32_t block = second ? blockIdx.x - blocks : blockIdx.x, n_blocks = second ? gridDim.x - blocks : blocks;
@@ -275,7 +296,17 @@ __global__ void __launch_bounds__(1024) k_head_max(HeadMatrix A, HeadMatrix B, u
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) {
             const uint32_t r = min(r0 + i, rows - 1);
-            const float* p = static_cast<const float*>(M.x) + (int64_t)(M.token ? M.token[r] : r) * M.ld + c;
+            const int64_t at = (int64_t)(M.token ? M.token[r] : r) * M.ld + c;
+            if (!F32) {
+                const uint16_t* p = static_cast<const uint16_t*>(M.x) + at;
+                halves4_any four = {};
+                if (c + 4 <= M.dim) four = *reinterpret_cast<const halves4_any*>(p);
+                else for (uint32_t e = 0; c + e < M.dim; ++e) four[e] = p[e];
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) v[i][e] = __float_as_uint(F16::value(four[e]));
+                continue;
+            }
+            const float* p = static_cast<const float*>(M.x) + at;
             if (c + 4 <= M.dim) {
                 v[i] = *reinterpret_cast<const words4*>(p);
             } else {
@@ -310,13 +341,17 @@ __device__ __forceinline__ void split_f32(float x, float s, uint16_t* hi, uint16
 
 // A matrix into rows of ld_out, zeros past its width; with `count`, zeros in the rows behind it up to the next multiple of 64.  Eight
 // elements of four rows a thread: four loads on their way.  32003 rows of 1001 in bf16 (130 MB) 28 us, 4.6 TB/s; with one row a thread
-// 48 us.
+// 48 us.  SCALED: where the tokens' exponents differ, also the rows times 2^(the row's exponent - the largest), in binary32 rounded once:
+// in bf16 that is exact; fp16 takes them at the scale of the matrix's largest element, as the halves of binary32 are taken.
+struct Planes { uint16_t *hi, *lo; };              // lo: of binary32 operands
 constexpr uint32_t PACK_ROWS = 4;
-template <bool F32>
-__global__ void __launch_bounds__(256) k_head_pack(HeadMatrix M, Spread spread, const uint32_t* __restrict__ max_bits,
-                                                   uint16_t* __restrict__ hi, uint16_t* __restrict__ lo, uint32_t ld_out) {
+template <class E, bool F32, bool SCALED>
+__global__ void __launch_bounds__(256) k_head_pack(HeadMatrix M, Spread spread, const uint32_t* __restrict__ max_bits, Planes out,
+                                                   Planes scaled, const int32_t* __restrict__ exponent, uint32_t ld_out,
+                                                   const HeadScalars* __restrict__ S) {
+    constexpr bool IS_F16 = !F32 && std::is_same<E, F16>::value;
     const uint32_t rows = M.count ? *M.count : M.rows, end = M.count ? (rows + 63) & ~63u : rows;
-    const float s = F32 ? split_scale(*max_bits) : 1.0f;
+    const float s = F32 || (SCALED && IS_F16) ? split_scale(*max_bits) : 1.0f;
     const uint32_t c = spread.unit() * 8, r0 = spread.row() * PACK_ROWS;
     if (c >= ld_out) return;
     constexpr int WORDS = F32 ? 2 : 1;
@@ -341,18 +376,30 @@ __global__ void __launch_bounds__(256) k_head_pack(HeadMatrix M, Spread spread, 
                 }
         }
     }
+    const bool alike = !SCALED || S->alike;
 #pragma unroll
     for (uint32_t i = 0; i < PACK_ROWS; ++i) {
         if (r0 + i >= end) break;
         const size_t at = (size_t)(r0 + i) * ld_out + c;
-        if (F32) {
+        auto put = [&](const Planes& to, int shift) {
             uint16_t a[8], b[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) split_f32(__uint_as_float(v[i][e / 4 % WORDS][e % 4]), s, &a[e], &b[e]);
-            *reinterpret_cast<uint4*>(hi + at) = *reinterpret_cast<const uint4*>(a);
-            *reinterpret_cast<uint4*>(lo + at) = *reinterpret_cast<const uint4*>(b);
-        } else {
-            *reinterpret_cast<words4*>(hi + at) = v[i][0];
+            for (int e = 0; e < 8; ++e) {
+                if (F32) {
+                    split_f32(ldexpf(__uint_as_float(v[i][e / 4 % WORDS][e % 4]), shift), s, &a[e], &b[e]);
+                } else {
+                    const uint16_t x = (uint16_t)(v[i][0][e / 2] >> (e % 2 * 16));
+                    a[e] = E::bits(ldexpf(E::value(x) * s, shift));
+                }
+            }
+            *reinterpret_cast<uint4*>(to.hi + at) = *reinterpret_cast<const uint4*>(a);
+            if (F32) *reinterpret_cast<uint4*>(to.lo + at) = *reinterpret_cast<const uint4*>(b);
+        };
+        if (F32) put(out, 0);
+        else *reinterpret_cast<words4*>(out.hi + at) = v[i][0];
+        if (!alike) {
+            const int32_t of = r0 + i < rows ? exponent[r0 + i] : NO_EXPONENT;
+            put(scaled, of == NO_EXPONENT ? 0 : of - S->most);
         }
     }
 }
@@ -408,11 +455,15 @@ struct RowGradient {        // what a row's dz takes besides its logits
         return c1 * exp_of(z - lse) + c2 * exp_of(z * t_inv - lse_t);
     }
 };
-__device__ __forceinline__ RowGradient row_gradient(const HeadRows& R, uint32_t row, float most, float t, bool soft) {
+// Times `scale`, what a product of dz times 2^(DZ_BITS - exponent) is to be multiplied by.
+__device__ __forceinline__ float dz_factor(float scale, int32_t exponent) {
+    return ldexpf(scale, (exponent == NO_EXPONENT ? 0 : exponent) - DZ_BITS);
+}
+__device__ __forceinline__ RowGradient row_gradient(const HeadRows& R, uint32_t row, float t, bool soft) {
     RowGradient g;
-    const float to = most > 0.0f ? 1.0f : 0.0f, by = most > 0.0f ? most : 1.0f;
-    g.c1 = to * R.hard[row] / by * DZ_SCALE;
-    g.c2 = soft ? to * (R.soft[row] / t) / by * DZ_SCALE : 0.0f;
+    const int32_t of = R.exponent[row], by = DZ_BITS - (of == NO_EXPONENT ? 0 : of);
+    g.c1 = ldexpf(R.hard[row], by);
+    g.c2 = soft ? ldexpf(R.soft[row] / t, by) : 0.0f;
     g.lse = R.lse[row];
     g.lse_t = soft ? R.lse_t[row] : 0.0f;
     g.t_inv = 1.0f / t;
@@ -510,7 +561,7 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_logits(Operand W, Operand
                 if (SOFT) St.sum_t[at] = sum_t;
             }
         } else if (row_in) {
-            g = row_gradient(R, q, S->most, t, SOFT);
+            g = row_gradient(R, q, t, SOFT);
         }
         if (PICK && found_from < found_to) {               // through LDS, where any lane can take any logit
 #pragma unroll
@@ -678,7 +729,7 @@ __global__ void __launch_bounds__(256) k_head_dz(HeadPiece G, uint32_t group, He
                 else m[v] = St.m[(size_t)((G.first + p) / group) * St.ld + row];
             }
         }
-        const RowGradient g = row_gradient(R, row, S->most, T.t, SOFT);
+        const RowGradient g = row_gradient(R, row, T.t, SOFT);
         const uint32_t label = SOFT ? ~0u : (uint32_t)R.label[row] - G.first;
 #pragma unroll
         for (int v = 0; v < PARTS; ++v) {
@@ -716,7 +767,7 @@ template <class E, bool F32, bool SOFT>
 __global__ void __launch_bounds__(256) k_head_targets(HeadPiece G, HeadRows R, Teacher T, const HeadScalars* __restrict__ S) {
     const uint32_t row = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= S->count) return;
-    const RowGradient g = row_gradient(R, row, S->most, T.t, SOFT);
+    const RowGradient g = row_gradient(R, row, T.t, SOFT);
     for (uint32_t k = threadIdx.x & 63; k <= (SOFT ? T.top : 0u); k += 64) {
         uint32_t at;
         float d;
@@ -785,7 +836,7 @@ __global__ void __launch_bounds__(256) k_head_dh_out(const float* __restrict__ s
     const int32_t row = R.row[token];
     f32x4 x = {};
     if (row >= 0) {
-        const float factor = scale * S->most * (1.0f / DZ_SCALE), s = F32 ? 1.0f / split_scale(S->w_max) : 1.0f;
+        const float factor = dz_factor(scale, R.exponent[row]), s = F32 ? 1.0f / split_scale(S->w_max) : 1.0f;
         const float* from = sums + (size_t)row * ld + c;
         const size_t step = (size_t)rows * ld;
         uint32_t v = 0;
@@ -812,7 +863,7 @@ __global__ void __launch_bounds__(256) k_head_dh_out(const float* __restrict__ s
 // dW of a piece: rows of the vocabulary, summed over the rows of tokens.  Where tokens are few it is bound by writing dW: 5 tokens x 768 x
 // 8192 7 us, 684 x 1001 x 32003 with rows of odd length 51 us (90 us while those were written element by element).
 template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool F32>
-__global__ void __launch_bounds__(WP * WQ * 64) k_head_dw(Operand H, Operand G, float scale, void* __restrict__ dw, int64_t ld_dw,
+__global__ void __launch_bounds__(WP * WQ * 64) k_head_dw(Operand H, Planes scaled, Operand G, float scale, void* __restrict__ dw, int64_t ld_dw,
                                                           uint32_t first, uint32_t dim, const HeadScalars* __restrict__ S) {
     typedef Product<E, BP, BQ, WP, WQ, true, true> M;
     __shared__ __align__(1024) char lds[M::LDS];
@@ -821,11 +872,14 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_dw(Operand H, Operand G, 
     tile_of(blockIdx.x, (dim + BP - 1) / BP, (n + BQ - 1) / BQ, &tp, &tq);
     const uint32_t k_end = (count + BK - 1) & ~(BK - 1);
     H.summed = G.summed = k_end;
+    const bool alike = S->alike;
+    if (!alike) H.hi = scaled.hi, H.lo = F32 ? scaled.lo : nullptr;
     M mm;
     mm.run(H, G, tp * BP, tq * BQ, 0, k_end, lds);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t p0 = tp * BP + M::p_of(wave), q0 = tq * BQ + M::q_of(wave);
-    const float factor = scale * S->most * (1.0f / DZ_SCALE), s = F32 ? 1.0f / split_scale(S->h_max) : 1.0f;
+    const float factor = dz_factor(scale, S->most);
+    const float s = F32 || (std::is_same<E, F16>::value && !alike) ? 1.0f / split_scale(S->h_max) : 1.0f;
     typedef Rows32<OUT == OUT_F32 ? 4 : 2, BP / WP> Out;
     static_assert(M::WAVES * Out::BYTES <= M::LDS, "a wavefront's rows");
     char* mine = lds + wave * Out::BYTES;

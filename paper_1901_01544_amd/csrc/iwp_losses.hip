@@ -76,6 +76,7 @@ struct HeadPlan {
     HeadStats St;
     Teacher T;
     uint16_t *h_hi, *h_lo, *w_hi, *w_lo, *g_hi, *g_lo;
+    uint16_t *hs_hi, *hs_lo;                             // h times powers of two for the tokens' coefficients
     float* sums;
     size_t bytes;
 };
@@ -125,6 +126,7 @@ HeadPlan head_plan(uint32_t tokens, uint32_t dim, uint32_t vocab, uint32_t dtype
     c.take(p.R.label, p.rows);
     c.take(p.R.hard, p.rows);
     c.take(p.R.soft, p.rows);
+    c.take(p.R.exponent, p.rows);
     c.take(p.R.z_label, p.rows);
     c.take(p.R.lse, p.rows);
     c.take(p.R.lse_t, p.rows);
@@ -147,6 +149,8 @@ HeadPlan head_plan(uint32_t tokens, uint32_t dim, uint32_t vocab, uint32_t dtype
     }
     c.take(p.h_hi, (size_t)p.rows * p.dim_padded);
     if (p.f32) c.take(p.h_lo, (size_t)p.rows * p.dim_padded);
+    c.take(p.hs_hi, (size_t)p.rows * p.dim_padded);
+    if (p.f32) c.take(p.hs_lo, (size_t)p.rows * p.dim_padded);
     if (copy_w) c.take(p.w_hi, (size_t)vocab * p.dim_padded);
     if (p.f32) c.take(p.w_lo, (size_t)vocab * p.dim_padded);
     c.take(p.g_hi, (size_t)p.rows * p.ld_logits);
@@ -191,7 +195,8 @@ int launch_dw(const HeadPlan& p, const HeadCall& c, const Operand& H, const Oper
     return with_tile(tile_for(p.dim, G.extent), [&](auto tile) {
         typedef decltype(tile) T;
         auto kernel = k_head_dw<typename K::E, T::BP, T::BQ, T::WP, T::WQ, OUT, K::F32>;
-        IWP_LAUNCH_BLOCK("k_head_dw", kernel, tiles_of<T>(p.dim, G.extent), T::THREADS, c.s, H, G, c.scale, c.dw, c.ld_dw, first, p.dim, p.scalars);
+        IWP_LAUNCH_BLOCK("k_head_dw", kernel, tiles_of<T>(p.dim, G.extent), T::THREADS, c.s, H, (Planes{p.hs_hi, p.hs_lo}), G, c.scale,
+                         c.dw, c.ld_dw, first, p.dim, p.scalars);
         return (int)IWP_OK;
     });
 }
@@ -214,17 +219,24 @@ int head(const HeadPlan& p, const HeadCall& c) {
                      c.soft, c.temperature, p.R, c.loss, p.scalars);
     if (SOFT) IWP_LAUNCH_BLOCK("k_head_sort", k_head_sort, (tokens + 63) / 64, 1024, c.s, p.R, p.T, p.scalars);
     const HeadMatrix h{c.h, c.ld_h, p.tokens, p.dim, p.R.token, &p.scalars->count}, w{c.w, c.ld_w, p.vocab, p.dim, nullptr, nullptr};
-    if (K::F32) {
+    // without weights and a teacher all coefficients are the same
+    const bool scaled = c.dw && (SOFT || c.weight);
+    constexpr bool IS_F16 = !K::F32 && std::is_same<typename K::E, F16>::value;
+    if (K::F32 || (IS_F16 && scaled)) {
         auto blocks = [&](uint32_t rows, uint32_t most) { return std::max(1u, std::min((rows + 15) / 16 * ((p.dim + 1023) / 1024), most)); };
-        const uint32_t hb = blocks(p.tokens, 64), wb = blocks(p.vocab, 256);
-        IWP_LAUNCH_BLOCK("k_head_max", k_head_max, hb + wb, 1024, c.s, h, w, hb, p.scalars);
+        const uint32_t hb = blocks(p.tokens, K::F32 ? 64 : 256), wb = K::F32 ? blocks(p.vocab, 256) : 0;
+        IWP_LAUNCH_BLOCK("k_head_max", k_head_max<K::F32>, hb + wb, 1024, c.s, h, w, hb, p.scalars);
     }
     const Spread packed = spread(p.dim_padded / 8);
-    IWP_LAUNCH_BLOCK("k_head_pack", k_head_pack<K::F32>, blocks_of(packed, (p.rows + PACK_ROWS - 1) / PACK_ROWS), 256, c.s, h, packed, &p.scalars->h_max, p.h_hi, p.h_lo,
-                     p.dim_padded);
-    if (p.copy_w)
-        IWP_LAUNCH_BLOCK("k_head_pack", k_head_pack<K::F32>, blocks_of(packed, (p.vocab + PACK_ROWS - 1) / PACK_ROWS), 256, c.s, w, packed, &p.scalars->w_max, p.w_hi, p.w_lo,
-                         p.dim_padded);
+    auto pack = [&](auto kernel, const HeadMatrix& m, uint32_t rows, const uint32_t* max_bits, const Planes& to) {
+        IWP_LAUNCH_BLOCK("k_head_pack", kernel, blocks_of(packed, (rows + PACK_ROWS - 1) / PACK_ROWS), 256, c.s, m, packed, max_bits, to,
+                         (Planes{p.hs_hi, p.hs_lo}), p.R.exponent, p.dim_padded, p.scalars);
+        return (int)IWP_OK;
+    };
+    int rc = scaled ? pack(k_head_pack<typename K::E, K::F32, true>, h, p.rows, &p.scalars->h_max, Planes{p.h_hi, p.h_lo})
+                    : pack(k_head_pack<typename K::E, K::F32, false>, h, p.rows, &p.scalars->h_max, Planes{p.h_hi, p.h_lo});
+    if (!rc && p.copy_w) rc = pack(k_head_pack<typename K::E, K::F32, false>, w, p.vocab, &p.scalars->w_max, Planes{p.w_hi, p.w_lo});
+    if (rc) return rc;
     const uint16_t* w_hi = p.copy_w ? p.w_hi : static_cast<const uint16_t*>(c.w);
     const size_t ld_w = p.copy_w ? p.dim_padded : (size_t)c.ld_w;
     const uint32_t dim_w = p.copy_w ? p.dim_padded : p.dim;
@@ -237,7 +249,6 @@ int head(const HeadPlan& p, const HeadCall& c) {
         return Operand{w_hi + G.first * ld_w, p.w_lo ? p.w_lo + G.first * ld_w : nullptr, (uint32_t)ld_w, G.n, dim_w};
     };
     const bool gradients = c.dh || c.dw;
-    int rc;
     for (uint32_t i = 0; i < p.pieces; ++i) {
         const HeadPiece G = piece(i);
         rc = with_tile(p.logits_tile, [&](auto tile) {
