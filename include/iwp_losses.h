@@ -11,7 +11,11 @@
  *   IWP_F32   products of binary32 operands as three products of their halves (22 bits of each
  *             operand; sums in binary32), everything else in binary32
  *   IWP_BF16, IWP_F16   products of the operands as they are, sums in binary32; the logits'
- *             gradient is rounded to the operands' type before the two products that use it
+ *             gradient is rounded to the operands' type before the two products that use it.
+ *             IWP_BF16: the logits of the vocabulary's last piece (all of it, if it is worked through
+ *             at once) are kept for the gradient in 16 bits, off by at most 2^-13 (1 + d) where d is the
+ *             distance to the largest of 32 to 128 neighbouring entries' logits; those of the
+ *             other pieces are computed again, in binary32
  * Softmax statistics, losses and sums are binary32 throughout.
  */
 #ifndef IWP_LOSSES_H

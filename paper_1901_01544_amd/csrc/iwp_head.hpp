@@ -432,8 +432,11 @@ struct HeadStats {          // [groups, rows]: a group is the part of the vocabu
     uint32_t ld;
 };
 
-// How the logits of a piece are kept until the statistics are known: for bf16 operands as fp16 differences to the group's largest
-// (an error of 2^-12 of the distance to it, where bf16 would round the gradient to 2^-9), otherwise as binary32, by halves.
+// How the logits of a piece are kept until the statistics are known: binary32, by halves, or for bf16 operands 16 bits of the distance d
+// to the group's largest: of the binary32 number 1 + d, which is at least 1, four bits of the exponent and twelve of the
+// fraction.  That is off by at most 2^-13 (1 + d), which moves exp(-d) by less than rounding it to bf16 does (2^-8) up to d = 31.  (In
+// fp16, d itself would be off by up to 2^-11 d.)  The last code stands for entries without a share: d of more than 65500, or -inf.
+constexpr uint32_t ONE = 0x3f800000u, KEPT_SHIFT = 11, KEPT_NONE = 0xffffu;
 template <bool WIDE>
 __device__ __forceinline__ void keep_logit(float z, float m, uint16_t* hi, uint16_t* lo) {
     if (WIDE) {
@@ -441,12 +444,14 @@ __device__ __forceinline__ void keep_logit(float z, float m, uint16_t* hi, uint1
         *hi = b >> 16;
         *lo = (uint16_t)b;
     } else {
-        *hi = F16::bits(z - m);
+        const uint32_t d = __float_as_uint(m - z + 1.0f) - ONE;
+        *hi = (uint16_t)min((d + (1u << (KEPT_SHIFT - 1))) >> KEPT_SHIFT, KEPT_NONE);      // NaN (as of -inf to -inf) is above all numbers
     }
 }
 template <bool WIDE>
 __device__ __forceinline__ float kept_logit(uint16_t hi, uint16_t lo, float m) {
-    return WIDE ? __uint_as_float((uint32_t)hi << 16 | lo) : F16::value(hi) + m;
+    if (WIDE) return __uint_as_float((uint32_t)hi << 16 | lo);
+    return hi == KEPT_NONE ? m - INFINITY : m - (__uint_as_float(ONE + ((uint32_t)hi << KEPT_SHIFT)) - 1.0f);
 }
 
 struct RowGradient {        // what a row's dz takes besides its logits
