@@ -36,6 +36,7 @@ typedef enum { IWP_F32 = 0, IWP_BF16 = 1, IWP_F16 = 2 } iwp_dtype;
 #define IWP_MAX_DIM (1u << 16)
 #define IWP_MAX_VOCAB (1u << 22)
 #define IWP_MAX_TOP 1024u
+#define IWP_MAX_HELD ((uint64_t)1 << 38)        /* tokens x vocabulary entries whose logits are held at a time */
 #define IWP_MAX_EXPERTS 1024u
 
 /* ------------------------------------------------------------------ the head */

@@ -274,7 +274,8 @@ typedef uint16_t halves4_any __attribute__((ext_vector_type(4), aligned(2)));
 // How a kernel's 256 threads lie over rows of `chunks` units: 2^shift threads to a row, the rest of the row by further workgroups.
 struct Spread {
     uint32_t shift, across;
-    __device__ __forceinline__ uint32_t row() const { return blockIdx.x / across * (256u >> shift) + (threadIdx.x >> shift); }
+    __host__ __device__ uint32_t rows() const { return 256u >> shift; }        // of a workgroup
+    __device__ __forceinline__ uint32_t row() const { return blockIdx.x / across * rows() + (threadIdx.x >> shift); }
     __device__ __forceinline__ uint32_t unit() const { return (blockIdx.x % across << shift) + (threadIdx.x & ((1u << shift) - 1)); }
 };
 
@@ -346,13 +347,13 @@ __device__ __forceinline__ void split_f32(float x, float s, uint16_t* hi, uint16
 struct Planes { uint16_t *hi, *lo; };              // lo: of binary32 operands
 constexpr uint32_t PACK_ROWS = 4;
 template <class E, bool F32, bool SCALED>
-__global__ void __launch_bounds__(256) k_head_pack(HeadMatrix M, Spread spread, const uint32_t* __restrict__ max_bits, Planes out,
-                                                   Planes scaled, const int32_t* __restrict__ exponent, uint32_t ld_out,
+__global__ void __launch_bounds__(256) k_head_pack(HeadMatrix M, uint32_t first, Spread spread, const uint32_t* __restrict__ max_bits, 
+                                                   Planes out, Planes scaled, const int32_t* __restrict__ exponent, uint32_t ld_out,
                                                    const HeadScalars* __restrict__ S) {
     constexpr bool IS_F16 = !F32 && std::is_same<E, F16>::value;
     const uint32_t rows = M.count ? *M.count : M.rows, end = M.count ? (rows + 63) & ~63u : rows;
     const float s = F32 || (SCALED && IS_F16) ? split_scale(*max_bits) : 1.0f;
-    const uint32_t c = spread.unit() * 8, r0 = spread.row() * PACK_ROWS;
+    const uint32_t c = spread.unit() * 8, r0 = first + spread.row() * PACK_ROWS;
     if (c >= ld_out) return;
     constexpr int WORDS = F32 ? 2 : 1;
     words4 v[PACK_ROWS][WORDS];
@@ -715,9 +716,9 @@ __device__ __forceinline__ bool target_dz(uint32_t k, const HeadPiece& G, uint32
 // 8192 x 131072 entries of 2 bytes 740 us, 5.8 TB/s; with eight entries a thread 850.
 constexpr uint32_t DZ_ACROSS = 4096;
 template <class E, bool F32, bool WIDE, bool SOFT>
-__global__ void __launch_bounds__(256) k_head_dz(HeadPiece G, uint32_t group, HeadStats St, HeadRows R, Teacher T,
+__global__ void __launch_bounds__(256) k_head_dz(HeadPiece G, uint32_t first_row, uint32_t group, HeadStats St, HeadRows R, Teacher T,
                                                  const HeadScalars* __restrict__ S) {
-    const uint32_t count = S->count, across = (G.ld + DZ_ACROSS - 1) / DZ_ACROSS, row = blockIdx.x / across;
+    const uint32_t count = S->count, across = (G.ld + DZ_ACROSS - 1) / DZ_ACROSS, row = first_row + blockIdx.x / across;
     const uint32_t first = blockIdx.x % across * DZ_ACROSS + threadIdx.x * 8;
     if (row >= ((count + 63) & ~63u)) return;
     constexpr int PARTS = DZ_ACROSS / 2048;
@@ -834,9 +835,9 @@ __device__ __forceinline__ void put(void* out, int64_t at, float x) {
 // entries a thread.
 template <int OUT, bool F32>
 __global__ void __launch_bounds__(256) k_head_dh_out(const float* __restrict__ sums, uint32_t splits, uint32_t rows, uint32_t ld,
-                                                     HeadRows R, Spread spread, uint32_t tokens, uint32_t dim, float scale, void* __restrict__ dh,
+                                                     HeadRows R, uint32_t first, Spread spread, uint32_t tokens, uint32_t dim, float scale, void* __restrict__ dh,
                                                      int64_t ld_dh, const HeadScalars* __restrict__ S) {
-    const uint32_t token = spread.row(), c = spread.unit() * 4;
+    const uint32_t token = first + spread.row(), c = spread.unit() * 4;
     if (token >= tokens || c >= dim) return;
     const int32_t row = R.row[token];
     f32x4 x = {};

@@ -8,6 +8,7 @@
 #include "iwp_balance.hpp"
 #include "iwp_head.hpp"
 #include "iwp_host.hpp"
+#include "iwp_launch_rows.hpp"
 
 using namespace iwp;
 
@@ -87,13 +88,16 @@ Spread spread(uint32_t units) {
     s.across = (units + (1u << s.shift) - 1) >> s.shift;
     return s;
 }
-uint32_t blocks_of(const Spread& s, uint32_t rows) { return (rows + (256u >> s.shift) - 1) / (256u >> s.shift) * s.across; }
 
 bool readable(const void* w, int64_t ld_w, uint32_t dim, uint32_t dtype) {
     return dtype != IWP_F32 && aligned(w, 16) && ld_w % 8 == 0 && dim % 8 == 0;
 }
 
 constexpr uint32_t MAX_SPLITS = 32;
+
+uint32_t held(uint32_t vocab, uint32_t piece) {         // entries of the vocabulary whose logits are held at a time
+    return piece == 0 || piece >= vocab ? vocab : std::min(vocab, round_up(piece, TILE_VOCAB));
+}
 
 HeadPlan head_plan(uint32_t tokens, uint32_t dim, uint32_t vocab, uint32_t dtype, bool copy_w, uint32_t top, uint32_t piece,
                    void* workspace) {
@@ -102,7 +106,7 @@ HeadPlan head_plan(uint32_t tokens, uint32_t dim, uint32_t vocab, uint32_t dtype
     p.T.t = 1.0f;
     p.f32 = dtype == IWP_F32;
     p.wide = dtype != IWP_BF16;
-    p.piece = piece == 0 || piece >= vocab ? vocab : std::min(vocab, round_up(piece, TILE_VOCAB));
+    p.piece = held(vocab, piece);
     p.pieces = (vocab + p.piece - 1) / p.piece;
     p.rows = round_up(std::max(tokens, 1u), tokens <= Few::BQ ? (uint32_t)Few::BQ : (uint32_t)Big::BQ);
     p.dim_padded = round_up(dim, BK);
@@ -160,9 +164,11 @@ HeadPlan head_plan(uint32_t tokens, uint32_t dim, uint32_t vocab, uint32_t dtype
     return p;
 }
 
-bool sizes_ok(uint32_t tokens, uint32_t dim, uint32_t vocab, uint32_t dtype, uint32_t top) {
+// Up to IWP_MAX_HELD logits at a time every product's launch stays below 2^31 threads: 512 for 256 x 256 logits or gradients (the smaller
+// tiles are taken where tiles are few).
+bool sizes_ok(uint32_t tokens, uint32_t dim, uint32_t vocab, uint32_t dtype, uint32_t top, uint32_t piece) {
     return tokens <= IWP_MAX_TOKENS && dim >= 1 && dim <= IWP_MAX_DIM && vocab >= 1 && vocab <= IWP_MAX_VOCAB && dtype <= IWP_F16 &&
-           top <= IWP_MAX_TOP;
+           top <= IWP_MAX_TOP && (uint64_t)tokens * held(vocab, piece) <= IWP_MAX_HELD;
 }
 
 struct HeadCall {
@@ -229,9 +235,11 @@ int head(const HeadPlan& p, const HeadCall& c) {
     }
     const Spread packed = spread(p.dim_padded / 8);
     auto pack = [&](auto kernel, const HeadMatrix& m, uint32_t rows, const uint32_t* max_bits, const Planes& to) {
-        IWP_LAUNCH_BLOCK("k_head_pack", kernel, blocks_of(packed, (rows + PACK_ROWS - 1) / PACK_ROWS), 256, c.s, m, packed, max_bits, to,
-                         (Planes{p.hs_hi, p.hs_lo}), p.R.exponent, p.dim_padded, p.scalars);
-        return (int)IWP_OK;
+        return in_launches(rows, packed.rows() * PACK_ROWS, packed.across, 256, [&](uint32_t first, uint32_t blocks) {
+            IWP_LAUNCH_BLOCK("k_head_pack", kernel, blocks, 256, c.s, m, first, packed, max_bits, to, (Planes{p.hs_hi, p.hs_lo}), p.R.exponent,
+                             p.dim_padded, p.scalars);
+            return (int)IWP_OK;
+        });
     };
     int rc = scaled ? pack(k_head_pack<typename K::E, K::F32, true>, h, p.rows, &p.scalars->h_max, Planes{p.h_hi, p.h_lo})
                     : pack(k_head_pack<typename K::E, K::F32, false>, h, p.rows, &p.scalars->h_max, Planes{p.h_hi, p.h_lo});
@@ -266,8 +274,11 @@ int head(const HeadPlan& p, const HeadCall& c) {
         const bool kept = i + 1 == p.pieces;
         if (kept) {
             auto kernel = k_head_dz<typename K::E, K::F32, K::WIDE, SOFT>;
-            IWP_LAUNCH_BLOCK("k_head_dz", kernel, (p.ld_logits + DZ_ACROSS - 1) / DZ_ACROSS * p.rows, 256, c.s, G, p.group, p.St, p.R, p.T,
-                             p.scalars);
+            rc = in_launches(p.rows, 1, (p.ld_logits + DZ_ACROSS - 1) / DZ_ACROSS, 256, [&](uint32_t first, uint32_t blocks) {
+                IWP_LAUNCH_BLOCK("k_head_dz", kernel, blocks, 256, c.s, G, first, p.group, p.St, p.R, p.T, p.scalars);
+                return (int)IWP_OK;
+            });
+            if (rc) return rc;
         } else {
             rc = p.rows < Big::BQ ? launch_logits<K, Few, GRADIENT, SOFT>(p, c, weight(G), H, G)
                                   : launch_logits<K, Big, GRADIENT, SOFT>(p, c, weight(G), H, G);
@@ -293,15 +304,17 @@ int head(const HeadPlan& p, const HeadCall& c) {
         }
     }
     const Spread out = spread((p.dim + 3) / 4);
-    if (c.dh && p.tokens)
-        IWP_LAUNCH_BLOCK("k_head_dh_out", (k_head_dh_out<K::OUT, K::F32>), blocks_of(out, p.tokens), 256, c.s, p.sums, p.splits, p.rows,
-                         p.ld_sums, p.R, out, p.tokens, p.dim, c.scale, c.dh, c.ld_dh, p.scalars);
-    return IWP_OK;
+    if (!c.dh) return IWP_OK;
+    return in_launches(p.tokens, out.rows(), out.across, 256, [&](uint32_t first, uint32_t blocks) {
+        IWP_LAUNCH_BLOCK("k_head_dh_out", (k_head_dh_out<K::OUT, K::F32>), blocks, 256, c.s, p.sums, p.splits, p.rows, p.ld_sums, p.R, first,
+                         out, p.tokens, p.dim, c.scale, c.dh, c.ld_dh, p.scalars);
+        return (int)IWP_OK;
+    });
 }
 
 int head_call(const HeadCall& c, uint32_t tokens, uint32_t dim, uint32_t vocab, uint32_t dtype, uint32_t top, uint32_t piece, void* workspace,
               size_t workspace_bytes) {
-    if (!sizes_ok(tokens, dim, vocab, dtype, top)) return IWP_EINVAL;
+    if (!sizes_ok(tokens, dim, vocab, dtype, top, piece)) return IWP_EINVAL;
     if (c.dw && c.dw_dtype != dtype && c.dw_dtype != IWP_F32) return IWP_EINVAL;
     if (!std::isfinite(c.scale) || !std::isfinite(c.hard) || !std::isfinite(c.soft) || !(c.temperature > 0.0f) || !std::isfinite(c.temperature))
         return IWP_EINVAL;
@@ -379,7 +392,7 @@ extern "C" {
 
 size_t iwp_head_workspace_bytes(uint32_t tokens, uint32_t dim, uint32_t vocab, uint32_t dtype, const void* w, int64_t ld_w, uint32_t top,
                                 uint32_t piece) {
-    if (!sizes_ok(tokens, dim, vocab, dtype, top)) return 0;
+    if (!sizes_ok(tokens, dim, vocab, dtype, top, piece)) return 0;
     return head_plan(tokens, dim, vocab, dtype, !readable(w, ld_w, dim, dtype), top, piece, nullptr).bytes;
 }
 
