@@ -90,6 +90,7 @@ __global__ void __launch_bounds__(256) k_head_teacher(const int32_t* __restrict_
         }
     }
     for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    lanes_exchange();
     any = __ballot(any) != 0;
     if (__ballot(nan)) m = NAN;
     float sum = 0.0f;
@@ -105,6 +106,7 @@ __global__ void __launch_bounds__(256) k_head_teacher(const int32_t* __restrict_
         if (in && q != 0.0f) entropy += q * log_q;
     }
     for (int o = 32; o; o >>= 1) entropy += __shfl_xor(entropy, o);
+    lanes_exchange();
     const int32_t y = label ? label[i] : -1;
     bool is_label = false;
     for (uint32_t k = lane; k < T.top; k += 64) {
@@ -258,6 +260,17 @@ __device__ __forceinline__ float split_scale(uint32_t max_bits) {
 // A sum of products of two split operands -> the sum itself, in two factors that are normal numbers.
 __device__ __forceinline__ float unsplit(float sum, float sp, float sq) { return sum * (1.0f / sp) * (1.0f / sq); }
 
+// Eight entries of 16 bits at a 16-byte aligned place
+__device__ __forceinline__ void load8(const uint16_t* from, uint16_t (&x)[8]) {
+    const quad v = *reinterpret_cast<const quad*>(from);
+    __builtin_memcpy(x, &v, 16);
+}
+__device__ __forceinline__ void store8(uint16_t* to, const uint16_t (&x)[8]) {
+    quad v;
+    __builtin_memcpy(&v, x, 16);
+    *reinterpret_cast<quad*>(to) = v;
+}
+
 struct HeadMatrix {        // rows of a caller's matrix; those of `token` alone where it is given, `count` of them
     const void* x;
     int64_t ld;
@@ -267,9 +280,9 @@ struct HeadMatrix {        // rows of a caller's matrix; those of `token` alone 
 };
 
 // 128-bit and 64-bit accesses at an element's own alignment
-typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t words4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint16_t halves4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(4), may_alias));
+typedef uint32_t words4_any __attribute__((ext_vector_type(4), aligned(2), may_alias));
+typedef uint16_t halves4_any __attribute__((ext_vector_type(4), aligned(2), may_alias));
 
 // How a kernel's 256 threads lie over rows of `chunks` units: 2^shift threads to a row, the rest of the row by further workgroups.
 struct Spread {
@@ -393,8 +406,8 @@ __global__ void __launch_bounds__(256) k_head_pack(HeadMatrix M, uint32_t first,
                     a[e] = E::bits(ldexpf(E::value(x) * s, shift));
                 }
             }
-            *reinterpret_cast<uint4*>(to.hi + at) = *reinterpret_cast<const uint4*>(a);
-            if (F32) *reinterpret_cast<uint4*>(to.lo + at) = *reinterpret_cast<const uint4*>(b);
+            store8(to.hi + at, a);
+            if (F32) store8(to.lo + at, b);
         };
         if (F32) put(out, 0);
         else *reinterpret_cast<words4*>(out.hi + at) = v[i][0];
@@ -577,6 +590,7 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_logits(Operand W, Operand
                     const f32x4 v = {mm.acc[a][b][c * 4], mm.acc[a][b][c * 4 + 1], mm.acc[a][b][c * 4 + 2], mm.acc[a][b][c * 4 + 3]};
                     Picked::put(picked_lds, a * 32 + p_in_fragment(c * 4, lane), lane, &v);
                 }
+            lanes_exchange();
             const uint32_t stretch = (G.first + p0) / T.width * T.width, rows_from = (q0 & 63u) + b * 32;
             for (uint32_t i = found_from + lane; i < found_to; i += 64) {
                 const uint32_t word = i < found_from + 64 ? found : list[i];
@@ -584,6 +598,7 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_logits(Operand W, Operand
                 if (p < (uint32_t)(BP / WP) && row < 32)
                     T.z[(size_t)(q0 + b * 32 + row) * T.top + (word & 1023u)] = Picked::value(picked_lds, row, p);
             }
+            lanes_exchange();
         }
         if (MODE == STATISTICS) continue;
         typedef Rows32<2, BP / WP> Out;
@@ -615,7 +630,7 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_logits(Operand W, Operand
 #pragma unroll
                 for (int c = 0; c < 4; ++c) Out::put(mine, a * 32 + p_in_fragment(c * 4, lane), lane, plane ? &lo[a][c] : &hi[a][c]);
             uint16_t* to = (plane ? G.lo : G.hi) + (size_t)(q0 + b * 32) * G.ld + p0;
-            Out::each(mine, lane, [&](uint32_t row, uint32_t p, uint4 v) { *reinterpret_cast<uint4*>(to + (size_t)row * G.ld + p) = v; });
+            Out::each(mine, lane, [&](uint32_t row, uint32_t p, quad v) { *reinterpret_cast<quad*>(to + (size_t)row * G.ld + p) = v; });
         }
     }
 }
@@ -730,8 +745,8 @@ __global__ void __launch_bounds__(256) k_head_dz(HeadPiece G, uint32_t first_row
             const uint32_t p = first + v * 2048;
             const size_t at = (size_t)row * G.ld + p;
             if (p < G.ld) {
-                *reinterpret_cast<uint4*>(hi[v]) = *reinterpret_cast<const uint4*>(G.hi + at);
-                if (WIDE) *reinterpret_cast<uint4*>(lo[v]) = *reinterpret_cast<const uint4*>(G.lo + at);
+                load8(G.hi + at, hi[v]);
+                if (WIDE) load8(G.lo + at, lo[v]);
                 else m[v] = St.m[(size_t)((G.first + p) / group) * St.ld + row];
             }
         }
@@ -762,8 +777,8 @@ __global__ void __launch_bounds__(256) k_head_dz(HeadPiece G, uint32_t first_row
         const uint32_t p = first + v * 2048;
         const size_t at = (size_t)row * G.ld + p;
         if (p < G.ld) {
-            *reinterpret_cast<uint4*>(G.hi + at) = *reinterpret_cast<const uint4*>(hi[v]);
-            if (F32) *reinterpret_cast<uint4*>(G.lo + at) = *reinterpret_cast<const uint4*>(lo[v]);
+            store8(G.hi + at, hi[v]);
+            if (F32) store8(G.lo + at, lo[v]);
         }
     }
 }
@@ -905,7 +920,7 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_dw(Operand H, Planes scal
                     for (int e = 0; e < 4; ++e) four |= (uint64_t)(OUT == OUT_BF16 ? Bf16::bits(v[e]) : F16::bits(v[e])) << (16 * e);
                 Out::put(mine, a * 32 + p_in_fragment(c * 4, lane), lane, OUT == OUT_F32 ? (const void*)&v : (const void*)&four);
             }
-        Out::each(mine, lane, [&](uint32_t row, uint32_t p, uint4 v) {
+        Out::each(mine, lane, [&](uint32_t row, uint32_t p, quad v) {
             const uint32_t q = q0 + b * 32 + row;
             if (q >= n || p0 + p >= dim) return;
             char* to = static_cast<char*>(dw) + ((int64_t)(first + q) * ld_dw + p0 + p) * SIZE;

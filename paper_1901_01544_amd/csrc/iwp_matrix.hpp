@@ -24,6 +24,18 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+// What is written to memory as one type and read as another goes through these: the compiler may not take such accesses apart by their type.
+typedef uint32_t quad __attribute__((ext_vector_type(4), may_alias));
+typedef float f32x4_bytes __attribute__((ext_vector_type(4), may_alias));
+typedef float f32_bytes __attribute__((may_alias));
+typedef uint64_t u64_bytes __attribute__((may_alias));
+
+// Between writes to LDS and reads of them by other lanes of the same wavefront, in either order: no instruction (a wavefront's LDS accesses
+// are done in order), but the compiler must not move them across.
+__device__ __forceinline__ void lanes_exchange() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 
 struct Bf16 {
     typedef __bf16 scalar;
@@ -297,20 +309,22 @@ struct Rows32 {
     // four entries from p on (a multiple of 4) of this lane's row
     static __device__ __forceinline__ void put(char* lds, uint32_t p, int lane, const void* four) {
         char* to = lds + place(lane & 31, p / PER_CHUNK) + (p % PER_CHUNK) * SIZE;
-        if (SIZE == 2) *reinterpret_cast<uint64_t*>(to) = *static_cast<const uint64_t*>(four);
-        else *reinterpret_cast<f32x4*>(to) = *static_cast<const f32x4*>(four);
+        if (SIZE == 2) *reinterpret_cast<u64_bytes*>(to) = *static_cast<const u64_bytes*>(four);
+        else *reinterpret_cast<f32x4_bytes*>(to) = *static_cast<const f32x4_bytes*>(four);
     }
     static __device__ __forceinline__ float value(const char* lds, uint32_t row, uint32_t p) {      // of 4 bytes
-        return *reinterpret_cast<const float*>(lds + place(row, p / 4) + (p % 4) * 4);
+        return *reinterpret_cast<const f32_bytes*>(lds + place(row, p / 4) + (p % 4) * 4);
     }
     // store(row, first entry, 16 bytes) for every chunk
     template <class F>
     static __device__ __forceinline__ void each(const char* lds, int lane, F store) {
+        lanes_exchange();
 #pragma unroll
         for (int i = 0; i < 32 * CHUNKS / 64; ++i) {
             const uint32_t at = i * 64 + lane, row = at / CHUNKS, chunk = at % CHUNKS;
-            store(row, chunk * PER_CHUNK, *reinterpret_cast<const uint4*>(lds + place(row, chunk)));
+            store(row, chunk * PER_CHUNK, *reinterpret_cast<const quad*>(lds + place(row, chunk)));
         }
+        lanes_exchange();
     }
 };
 
