@@ -29,6 +29,7 @@ import argparse
 import hashlib
 import json
 import os
+import re
 import sys
 import time
 
@@ -91,13 +92,21 @@ def threshold_dominant_bytes(ps, W_acc, W_list, n_lead, pairs):
 
 
 def kernel_source_hash():
-    """sha256 over the kernel sources (file names and contents, sorted): what a counter run was taken on."""
+    """sha256 over the sources of the step's kernels, csrc/iwp_api.hip and all that it includes by a path (file names and contents,
+    sorted): what a counter run was taken on.  Sources of other calls (the losses') do not count."""
+    todo = [os.path.join(ROOT, "paper_1901_01544_amd", "csrc", "iwp_api.hip")]
+    found = {}
+    while todo:
+        path = os.path.normpath(todo.pop())
+        if path in found:
+            continue
+        with open(path, "rb") as f:
+            found[path] = f.read()
+        todo += [os.path.join(os.path.dirname(path), name) for name in re.findall(r'^#include "([^"]+)"', found[path].decode(), re.M)]
     h = hashlib.sha256()
-    d = os.path.join(ROOT, "paper_1901_01544_amd", "csrc")
-    for name in sorted(os.listdir(d)):
-        if name.endswith((".hip", ".hpp", ".h")):
-            h.update(name.encode())
-            h.update(open(os.path.join(d, name), "rb").read())
+    for path in sorted(found):
+        h.update(os.path.basename(path).encode())
+        h.update(found[path])
     return h.hexdigest()
 
 
@@ -238,7 +247,7 @@ def result_block(ps, cfg, route, hinted, W_acc, W_list, pool, steps, warmup, ms_
             "traffic": traffic,
             "traffic_source": ("profiles/traffic.json: rocprofv3 --pmc FETCH_SIZE / WRITE_SIZE on these kernel sources"
                                if traffic is not None else
-                               "none on file for these kernel sources (profiles/traffic.json is stamped with a hash of csrc/)"),
+                               "none on file for these kernel sources (profiles/traffic.json is stamped with a hash of csrc/iwp_api.hip and what it includes)"),
             "algorithmic_bytes_per_launch": dom_bytes,
             "avg_launch_ms": dom_ms,
             "launches_timed": dom_cnt,
