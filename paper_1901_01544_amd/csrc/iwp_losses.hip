@@ -339,9 +339,12 @@ int head_call(const HeadCall& c, uint32_t tokens, uint32_t dim, uint32_t vocab, 
 }
 
 constexpr uint32_t BALANCE_GROUPS = 512;
-// Logits up to which one workgroup does it all: 64 tokens x 8 experts 5.0 us of kernels and 7.5 us a call, as three launches 10.2 and
-// 14.6.  Its 16 wavefronts read this many in four rounds at most.
+// One workgroup does it all where that is up to this many logits, 16 a lane of its 16 wavefronts, or all tokens at once.  us a call, and as
+// three launches: 64 tokens x 8 experts in binary32 6.8 and 11.9; 16 logits a lane: 2048 x 8 11.3 and 11.8, 1024 x 9 12.8 and 11.8, 256 x 33
+// in bf16 12.0 and 11.9; more, where tokens do not fill their lanes (a power of two, 16 bytes or more each): 1820 x 9 20 and 12, 16384 x 1
+// 33 and 12, in bf16 50 and 12.  16 x 1024 at once 11.8 and 19.
 constexpr uint64_t BALANCE_ONE = 16384;
+constexpr uint32_t BALANCE_ONE_LANE = BALANCE_ONE / (BALANCE_ONE_WAVES * 64);
 
 uint32_t balance_groups(uint32_t tokens) { return std::max(1u, std::min(BALANCE_GROUPS, (tokens + 3) / 4)); }
 
@@ -362,7 +365,8 @@ int balance_run(const Router& r, const BalanceGradient& g, float* loss, int32_t*
     auto one = k_balance_one<IN, CHUNKS>;
     auto rows = k_balance_rows<IN, CHUNKS>;
     auto grad = k_balance_grad<IN, CHUNKS>;
-    if ((uint64_t)r.tokens * r.experts <= BALANCE_ONE) {
+    const uint32_t rounds = std::max(1u, BALANCE_ONE_LANE / TokenLanes<IN, CHUNKS>::N);
+    if ((uint64_t)r.tokens * r.experts <= BALANCE_ONE && r.tokens <= rounds * BALANCE_ONE_WAVES * (64 / r.lanes)) {
         IWP_LAUNCH_BLOCK("k_balance_one", one, 1, BALANCE_ONE_WAVES * 64, s, r, g, counts, loss);
         return IWP_OK;
     }
