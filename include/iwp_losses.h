@@ -8,8 +8,10 @@
  * HIP graph may capture them), argument errors found before anything is launched, the same bytes
  * for the same inputs.  What differs: rows may be strided (ld = elements from row to row, the
  * elements of a row lie together), and three types of data are taken:
- *   IWP_F32   products of binary32 operands as three products of their halves (22 bits of each
- *             operand; sums in binary32), everything else in binary32
+ *   IWP_F32   products of binary32 operands as three products of their halves, sums in binary32: 22 bits
+ *             of an element that is at least 2^-27 of its matrix's largest finite one (in h: of the
+ *             tokens that count), 2^-49 of that one below; the logits' gradient likewise, against its
+ *             token's coefficients; everything else in binary32
  *   IWP_BF16, IWP_F16   products of the operands as they are, sums in binary32; the logits'
  *             gradient is rounded to the operands' type before the two products that use it.
  *             IWP_BF16: the logits of the vocabulary's last piece (all of it, if it is worked through
@@ -46,8 +48,8 @@ typedef enum { IWP_F32 = 0, IWP_BF16 = 1, IWP_F16 = 2 } iwp_dtype;
  * first, one of 32 bits is split there); top: the teacher's entries per token (0: cross entropy);
  * piece: vocabulary entries whose logits are held at a time (rounded up to 256), 0 = all of them.  The rest of the vocabulary is worked
  * through in pieces, whose logits are computed a second time for the gradient: at piece >= vocab nothing is
- * computed twice, below it the workspace holds a piece's logits instead of all of them (and 8 bytes per token
- * and 32 to 128 entries of the vocabulary).  256-byte aligned.  0 for sizes that the calls refuse. */
+ * computed twice, below it the workspace holds a piece's logits instead of all of them (and 8 bytes, with a
+ * teacher 12, per token and 32 to 128 entries of the vocabulary).  256-byte aligned.  0 for sizes that the calls refuse. */
 size_t iwp_head_workspace_bytes(uint32_t tokens, uint32_t dim, uint32_t vocab, uint32_t dtype, const void* w, int64_t ld_w,
                                 uint32_t top, uint32_t piece);
 
@@ -87,7 +89,8 @@ int iwp_head_distill(const void* h, int64_t ld_h, const void* w, int64_t ld_w, u
 size_t iwp_balance_workspace_bytes(uint32_t tokens, uint32_t experts);
 
 /* Load balance of a router's choice.  x: [tokens, experts] logits; chosen: [tokens, slots] experts, packed, entries
- * outside [0, experts) are slots given to nobody; keep: [tokens] bytes, 0 = the token does not count, NULL = all count.
+ * outside [0, experts) are slots given to nobody; keep: [tokens] bytes, 0 = the token does not count, NULL = no token is left out by it.
+ * A token whose logits are all -inf does not count either.
  * With N tokens that count, p = softmax(x), L = log sum exp x, share_e = counts[e] / (N * slots):
  *   counts[e] = slots given to expert e
  *   loss[0] = experts * sum_e share_e * mean(p_e),  loss[1] = mean(L^2)

@@ -257,7 +257,8 @@ __device__ __forceinline__ float split_scale(uint32_t max_bits) {
     const int e = max(1, (int)(max_bits >> 23)) - 127;
     return __uint_as_float((uint32_t)min(127 + 13 - e, 254) << 23);
 }
-// A sum of products of two split operands -> the sum itself, in two factors that are normal numbers.
+// A sum of products of two split operands -> the sum itself.  In two factors, each a power of two that binary32 has: their product may lie
+// outside it.
 __device__ __forceinline__ float unsplit(float sum, float sp, float sq) { return sum * (1.0f / sp) * (1.0f / sq); }
 
 // Eight entries of 16 bits at a 16-byte aligned place
