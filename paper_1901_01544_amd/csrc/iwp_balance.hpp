@@ -5,7 +5,7 @@
 // The counts are needed before the first gradient, so the logits are read twice; the second time they come from the memory-side
 // cache where they fit.  131072 tokens x 256 experts in binary32 (134 MB): sums 41 us (3.3 TB/s), joining the workgroups' sums 6,
 // gradient 50 (5.4 TB/s read and written).  With a wavefront per token, which takes six steps to a sum instead of four and a
-// quarter of the tokens to a step, the sums took 102 us.  16384 x 64 in bf16: 6 + 6 + 6 us, launches for the most part.
+// quarter of the tokens to a step, the sums took 102 us.  16384 x 64 in bf16: 5 + 5 + 5 us, launches for the most part.
 #pragma once
 
 #include <hip/hip_runtime.h>

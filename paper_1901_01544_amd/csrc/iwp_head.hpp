@@ -67,7 +67,7 @@ static_assert(IWP_MAX_TOP <= 1u << 10 && IWP_MAX_VOCAB / STRETCHES <= 1u << 16, 
 // ------------------------------------------------------------------ tokens
 
 // Softmax of the teacher's entries of one token at temperature t; a wavefront per token.  An index that occurs again hands its share to
-// the first of its kind, for which every entry is compared with every other in LDS: 13 us for 4096 tokens of 64 entries.
+// the first of its kind, for which every entry is compared with every other in LDS: 11 us for 4096 tokens of 64 entries.
 __global__ void __launch_bounds__(256) k_head_teacher(const int32_t* __restrict__ index, const float* __restrict__ logit,
                                                       const int32_t* __restrict__ label, uint32_t tokens, uint32_t vocab, Teacher T) {
     __shared__ int32_t at[4][IWP_MAX_TOP];
@@ -130,9 +130,9 @@ __global__ void __launch_bounds__(256) k_head_teacher(const int32_t* __restrict_
     }
 }
 
-// One workgroup: numbers the tokens that count, in order, and finds the powers of two of their coefficients.  The products then run over those tokens
-// alone: what stands in the others' rows is never read, nor computed with.  Bound by its rounds of 1024 tokens, each two
-// barriers: 5 us for 1000 tokens, 13 us for 8192.
+// One workgroup: numbers the tokens that count, in order, and finds the powers of two of their coefficients.  The products then run over
+// those tokens alone: what stands in the others' rows is never read, nor computed with.  Bound by its rounds of 1024 tokens, each two
+// barriers: 5 us for 1000 tokens, 9 for 4096, 16 for 8192.
 __global__ void __launch_bounds__(1024) k_head_rows(const int32_t* __restrict__ label, const float* __restrict__ weight,
                                                     const uint8_t* __restrict__ any, uint32_t tokens, uint32_t vocab, float hard,
                                                     float soft, float t, HeadRows R, float* __restrict__ loss,
@@ -201,8 +201,8 @@ __global__ void __launch_bounds__(1024) k_head_rows(const int32_t* __restrict__ 
 }
 
 // Sorts the teacher's entries of 64 rows into stretches of the vocabulary, for the logits' product, whose wavefronts then find theirs
-// without a search.  Inside a stretch their order is nobody's concern.  4096 tokens x 2048 x 32768 with 64 entries: 11 us here and
-// 45 us more in the product.  A dot product of its own for every entry, a wavefront each, took 409 us; reading the rows' entries
+// without a search.  Inside a stretch their order is nobody's concern.  4096 tokens x 2048 x 32768 with 64 entries: 9 us here and
+// 12 us more in the product.  A dot product of its own for every entry, a wavefront each, took 409 us; reading the rows' entries
 // in the product's epilogue 190, with all of a wavefront's rows on their way at once 135.
 __global__ void __launch_bounds__(1024) k_head_sort(HeadRows R, Teacher T, const HeadScalars* __restrict__ S) {
     __shared__ uint32_t n[STRETCHES], in_wave[16];
@@ -294,8 +294,8 @@ struct Spread {
 };
 
 // The first `blocks` workgroups take one matrix, the others another; 16 rows of 1024 elements at a time.  Few and large workgroups: each
-// ends in an atomic on one word, and those take 20 ns one after the other (75 MB: 19 us with 320 workgroups, 37 to 41 with 2560).
-// Operands of fp16: one matrix, and only where its rows are about to be scaled.
+// ends in an atomic on one word, and those take 20 ns one after the other (75 MB: 19 to 21 us with 320 workgroups, 37 to 41 with
+// 2560).  Operands of fp16: one matrix, and only where its rows are about to be scaled (67 MB: 30 us).
 template <bool F32>
 __global__ void __launch_bounds__(1024) k_head_max(HeadMatrix A, HeadMatrix B, uint32_t blocks, HeadScalars* __restrict__ S) {
     if (!F32 && S->alike) return;
@@ -357,7 +357,8 @@ __device__ __forceinline__ void split_f32(float x, float s, uint16_t* hi, uint16
 // A matrix into rows of ld_out, zeros past its width; with `count`, zeros in the rows behind it up to the next multiple of 64.  Eight
 // elements of four rows a thread: four loads on their way.  32003 rows of 1001 in bf16 (130 MB) 28 us, 4.6 TB/s; with one row a thread
 // 48 us.  SCALED: where the tokens' exponents differ, also the rows times 2^(the row's exponent - the largest), in binary32 rounded once:
-// in bf16 that is exact; fp16 takes them at the scale of the matrix's largest element, as the halves of binary32 are taken.
+// in bf16 that is exact; fp16 takes them at the scale of the matrix's largest element, as the halves of binary32 are taken.  8192 x 4096 in
+// bf16 41 us instead of 31, in a call of 2.86 ms at 16384 entries.
 struct Planes { uint16_t *hi, *lo; };              // lo: of binary32 operands
 constexpr uint32_t PACK_ROWS = 4;
 template <class E, bool F32, bool SCALED>
@@ -729,7 +730,7 @@ __device__ __forceinline__ bool target_dz(uint32_t k, const HeadPiece& G, uint32
 
 // In place on a kept piece: a workgroup takes 4096 entries of a row, twice eight a thread.  The label's entry is put right here, the
 // teacher's are by k_head_targets (handed around through LDS in here they cost 65 us at 4096 x 32768, there 9).  Bound by memory:
-// 8192 x 131072 entries of 2 bytes 740 us, 5.8 TB/s; with eight entries a thread 850.
+// 8192 x 131072 entries of 2 bytes 750 us, 5.7 TB/s; with eight entries a thread 850.
 constexpr uint32_t DZ_ACROSS = 4096;
 template <class E, bool F32, bool WIDE, bool SOFT>
 __global__ void __launch_bounds__(256) k_head_dz(HeadPiece G, uint32_t first_row, uint32_t group, HeadStats St, HeadRows R, Teacher T,
@@ -883,7 +884,7 @@ __global__ void __launch_bounds__(256) k_head_dh_out(const float* __restrict__ s
 }
 
 // dW of a piece: rows of the vocabulary, summed over the rows of tokens.  Where tokens are few it is bound by writing dW: 5 tokens x 768 x
-// 8192 7 us, 684 x 1001 x 32003 with rows of odd length 51 us (90 us while those were written element by element).
+// 8192 7 us, 684 x 1001 x 32003 with rows of odd length 51 to 54 us (90 us while those were written element by element).
 template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool F32>
 __global__ void __launch_bounds__(WP * WQ * 64) k_head_dw(Operand H, Planes scaled, Operand G, float scale, void* __restrict__ dw, int64_t ld_dw,
                                                           uint32_t first, uint32_t dim, const HeadScalars* __restrict__ S) {

@@ -30,7 +30,10 @@ uint32_t tiles_of(uint32_t np, uint32_t nq) { return (np + T::BP - 1) / T::BP * 
 // The largest tile of which there are enough for most of the 256 compute units.  us with the large tile and with the one taken: logits of
 // 5 tokens x 768 x 8192 (32 large tiles, 128 small) 24.6 and 11.7, its dH 14.0 and 7.8; binary32 logits of 37 x 512 x 1000 (4, 16)
 // 34.9 and 16.7, its dH 30.5 and 16.1, its dW (8, 128) 11.0 and 4.7; dW of 800 x 640 x 10007 (120 large, 395 middling) 60.2 and
-// 40.5.  With 160 large tiles (the binary32 logits of that size) they take 57 us, two thirds of the rate of a full chip.
+// 40.5.  At the limit, logits and dW of 1024 tokens x 1024 in bf16, large tiles and middling ones (small):
+//   64 large tiles   33 and 29   21 and 20 (24 and 24)        160   33 and 29   36 and 34
+//   128              33 and 29   26 and 24                    192   35 and 31   36 and 34      256   39 and 36   43 and 40
+// in binary32 96 tiles 65, 50; 160 tiles 72, 87.  (Two middling tiles fit a compute unit: 128 large ones make 512, one round of the chip.)
 constexpr uint32_t ENOUGH_TILES = 160;
 TileKind tile_for(uint32_t np, uint32_t nq) {
     if (tiles_of<Big>(np, nq) >= ENOUGH_TILES) return BIG;
@@ -93,6 +96,8 @@ bool readable(const void* w, int64_t ld_w, uint32_t dim, uint32_t dtype) {
     return dtype != IWP_F32 && aligned(w, 16) && ld_w % 8 == 0 && dim % 8 == 0;
 }
 
+// A split's sums are tokens x dim in binary32, written and read again.  dH and the joining of its sums, us, with 16, 32 and 64 splits at most: 64
+// tokens x 1024 x 131072 107, 73, 92; 100 x 512 x 131072 156, 89, 59; 256 x 1024 x 131072 207, 134, 118; 64 x 512 x 32768 30, 24, 27.
 constexpr uint32_t MAX_SPLITS = 32;
 
 uint32_t held(uint32_t vocab, uint32_t piece) {         // entries of the vocabulary whose logits are held at a time
@@ -115,7 +120,9 @@ HeadPlan head_plan(uint32_t tokens, uint32_t dim, uint32_t vocab, uint32_t dtype
     p.logits_tile = p.rows < Big::BQ ? FEW : tile_for(p.piece, p.tokens);   // a tile's rows are all written
     p.group = p.logits_tile == BIG ? Big::GROUP : p.logits_tile == MID ? Mid::GROUP : Few::GROUP;
     p.groups = (uint32_t)(((uint64_t)p.pieces * p.ld_logits + p.group - 1) / p.group);
-    // dH has few tiles and a long sum: its vocabulary is split until the compute units are full, at least 8 LDS tiles each
+    // dH has few tiles and a long sum: its vocabulary is split until the compute units are full, at least 8 LDS tiles each.  Up to 64 tokens
+    // small tiles, above that large ones: 64 x 512 x 32768 16 us, 100 x 512 x 32768 27 (small tiles 18), 200 x 768 x 32768 32 (35), 256 x 1024
+    // x 131072 121 (181)
     const uint32_t steps = (p.piece + BK - 1) / BK;
     p.dh_tile = tokens <= Few::BQ ? FEW : BIG;
     const uint32_t tiles = std::max(1u, p.dh_tile == FEW ? tiles_of<Few>(dim, tokens) : tiles_of<Big>(dim, tokens));

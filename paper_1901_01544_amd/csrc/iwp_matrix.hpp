@@ -6,7 +6,7 @@
 // entries of P for one entry of Q: P is the index that is contiguous in the product, Q its row.
 //
 // Bound by the matrix cores and the power that they draw.  8192 tokens x 4096 x 131072 entries in bf16, 8.8 TFLOP a product: logits
-// with their statistics 7.2 to 7.4 ms (1.2 PFLOP/s), dH 7.1 to 7.3, dW 7.0 to 7.2 (1.2 to 1.26); the library's products of
+// with their statistics 7.0 to 7.4 ms (1.2 to 1.26 PFLOP/s), dH 6.8 to 7.3, dW 7.0 to 7.2 (1.2 to 1.3); the library's products of
 // 8192^3 reach 1.40, 1.23 and 1.09 for the same three layouts.  The matrix cores are busy 63 to 67 % of the cycles, at a clock of
 // 1.75 to 1.82 GHz instead of 2.4; LDS has no bank conflicts, and what is fetched from memory is 7 GB a product.
 #pragma once
