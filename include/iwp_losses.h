@@ -60,8 +60,9 @@ size_t iwp_head_workspace_bytes(uint32_t tokens, uint32_t dim, uint32_t vocab, u
  *   dh, dw  = gradients of scale * sum_i loss[i]
  * A token that does not count has loss 0, a dh row of zeros, and no part in dw whatever its row of h holds.  (A NaN or an
  * infinity in the row of a token that counts, in w or in a weight makes what depends on it NaN or infinite, as by the definition: a weight
- * its own token's loss and dh row, and dw.)  A token's dh row has the same relative error whatever the weights are.  In dw a token's
- * part is exact to that error or, where that is more, to 2^-48 (IWP_F32) or 2^-37 (IWP_F16) of the largest weight's times the largest |h|.
+ * its own token's loss and dh row, and dw; an infinity in w all losses and gradients, also where its logits are -inf.)  A token's dh
+ * row has the same relative error whatever the weights are.  In dw a token's part is exact to that error or, where that is more,
+ * to 2^-48 (IWP_F32) or 2^-37 (IWP_F16) of the largest coefficient (the weight times what it multiplies) times the largest |h|.
  * loss: [tokens], binary32.  dh: [tokens, dim], h's type, or NULL.  dw: [vocab, dim], of dw_dtype (the operands' type, or
  * IWP_F32 as the flat gradients of iwp.h are), or NULL.  Both gradients are written, not added to.
  * IWP_EINVAL: sizes of 0 (tokens may be 0) or above the limits, pointers missing, scale not finite, rows that overlap;

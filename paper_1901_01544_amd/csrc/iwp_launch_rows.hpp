@@ -11,7 +11,7 @@ namespace iwp {
 constexpr uint64_t MOST_THREADS = 0xffffffffu;
 
 // f(first row, workgroups) for launches of `threads` to a workgroup that take rows_per_block rows by `across` workgroups; the first result
-// that is not 0, or 0.  Only sizes beyond most memories take a second launch.
+// that is not 0, or 0.  across * threads fits 32 bits.  Only sizes beyond most memories take a second launch.
 template <class F>
 int in_launches(uint32_t rows, uint32_t rows_per_block, uint32_t across, uint32_t threads, F f) {
     const uint64_t most = MOST_THREADS / threads / across * rows_per_block;
