@@ -1,0 +1,63 @@
+/*
+ * iwp_experts.h -- C ABI of a routed layer's operators: the choice of experts with its gradient, and the
+ * products of every token's rows with the matrices of the experts chosen for it, with theirs.
+ *
+ * Conventions are those of iwp_losses.h: device pointers, caller-owned buffers, kernels enqueued on
+ * `hip_stream` and nothing else, argument errors found before anything is launched, the same bytes
+ * for the same inputs, strided rows (ld = elements from row to row), data of iwp_dtype.
+ */
+#ifndef IWP_EXPERTS_H
+#define IWP_EXPERTS_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "iwp_losses.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef enum { IWP_SOFTMAX = 0, IWP_SIGMOID = 1 } iwp_scores;
+
+#define IWP_MAX_ROWS (1u << 24)                 /* tokens x slots of the products */
+
+/* ------------------------------------------------------------------ the choice */
+
+/* Chooses `slots` experts for every token from a router's logits.  x: [tokens, experts]; with s = softmax(x) over
+ * the token's experts or 1 / (1 + exp(-x)), and bias: [experts] binary32, or NULL for zeros:
+ *   c_e        = s_e + bias_e, by which experts are chosen, in binary64 (without a bias: by the logits themselves, in
+ *                whose order the scores are)
+ *   groups     the experts in `groups` equal runs, of which a token may use the top_groups with the largest sum of their
+ *                group_top (1 or 2) largest c
+ *   chosen[k]  the experts with the largest c there, the largest first; among equals (of experts and of groups) the lower index
+ *   weight[k]  scale * s_e of the k-th, with `renormalise` scale * s_e / (sum of s over the token's chosen experts); the bias has no part in it
+ * Experts whose logit is -inf or NaN or whose c is -inf or NaN are never chosen; slots that are left over hold -1 and weight 0, and
+ * so do all slots of tokens with keep[i] == 0 (keep: [tokens] bytes, NULL = every token counts).  A token with a NaN among its logits has
+ * weights of NaN.  A logit of +inf makes a softmax NaN, as by the definition; such a token's weights are NaN, its choice without a bias is
+ * by the logits' order.
+ * chosen: [tokens, slots] int32, weight: [tokens, slots] binary32, packed: `chosen` is what iwp_balance and
+ * iwp_expert_product take.  No workspace.
+ * IWP_EINVAL: experts of 0 or above IWP_MAX_EXPERTS, tokens above IWP_MAX_TOKENS (0 tokens: nothing is done), groups that do not divide the
+ * experts, slots of 0 or more than top_groups * experts / groups, group_top above experts / groups, scale not finite, pointers missing,
+ * ld_x < experts; IWP_EALIGN: a buffer not aligned to its elements. */
+int iwp_route(const void* x, int64_t ld_x, uint32_t tokens, uint32_t experts, uint32_t dtype, const float* bias,
+              uint32_t scores, uint32_t groups, uint32_t top_groups, uint32_t group_top, uint32_t renormalise, float scale,
+              const uint8_t* keep, int32_t* chosen, float* weight, uint32_t slots, void* hip_stream);
+
+/* The logits' gradient: dx = plus + sum_k dweight[k] * (gradient of weight[k]), rounded once.  chosen, dweight: [tokens, slots], packed,
+ * chosen[] distinct experts as iwp_route wrote them; entries outside [0, experts) are left out, whatever their dweight.  plus: NULL, or
+ * another gradient of x of its type (that of iwp_balance, say), which may be dx itself.  With D_j the dweight of the slot that holds j, or 0:
+ *   softmax                dx_j = scale s_j (D_j - sum_k dweight_k s_k)
+ *   softmax, renormalised  dx_j = scale v_j (D_j - sum_k dweight_k v_k) for chosen j, else 0; v = s / (sum of s over the chosen)
+ *   sigmoid                dx_j = scale s_j (1 - s_j) D_j
+ *   sigmoid, renormalised  dx_j = scale v_j (1 - s_j) (D_j - sum_k dweight_k v_k) for chosen j
+ * Rows of tokens with keep[i] == 0 are plus, or 0.  An expert that occurs twice in a row of chosen[] counts as two slots.  Everything else as above. */
+int iwp_route_gradient(const void* x, int64_t ld_x, uint32_t tokens, uint32_t experts, uint32_t dtype, const int32_t* chosen,
+                       const float* dweight, uint32_t slots, uint32_t scores, uint32_t renormalise, float scale,
+                       const uint8_t* keep, const void* plus, int64_t ld_plus, void* dx, int64_t ld_dx, void* hip_stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* IWP_EXPERTS_H */

@@ -13,7 +13,7 @@ import sys
 import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SOURCES = [os.path.join(HERE, "csrc", name) for name in ("iwp_api.hip", "iwp_losses.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("iwp_api.hip", "iwp_losses.hip", "iwp_experts.hip", "iwp_clip.hip")]
 LIB = os.path.join(HERE, "libiwp.so")
 CALL_SRC = os.path.join(HERE, "csrc", "call.cpp")
 # named after the interpreter's version, so that another one fails to import it instead of loading it

@@ -1,6 +1,6 @@
-// The Python binding's way into the library: arguments of the hot calls -> the C functions of include/iwp.h and
-// include/iwp_losses.h.  Argument marshalling only; the library itself is opened by iwp.py, which hands over its functions'
-// addresses (bind, bind_losses).
+// The Python binding's way into the library: arguments of the hot calls -> the C functions of include/iwp.h, include/iwp_losses.h,
+// include/iwp_experts.h and include/iwp_clip.h.  Argument marshalling only; the library itself is opened by iwp.py, which hands over its
+// functions' addresses (bind, bind_losses, bind_layers).
 //
 // Bound by the host: a call is a few launches of 3 us each, and through ctypes the arguments of one took 4 to 8 us (0.4 us per
 // tensor for its three checks, 0.9 us per table of workers, 1.1 us for the call).  A small exchange (two calls, one launch
@@ -16,6 +16,8 @@
 #include <utility>
 
 #include "../../include/iwp.h"
+#include "../../include/iwp_clip.h"
+#include "../../include/iwp_experts.h"
 #include "../../include/iwp_losses.h"
 
 namespace {
@@ -141,6 +143,8 @@ PyObject* call(const char* name, int (*f)(A...), PyObject* const* args, Py_ssize
 
 #define EACH_LOSS_CALL(DO) DO(iwp_head_cross_entropy) DO(iwp_head_distill) DO(iwp_balance)
 
+#define EACH_LAYER_CALL(DO) DO(iwp_route) DO(iwp_route_gradient) DO(iwp_clip)
+
 #define DO(name)                                                                    \
     decltype(&::name) f_##name = nullptr;                                           \
     PyObject* py_##name(PyObject*, PyObject* const* args, Py_ssize_t n) {           \
@@ -148,9 +152,10 @@ PyObject* call(const char* name, int (*f)(A...), PyObject* const* args, Py_ssize
     }
 EACH_HOT_CALL(DO)
 EACH_LOSS_CALL(DO)
+EACH_LAYER_CALL(DO)
 #undef DO
 
-// bind({name: address}), bind_losses({name: address}): where the loaded library's functions are.
+// bind({name: address}), bind_losses({name: address}), bind_layers({name: address}): where the loaded library's functions are.
 #define DO(name)                                                                                              \
     {                                                                                                         \
         PyObject* o = PyDict_GetItemString(addresses, #name);                                                 \
@@ -167,6 +172,11 @@ PyObject* bind(PyObject*, PyObject* addresses) {
 PyObject* bind_losses(PyObject*, PyObject* addresses) {
     if (!PyDict_Check(addresses)) return PyErr_Format(PyExc_TypeError, "a dict of addresses");
     EACH_LOSS_CALL(DO)
+    Py_RETURN_NONE;
+}
+PyObject* bind_layers(PyObject*, PyObject* addresses) {
+    if (!PyDict_Check(addresses)) return PyErr_Format(PyExc_TypeError, "a dict of addresses");
+    EACH_LAYER_CALL(DO)
     Py_RETURN_NONE;
 }
 #undef DO
@@ -187,17 +197,25 @@ PyObject* loss_names(PyObject*, PyObject*) {
     EACH_LOSS_CALL(DO)
     return out;
 }
+PyObject* layer_names(PyObject*, PyObject*) {
+    PyObject* out = PyList_New(0);
+    EACH_LAYER_CALL(DO)
+    return out;
+}
 #undef DO
 
 PyMethodDef methods[] = {
 #define DO(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr},
     EACH_HOT_CALL(DO)
     EACH_LOSS_CALL(DO)
+    EACH_LAYER_CALL(DO)
 #undef DO
     {"bind", bind, METH_O, nullptr},
     {"bind_losses", bind_losses, METH_O, nullptr},
+    {"bind_layers", bind_layers, METH_O, nullptr},
     {"names", names, METH_NOARGS, nullptr},
     {"loss_names", loss_names, METH_NOARGS, nullptr},
+    {"layer_names", layer_names, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -18,16 +18,12 @@
 
 namespace iwp {
 
-constexpr float LOG2E = 1.44269504088896340736f;
 // A row of dz is held relative to its own token's coefficients: divided by 2^e, the power of two at or below |c1| + |c2|, an entry is less
 // than 2 in size.  Times 2^14, fp16 has room for entries down to 2^-38 of the coefficients, the halves of binary32 down to 2^-49, and none
 // overflows.  dH's rows take 2^e back one by one.  dW sums over the tokens: its product takes hidden states times 2^(e - the largest
 // e), a copy of them that is made where the tokens' powers differ.
 constexpr int DZ_BITS = 14;
 constexpr int32_t NO_EXPONENT = 1 << 20;           // of coefficients that are 0, infinite or NaN: not scaled, and no other token's concern
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
 
 struct HeadScalars {
     uint32_t count;        // tokens that count
@@ -261,36 +257,12 @@ __device__ __forceinline__ float split_scale(uint32_t max_bits) {
 // outside it.
 __device__ __forceinline__ float unsplit(float sum, float sp, float sq) { return sum * (1.0f / sp) * (1.0f / sq); }
 
-// Eight entries of 16 bits at a 16-byte aligned place
-__device__ __forceinline__ void load8(const uint16_t* from, uint16_t (&x)[8]) {
-    const quad v = *reinterpret_cast<const quad*>(from);
-    __builtin_memcpy(x, &v, 16);
-}
-__device__ __forceinline__ void store8(uint16_t* to, const uint16_t (&x)[8]) {
-    quad v;
-    __builtin_memcpy(&v, x, 16);
-    *reinterpret_cast<quad*>(to) = v;
-}
-
 struct HeadMatrix {        // rows of a caller's matrix; those of `token` alone where it is given, `count` of them
     const void* x;
     int64_t ld;
     uint32_t rows, dim;
     const uint32_t* token;
     const uint32_t* count;
-};
-
-// 128-bit and 64-bit accesses at an element's own alignment
-typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(4), may_alias));
-typedef uint32_t words4_any __attribute__((ext_vector_type(4), aligned(2), may_alias));
-typedef uint16_t halves4_any __attribute__((ext_vector_type(4), aligned(2), may_alias));
-
-// How a kernel's 256 threads lie over rows of `chunks` units: 2^shift threads to a row, the rest of the row by further workgroups.
-struct Spread {
-    uint32_t shift, across;
-    __host__ __device__ uint32_t rows() const { return 256u >> shift; }        // of a workgroup
-    __device__ __forceinline__ uint32_t row() const { return blockIdx.x / across * rows() + (threadIdx.x >> shift); }
-    __device__ __forceinline__ uint32_t unit() const { return (blockIdx.x % across << shift) + (threadIdx.x & ((1u << shift) - 1)); }
 };
 
 // The first `blocks` workgroups take one matrix, the others another; 16 rows of 1024 elements at a time.  Few and large workgroups: each
@@ -418,19 +390,6 @@ __global__ void __launch_bounds__(256) k_head_pack(HeadMatrix M, uint32_t first,
             put(scaled, of == NO_EXPONENT ? 0 : of - S->most);
         }
     }
-}
-
-// ------------------------------------------------------------------ the tiles' order
-
-// Workgroups go to the chip's eight dies in turn, and each die has an L2 of its own: each takes a stretch of the tiles in an order
-// in which some dozens in a row share few rows and columns (8 of Q by as many of P as run at a time).
-__device__ __forceinline__ void tile_of(uint32_t block, uint32_t np, uint32_t nq, uint32_t* p, uint32_t* q) {
-    const uint32_t n = np * nq, per = n / 8, more = n % 8, die = block % 8, in = block / 8;
-    const uint32_t at = die * per + min(die, more) + in;
-    constexpr uint32_t TALL = 8;
-    const uint32_t group = at / (np * TALL), first = group * TALL, tall = min(TALL, nq - first), rest = at - group * np * TALL;
-    *p = rest / tall;
-    *q = first + rest % tall;
 }
 
 // ------------------------------------------------------------------ logits
@@ -839,13 +798,6 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_head_dh(Operand W, Operand G, 
                 *to_sum = v;
             }
     }
-}
-
-enum OutType { OUT_F32, OUT_BF16, OUT_F16 };
-template <int OUT>
-__device__ __forceinline__ void put(void* out, int64_t at, float x) {
-    if (OUT == OUT_F32) static_cast<float*>(out)[at] = x;
-    else static_cast<uint16_t*>(out)[at] = OUT == OUT_BF16 ? Bf16::bits(x) : F16::bits(x);
 }
 
 // dH: the splits' sums in order, times what dz and W were scaled by, to the token's row; zeros for tokens that do not count.  Four

@@ -29,6 +29,14 @@ typedef uint32_t quad __attribute__((ext_vector_type(4), may_alias));
 typedef float f32x4_bytes __attribute__((ext_vector_type(4), may_alias));
 typedef float f32_bytes __attribute__((may_alias));
 typedef uint64_t u64_bytes __attribute__((may_alias));
+// 128-bit and 64-bit accesses at an element's own alignment
+typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(4), may_alias));
+typedef uint32_t words4_any __attribute__((ext_vector_type(4), aligned(2), may_alias));
+typedef uint16_t halves4_any __attribute__((ext_vector_type(4), aligned(2), may_alias));
+
+constexpr float LOG2E = 1.44269504088896340736f;
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
 
 // Between writes to LDS and reads of them by other lanes of the same wavefront, in either order: no instruction (a wavefront's LDS accesses
 // are done in order), but the compiler must not move them across.
@@ -50,6 +58,32 @@ struct F16 {
     }
     static __device__ __forceinline__ uint16_t bits(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
     static __device__ __forceinline__ float value(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }
+};
+
+enum OutType { OUT_F32, OUT_BF16, OUT_F16 };
+template <int OUT>
+__device__ __forceinline__ void put(void* out, int64_t at, float x) {
+    if (OUT == OUT_F32) static_cast<float*>(out)[at] = x;
+    else static_cast<uint16_t*>(out)[at] = OUT == OUT_BF16 ? Bf16::bits(x) : F16::bits(x);
+}
+
+// Eight entries of 16 bits at a 16-byte aligned place
+__device__ __forceinline__ void load8(const uint16_t* from, uint16_t (&x)[8]) {
+    const quad v = *reinterpret_cast<const quad*>(from);
+    __builtin_memcpy(x, &v, 16);
+}
+__device__ __forceinline__ void store8(uint16_t* to, const uint16_t (&x)[8]) {
+    quad v;
+    __builtin_memcpy(&v, x, 16);
+    *reinterpret_cast<quad*>(to) = v;
+}
+
+// How a kernel's 256 threads lie over rows of `chunks` units: 2^shift threads to a row, the rest of the row by further workgroups.
+struct Spread {
+    uint32_t shift, across;
+    __host__ __device__ uint32_t rows() const { return 256u >> shift; }        // of a workgroup
+    __device__ __forceinline__ uint32_t row() const { return blockIdx.x / across * rows() + (threadIdx.x >> shift); }
+    __device__ __forceinline__ uint32_t unit() const { return (blockIdx.x % across << shift) + (threadIdx.x & ((1u << shift) - 1)); }
 };
 
 constexpr uint32_t BK = 64;                        // summed entries per LDS tile: 128 bytes of a row
@@ -325,5 +359,16 @@ struct Rows32 {
         lanes_exchange();
     }
 };
+
+// Workgroups go to the chip's eight dies in turn, and each die has an L2 of its own: each takes a stretch of the tiles in an order
+// in which some dozens in a row share few rows and columns (8 of Q by as many of P as run at a time).
+__device__ __forceinline__ void tile_of(uint32_t block, uint32_t np, uint32_t nq, uint32_t* p, uint32_t* q) {
+    const uint32_t n = np * nq, per = n / 8, more = n % 8, die = block % 8, in = block / 8;
+    const uint32_t at = die * per + min(die, more) + in;
+    constexpr uint32_t TALL = 8;
+    const uint32_t group = at / (np * TALL), first = group * TALL, tall = min(TALL, nq - first), rest = at - group * np * TALL;
+    *p = rest / tall;
+    *q = first + rest % tall;
+}
 
 }  // namespace iwp

@@ -57,6 +57,7 @@ def load() -> C.CDLL:
     L = C.CDLL(LIB_PATH)
     call.bind({name: C.cast(getattr(L, name), _vp).value for name in call.names()})
     call.bind_losses({name: C.cast(getattr(L, name), _vp).value for name in call.loss_names()})
+    call.bind_layers({name: C.cast(getattr(L, name), _vp).value for name in call.layer_names()})
     # prototypes of every call, also of those that go through _call: for callers that use the library by ctypes
     L.iwp_workspace_bytes.argtypes = [C.c_uint32, C.c_uint32]
     L.iwp_workspace_bytes.restype = C.c_size_t
@@ -113,6 +114,12 @@ def load() -> C.CDLL:
     L.iwp_head_workspace_bytes.restype = C.c_size_t
     L.iwp_balance_workspace_bytes.argtypes = [C.c_uint32, C.c_uint32]
     L.iwp_balance_workspace_bytes.restype = C.c_size_t
+    L.iwp_tensors_create.argtypes = [C.POINTER(Layer), C.c_uint32, C.POINTER(_vp)]
+    L.iwp_tensors_create.restype = C.c_int
+    L.iwp_tensors_destroy.argtypes = [_vp]
+    L.iwp_tensors_destroy.restype = None
+    L.iwp_tensors_workspace_bytes.argtypes = [_vp, C.c_uint32]
+    L.iwp_tensors_workspace_bytes.restype = C.c_size_t
     L.iwp_strerror.argtypes = [C.c_int]
     L.iwp_strerror.restype = C.c_char_p
     L.iwp_last_hip_error.argtypes = []

@@ -1,0 +1,153 @@
+"""Clipping of the workers' gradients against its definition in 64 bits."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+HALF = 2.0 ** -24
+TABLES = {
+    "one element": [(0, 1)], "one short": [(3, 5)], "odd": [(1, 2047), (2048, 2048), (4097, 2049), (6151, 3)], "with empty ones": [(0, 0), (7, 100), (200, 0)],
+    "one workgroup's last": [(0, 64 * 2048)], "two launches' first": [(0, 64 * 2048 + 1)], "many small": [(17 * i, 1 + i % 16) for i in range(3000)],
+    "long": [(64, 5_000_003), (5_000_100, 77), (5_000_200, 1_234_567)],
+}
+
+
+@pytest.fixture(scope="module")
+def clipping(gpu_lib):
+    from paper_1901_01544_amd import clipping
+    return clipping
+
+
+def gradients(rows, W, seed=0, size=1.0, pad=5):
+    flat = max(o + n for o, n in rows) + pad
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    return [size * 2.0 ** p * torch.randn(flat, generator=gen, device=DEV) for p in range(W)]
+
+
+def call(clipping, rows, g, out, W=None, **how):
+    tensors = clipping.Tensors(rows)
+    norm = torch.full((len(g),), float("nan"), device=DEV)
+    ws = torch.full((tensors.workspace_bytes(len(g)),), 0xFF, dtype=torch.uint8, device=DEV)
+    clipping.clip(tensors, g, out, norm, ws, **how)
+    return norm
+
+
+def check(rows, g, out, before, norm, max_norm=float("inf"), scale=1.0):
+    """out's elements of the tensors: one rounding; what lies between them as it was."""
+    inside = torch.zeros(out[0].numel() if out[0] is not None else 0, dtype=torch.bool, device=DEV)
+    for o, n in rows:
+        inside[o:o + n] = True
+    for p, (a, b) in enumerate(zip(g, out)):
+        x = torch.where(inside, a.double(), 0.0)
+        want = x.square().sum().sqrt() * abs(scale)
+        assert abs(norm[p].double() - want) <= HALF * want * 1.01 + 2.0 ** -150, (norm[p].item(), want.item())
+        by = scale * min(1.0, max_norm / want.item()) if want.item() else scale
+        y = x * by
+        assert ((b.double() - y).abs()[inside] <= 1.01 * HALF * y.abs()[inside] + 2.0 ** -150).all()
+        assert torch.equal(b[~inside], before[p][~inside])
+
+
+@pytest.mark.parametrize("rows", TABLES.values(), ids=TABLES.keys())
+@pytest.mark.parametrize("W", [1, 3, 8])
+def test_norm_and_clipped(clipping, rows, W):
+    n = sum(n for _, n in rows)
+    g = gradients(rows, W)
+    for max_norm, scale in ((1.5 * n ** 0.5, 1.0), (0.25 * n ** 0.5, 0.125), (float("inf"), -1.0 / 3)):
+        before = [torch.full_like(x, 7.0) for x in g]
+        out = [x.clone() for x in before]
+        norm = call(clipping, rows, g, out, max_norm=max_norm, scale=scale)
+        check(rows, g, out, before, norm, max_norm, scale)
+        onto = [x.clone() for x in g]
+        again = call(clipping, rows, onto, onto, max_norm=max_norm, scale=scale)
+        assert torch.equal(again, norm)
+        check(rows, g, onto, g, norm, max_norm, scale)
+        assert torch.equal(call(clipping, rows, g, None, max_norm=max_norm, scale=scale), norm)
+
+
+def test_any_alignment(clipping):
+    """Flat buffers that begin at any element."""
+    rows = [(3, 10001), (10010, 300_000)]
+    for shift in (0, 1, 2, 3):
+        whole = gradients(rows, 2, seed=1, pad=20)
+        g = [x[shift:] for x in whole]
+        before = [torch.zeros_like(x)[3 - shift:] for x in whole]
+        n = min(x.numel() for x in g + before)
+        g, out = [x[:n] for x in g], [x[:n] for x in before]
+        norm = call(clipping, rows, g, out, max_norm=100.0)
+        check(rows, g, out, [torch.zeros_like(x) for x in out], norm, 100.0)
+
+
+@pytest.mark.parametrize("rows", [[(0, 5000)], [(0, 500_000)]], ids=["one launch", "two"])
+def test_workers_without_a_gradient(clipping, rows):
+    g = gradients(rows, 4, seed=2)
+    out = [x.clone() for x in g]
+    g[1] = g[3] = None
+    out[0] = None
+    norm = call(clipping, rows, g, out, max_norm=1.0)
+    assert norm[1] == 0 == norm[3] and norm[0] > 1 and torch.isfinite(norm).all()
+    same = gradients(rows, 4, seed=2)
+    assert torch.equal(out[1], same[1]) and torch.equal(out[3], same[3]) and not torch.equal(out[2], same[2])
+
+
+@pytest.mark.parametrize("n", [3000, 300_000])
+def test_values_at_the_ends_of_binary32(clipping, n):
+    rows = [(0, n)]
+    for size in (1e38, 1e-42, 0.0):
+        g = [torch.full((n,), size, device=DEV)]
+        out = [torch.empty_like(g[0])]
+        norm = call(clipping, rows, g, out, max_norm=1.0)
+        want = float(g[0][0].double()) * n ** 0.5
+        got = float("inf") if want > 3.4028235e38 else want
+        assert norm.item() == got or abs(norm.item() - got) <= 2 * HALF * got + 2.0 ** -149
+        y = float(g[0][0].double()) * min(1.0, 1.0 / want if want else 1.0)
+        assert ((out[0].double() - y).abs() <= 2 * HALF * abs(y) + 2.0 ** -149).all()
+    g = [torch.ones(n, device=DEV) for _ in range(3)]
+    g[0][n // 2], g[1][n - 1] = float("nan"), float("-inf")
+    out = [torch.empty_like(x) for x in g]
+    norm = call(clipping, rows, g, out, max_norm=1.0)
+    assert norm[0].isnan() and out[0].isnan().all()
+    assert norm[1].item() == float("inf") and out[1][-1].isnan() and (out[1][:-1] == 0).all()
+    assert torch.isfinite(out[2]).all()
+
+
+def test_zero_max_norm(clipping):
+    rows = [(0, 100), (128, 70_000)]
+    g = gradients(rows, 2, seed=3)
+    g[1].zero_()
+    out = [torch.full_like(x, 7.0) for x in g]
+    norm = call(clipping, rows, g, out, max_norm=0.0)
+    assert norm[0] > 0 and norm[1] == 0 and all((x[:100] == 0).all() and (x[128:70128] == 0).all() and (x[100:128] == 7).all() for x in out)
+
+
+@pytest.mark.parametrize("rows", [[(0, 5000)], [(0, 3_000_001)]], ids=["one launch", "two"])
+def test_same_bytes_on_another_stream_and_in_a_graph(clipping, rows):
+    g = gradients(rows, 5, seed=4)
+    tensors = clipping.Tensors(rows)
+
+    def buffers():
+        return [torch.empty_like(x) for x in g], torch.empty(5, device=DEV), torch.empty(tensors.workspace_bytes(5), dtype=torch.uint8, device=DEV)
+
+    def call(out, norm, ws):
+        clipping.clip(tensors, g, out, norm, ws, max_norm=50.0, scale=0.5)
+        return out, norm
+
+    first = call(*buffers())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        second = call(*buffers())
+    torch.cuda.synchronize()
+    out, norm, ws = buffers()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out, norm, ws)
+    n = rows[0][1]
+    for _ in range(3):
+        for t in out + [norm]:
+            t.fill_(5)
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(first[1], second[1]) and torch.equal(first[1], norm)
+        for a, b, c in zip(first[0], second[0], out):
+            assert torch.equal(a[:n], b[:n]) and torch.equal(a[:n], c[:n])
