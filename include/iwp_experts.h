@@ -57,6 +57,38 @@ int iwp_route_gradient(const void* x, int64_t ld_x, uint32_t tokens, uint32_t ex
                        const float* dweight, uint32_t slots, uint32_t scores, uint32_t renormalise, float scale,
                        const uint8_t* keep, const void* plus, int64_t ld_plus, void* dx, int64_t ld_dx, void* hip_stream);
 
+/* ------------------------------------------------------------------ the products */
+
+/* Products of rows with the matrices of the experts chosen for them.  A row for every slot: row i * slots + k goes to expert chosen[i, k].
+ *   x       [tokens, in], with every token's row for each of its slots, or with x_by_slot [tokens * slots, in], a row for each
+ *   w       [experts, out, in]: ld_w elements from row to row, step_w from matrix to matrix
+ *   chosen  [tokens, slots] int32, packed, as iwp_route writes it; entries outside [0, experts) are slots that nobody got
+ *   y       [tokens * slots, out]: y_r = W_chosen[r] x_r, zeros for slots of nobody
+ * All of one type, sums in binary32, rounded once.  Matrices of experts without rows are not read.  An infinity or a NaN in a row, or in an
+ * expert's matrix, shows in what depends on it by the definition, where an infinity may also make NaN, and nowhere else.
+ * Workspace: iwp_expert_product_workspace_bytes with the same sizes, 256-byte aligned; it has room for the rows gathered by expert
+ * and, where w's rows cannot be read by 16 bytes where they lie (address, ld_w, step_w and in), for a copy of w.
+ * IWP_EINVAL: sizes of 0 (tokens may be 0) or above the limits (IWP_MAX_TOKENS, IWP_MAX_ROWS slots, IWP_MAX_EXPERTS, IWP_MAX_DIM for in and
+ * out), slots above experts, pointers missing, rows that overlap (ld below the width; step below out rows); IWP_EALIGN: a
+ * buffer not aligned to its elements, or the workspace; IWP_ERANGE: rows that lie 2^24 bytes or more apart. */
+size_t iwp_expert_product_workspace_bytes(uint32_t tokens, uint32_t slots, uint32_t experts, uint32_t in, uint32_t out,
+                                          uint32_t dtype, const void* w, int64_t ld_w, int64_t step_w, uint32_t x_by_slot,
+                                          uint32_t gradient);
+int iwp_expert_product(const void* x, int64_t ld_x, uint32_t x_by_slot, const void* w, int64_t ld_w, int64_t step_w,
+                       uint32_t tokens, uint32_t slots, uint32_t experts, uint32_t in, uint32_t out, uint32_t dtype,
+                       const int32_t* chosen, void* y, int64_t ld_y, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Its gradients.  dy: [tokens * slots, out], of x's type; rows of slots of nobody are not read.
+ *   dx  like x, or NULL: W_chosen[r]^T dy_r of a slot's row (zeros for nobody's), or its sum over the token's slots, in binary32 and in their order
+ *   dw  [experts, out, in], of dw_dtype (x's type, or IWP_F32 as the flat gradients of iwp.h are), or NULL: the sum over an expert's rows of
+ *       dy_r x_r^T, zeros for an expert without rows
+ * Both are written, not added to.  Workspace: with gradient = 1. */
+int iwp_expert_product_gradient(const void* x, int64_t ld_x, uint32_t x_by_slot, const void* w, int64_t ld_w, int64_t step_w,
+                                uint32_t tokens, uint32_t slots, uint32_t experts, uint32_t in, uint32_t out, uint32_t dtype,
+                                const int32_t* chosen, const void* dy, int64_t ld_dy, void* dx, int64_t ld_dx, void* dw,
+                                int64_t ld_dw, int64_t step_dw, uint32_t dw_dtype, void* workspace, size_t workspace_bytes,
+                                void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

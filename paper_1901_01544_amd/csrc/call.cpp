@@ -143,7 +143,7 @@ PyObject* call(const char* name, int (*f)(A...), PyObject* const* args, Py_ssize
 
 #define EACH_LOSS_CALL(DO) DO(iwp_head_cross_entropy) DO(iwp_head_distill) DO(iwp_balance)
 
-#define EACH_LAYER_CALL(DO) DO(iwp_route) DO(iwp_route_gradient) DO(iwp_clip)
+#define EACH_LAYER_CALL(DO) DO(iwp_route) DO(iwp_route_gradient) DO(iwp_expert_product) DO(iwp_expert_product_gradient) DO(iwp_clip)
 
 #define DO(name)                                                                    \
     decltype(&::name) f_##name = nullptr;                                           \

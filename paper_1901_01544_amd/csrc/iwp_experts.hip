@@ -4,7 +4,9 @@
 #include <algorithm>
 #include <cmath>
 
+#include "iwp_grouped.hpp"
 #include "iwp_host.hpp"
+#include "iwp_launch_rows.hpp"
 #include "iwp_route.hpp"
 
 using namespace iwp;
@@ -44,6 +46,184 @@ struct TokenGrid {
         blocks = std::min((tokens + waves * at_once - 1) / (waves * at_once), ROUTE_GROUPS);
     }
 };
+
+// ------------------------------------------------------------------ the products
+
+struct Big { static constexpr int BP = 256, BQ = 256, WP = 2, WQ = 4, THREADS = 512; };
+struct Mid { static constexpr int BP = 128, BQ = 128, WP = 2, WQ = 2, THREADS = 256; };
+struct Few { static constexpr int BP = 64, BQ = 64, WP = 2, WQ = 2, THREADS = 256; };
+enum TileKind { BIG, MID, FEW };
+
+template <class F>
+int with_tile(TileKind kind, F f) {
+    switch (kind) {
+        case BIG: return f(Big{});
+        case MID: return f(Mid{});
+        default: return f(Few{});
+    }
+}
+
+template <class T>
+uint64_t tiles_of(uint64_t np, uint64_t nq) { return (np + T::BP - 1) / T::BP * ((nq + T::BQ - 1) / T::BQ); }
+
+constexpr uint64_t ENOUGH_TILES = 160;
+// `each`: entries of Q that one expert has; `many`: experts that have that many
+TileKind tile_for(uint64_t np, uint64_t each, uint64_t many) {
+    if (many * tiles_of<Big>(np, each) >= ENOUGH_TILES && each > Mid::BQ) return BIG;
+    return many * tiles_of<Mid>(np, each) >= ENOUGH_TILES && each > Few::BQ ? MID : FEW;
+}
+
+struct Carver {            // hands out 256-byte aligned parts; at == nullptr: only adds up
+    char* at;
+    size_t used = 0;
+    template <class T>
+    void take(T*& p, size_t n) {
+        p = at ? reinterpret_cast<T*>(at + used) : nullptr;
+        used += (n * sizeof(T) + 255) & ~size_t(255);
+    }
+};
+
+template <class T>
+T round_up(T x, T to) { return (x + to - 1) / to * to; }
+
+struct ProductSizes {
+    uint32_t tokens, slots, experts, in, out, dtype;
+    bool by_slot, gradient;
+    uint32_t rows() const { return tokens * slots; }
+    // rows of the gathered matrices: those of an expert end at a multiple of PAD_ROWS
+    uint32_t padded() const { return rows() + std::min(experts, rows()) * (PAD_ROWS - 1); }
+    bool ok() const {
+        return tokens <= IWP_MAX_TOKENS && slots >= 1 && experts >= 1 && experts <= IWP_MAX_EXPERTS && slots <= experts &&
+               (uint64_t)tokens * slots <= IWP_MAX_ROWS && in >= 1 && in <= IWP_MAX_DIM && out >= 1 && out <= IWP_MAX_DIM && dtype <= IWP_F16;
+    }
+};
+
+struct ProductPlan {
+    uint32_t deep, ld_x, ld_d;             // elements in 128 bytes; widths rounded up to that
+    TileKind rows_tile, dw_tile;
+    uint32_t height, max_tiles;
+    ExpertRows R;
+    char *x, *d, *w;                       // gathered rows, gathered gradients, copied matrices
+    float* sums;
+    size_t bytes;
+};
+
+bool readable(const void* w, int64_t ld, int64_t step, uint32_t in, uint32_t dtype) {
+    const int64_t chunk = 16 / size_of(dtype);
+    return aligned(w, 16) && ld % chunk == 0 && step % chunk == 0 && in % chunk == 0;
+}
+
+ProductPlan product_plan(const ProductSizes& z, bool copy_w, void* workspace) {
+    ProductPlan p{};
+    p.deep = ROW_BYTES / (uint32_t)size_of(z.dtype);
+    p.ld_x = round_up(z.in, p.deep);
+    p.ld_d = round_up(z.out, p.deep);
+    const uint32_t n = z.rows(), many = std::max(1u, std::min(z.experts, n)), each = (n + many - 1) / many;
+    p.rows_tile = tile_for(z.gradient ? z.in : z.out, each, many);
+    p.dw_tile = tile_for(z.in, z.out, z.experts);
+    p.height = p.rows_tile == BIG ? Big::BQ : p.rows_tile == MID ? Mid::BQ : Few::BQ;
+    p.max_tiles = n / p.height + many + 1;
+    Carver c{static_cast<char*>(workspace)};
+    c.take(p.R.start, z.experts + 1);
+    c.take(p.R.count, z.experts + 1);
+    c.take(p.R.slot, (size_t)z.padded() + n);
+    c.take(p.R.tile, p.max_tiles);
+    c.take(p.R.tiles, 1);
+    const size_t size = size_of(z.dtype);
+    c.take(p.x, (size_t)z.padded() * p.ld_x * size);
+    if (z.gradient) {
+        c.take(p.d, (size_t)z.padded() * p.ld_d * size);
+        if (!z.by_slot && z.slots > 1) c.take(p.sums, (size_t)n * p.ld_x);
+    }
+    if (copy_w) c.take(p.w, (size_t)z.experts * z.out * p.ld_x * size);
+    p.bytes = c.used;
+    return p;
+}
+
+Spread spread(uint32_t units) {
+    Spread s{0, 1};
+    while (s.shift < 8 && (1u << s.shift) < units) ++s.shift;
+    s.across = (units + (1u << s.shift) - 1) >> s.shift;
+    return s;
+}
+
+struct KindF32 { typedef F32 E; static constexpr int OUT = OUT_F32; };
+struct KindBf16 { typedef Bf16 E; static constexpr int OUT = OUT_BF16; };
+struct KindF16 { typedef F16 E; static constexpr int OUT = OUT_F16; };
+
+template <class F>
+int with_kind(uint32_t dtype, F f) {
+    if (dtype == IWP_F32) return f(KindF32{});
+    return dtype == IWP_BF16 ? f(KindBf16{}) : f(KindF16{});
+}
+
+int arrange(const ProductSizes& z, const ProductPlan& p, const int32_t* chosen, hipStream_t s) {
+    IWP_LAUNCH_BLOCK("k_expert_arrange", k_expert_arrange, 1, ARRANGE_WAVES * 64, s, chosen, z.rows(), z.experts, p.height, p.R);
+    return IWP_OK;
+}
+
+template <int SIZE>
+int gather(const ProductSizes& z, const ProductPlan& p, const void* x, int64_t ld, uint32_t dim, bool by_slot, char* out, uint32_t ld_out, hipStream_t s) {
+    const Spread sp = spread(ld_out * SIZE / 16);
+    return in_launches(z.padded(), sp.rows() * GATHER_ROWS, sp.across, 256, [&](uint32_t first, uint32_t blocks) {
+        IWP_LAUNCH_BLOCK("k_expert_gather", k_expert_gather<SIZE>, blocks, 256, s, x, ld, dim, z.slots, by_slot, z.experts, first, sp, p.R, out, ld_out);
+        return (int)IWP_OK;
+    });
+}
+
+// The matrices where the products read them: where they lie, or copied.
+template <int SIZE>
+int matrices(const ProductSizes& z, const ProductPlan& p, const void* w, int64_t ld, int64_t step, Matrices* W, hipStream_t s) {
+    *W = Matrices{static_cast<const char*>(w), step, (uint32_t)ld, z.out, z.in};
+    if (!p.w) return IWP_OK;
+    *W = Matrices{p.w, (int64_t)z.out * p.ld_x, p.ld_x, z.out, z.in};
+    const Spread sp = spread(p.ld_x * SIZE / 16);
+    return in_launches(z.experts * z.out, sp.rows() * GATHER_ROWS, sp.across, 256, [&](uint32_t first, uint32_t blocks) {
+        IWP_LAUNCH_BLOCK("k_expert_copy", k_expert_copy<SIZE>, blocks, 256, s, w, ld, step, z.out, z.in, z.experts, first, sp, p.R, p.w, p.ld_x);
+        return (int)IWP_OK;
+    });
+}
+
+template <class K, int OUT, bool TRANSPOSED>
+int rows_product(const ProductSizes& z, const ProductPlan& p, const Matrices& W, const Packed& X, const RowsOut& Y, hipStream_t s) {
+    return with_tile(p.rows_tile, [&](auto tile) {
+        typedef decltype(tile) T;
+        auto kernel = k_expert_rows<typename K::E, T::BP, T::BQ, T::WP, T::WQ, OUT, TRANSPOSED>;
+        const uint32_t np = ((TRANSPOSED ? z.in : z.out) + T::BP - 1) / T::BP;
+        IWP_LAUNCH_BLOCK("k_expert_rows", kernel, np * p.max_tiles, T::THREADS, s, W, X, p.R, z.experts, Y);
+        return (int)IWP_OK;
+    });
+}
+
+template <class K, int OUT>
+int dw_product(const ProductSizes& z, const ProductPlan& p, const Packed& X, const Packed& D, void* dw, int64_t ld, int64_t step, hipStream_t s) {
+    return with_tile(p.dw_tile, [&](auto tile) {
+        typedef decltype(tile) T;
+        auto kernel = k_expert_dw<typename K::E, T::BP, T::BQ, T::WP, T::WQ, OUT>;
+        IWP_LAUNCH_BLOCK("k_expert_dw", kernel, (uint32_t)(z.experts * tiles_of<T>(z.in, z.out)), T::THREADS, s, X, D, p.R, static_cast<char*>(dw), ld, step);
+        return (int)IWP_OK;
+    });
+}
+
+// HIP counts a launch's threads in 32 bits.  More rows by columns than this allows fit no memory.
+bool launches_fit(const ProductSizes& z, const ProductPlan& p) {
+    return with_tile(p.rows_tile, [&](auto tile) {
+        typedef decltype(tile) T;
+        return (int)((uint64_t)(std::max(z.in, z.out) + T::BP - 1) / T::BP * p.max_tiles * T::THREADS <= MOST_THREADS);
+    }) && with_tile(p.dw_tile, [&](auto tile) {
+        typedef decltype(tile) T;
+        return (int)(z.experts * tiles_of<T>(z.in, z.out) * T::THREADS <= MOST_THREADS);
+    });
+}
+
+// What both calls check: sizes, x, w and chosen.
+int product_checks(const ProductSizes& z, uint32_t x_by_slot, const void* x, int64_t ld_x, const void* w, int64_t ld_w, int64_t step_w, const int32_t* chosen) {
+    if (!z.ok() || x_by_slot > 1 || !launches_fit(z, product_plan(z, false, nullptr))) return IWP_EINVAL;
+    if (z.tokens && (!x || !chosen)) return IWP_EINVAL;
+    if (!w || ld_x < z.in || ld_w < z.in || (z.experts > 1 && step_w < (int64_t)(z.out - 1) * ld_w + z.in)) return IWP_EINVAL;
+    return IWP_OK;
+}
+bool too_far(int64_t ld, uint32_t dtype) { return ld >= (int64_t)((1u << 24) / size_of(dtype)); }
 
 }  // namespace
 
@@ -99,6 +279,86 @@ int iwp_route_gradient(const void* x, int64_t ld_x, uint32_t tokens, uint32_t ex
             IWP_LAUNCH_AS("k_route_gradient", kernel, g.blocks, g.waves * 64, g.lds, s, r);
             return (int)IWP_OK;
         });
+    });
+}
+
+size_t iwp_expert_product_workspace_bytes(uint32_t tokens, uint32_t slots, uint32_t experts, uint32_t in, uint32_t out, uint32_t dtype, const void* w,
+                                          int64_t ld_w, int64_t step_w, uint32_t x_by_slot, uint32_t gradient) {
+    const ProductSizes z{tokens, slots, experts, in, out, dtype, x_by_slot != 0, gradient != 0};
+    if (!z.ok()) return 0;
+    const ProductPlan p = product_plan(z, !readable(w, ld_w, step_w, in, dtype), nullptr);
+    return launches_fit(z, p) ? p.bytes : 0;
+}
+
+int iwp_expert_product(const void* x, int64_t ld_x, uint32_t x_by_slot, const void* w, int64_t ld_w, int64_t step_w, uint32_t tokens, uint32_t slots,
+                       uint32_t experts, uint32_t in, uint32_t out, uint32_t dtype, const int32_t* chosen, void* y, int64_t ld_y, void* workspace,
+                       size_t workspace_bytes, void* hip_stream) {
+    const ProductSizes z{tokens, slots, experts, in, out, dtype, x_by_slot != 0, false};
+    if (int rc = product_checks(z, x_by_slot, x, ld_x, w, ld_w, step_w, chosen)) return rc;
+    if ((tokens && !y) || ld_y < out) return IWP_EINVAL;
+    if (too_far(ld_x, dtype) || too_far(ld_w, dtype) || too_far(ld_y, dtype)) return IWP_ERANGE;
+    const size_t e = size_of(dtype);
+    if (!aligned(x, e) || !aligned(w, e) || !aligned(y, e) || !aligned(chosen, 4) || !aligned(workspace, 256)) return IWP_EALIGN;
+    if (tokens == 0) return IWP_OK;
+    const ProductPlan p = product_plan(z, !readable(w, ld_w, step_w, in, dtype), workspace);
+    if (!workspace || workspace_bytes < p.bytes) return IWP_EWORKSPACE;
+    const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    return with_kind(dtype, [&](auto kind) {
+        typedef decltype(kind) K;
+        constexpr int SIZE = K::E::SIZE;
+        Matrices W;
+        int rc = arrange(z, p, chosen, s);
+        if (!rc) rc = gather<SIZE>(z, p, x, ld_x, in, z.by_slot, p.x, p.ld_x, s);
+        if (!rc) rc = matrices<SIZE>(z, p, w, ld_w, step_w, &W, s);
+        if (!rc) rc = rows_product<K, K::OUT, false>(z, p, W, Packed{p.x, p.ld_x, in}, RowsOut{static_cast<char*>(y), ld_y}, s);
+        return rc;
+    });
+}
+
+int iwp_expert_product_gradient(const void* x, int64_t ld_x, uint32_t x_by_slot, const void* w, int64_t ld_w, int64_t step_w, uint32_t tokens,
+                                uint32_t slots, uint32_t experts, uint32_t in, uint32_t out, uint32_t dtype, const int32_t* chosen, const void* dy,
+                                int64_t ld_dy, void* dx, int64_t ld_dx, void* dw, int64_t ld_dw, int64_t step_dw, uint32_t dw_dtype, void* workspace,
+                                size_t workspace_bytes, void* hip_stream) {
+    const ProductSizes z{tokens, slots, experts, in, out, dtype, x_by_slot != 0, true};
+    if (int rc = product_checks(z, x_by_slot, x, ld_x, w, ld_w, step_w, chosen)) return rc;
+    if (dw && dw_dtype != dtype && dw_dtype != IWP_F32) return IWP_EINVAL;
+    if ((tokens && !dy) || ld_dy < out || (dx && ld_dx < in)) return IWP_EINVAL;
+    if (dw && (ld_dw < in || (experts > 1 && step_dw < (int64_t)(out - 1) * ld_dw + in))) return IWP_EINVAL;
+    if (too_far(ld_x, dtype) || too_far(ld_w, dtype) || too_far(ld_dy, dtype) || (dx && too_far(ld_dx, dtype)) || (dw && too_far(ld_dw, dw_dtype)))
+        return IWP_ERANGE;
+    const size_t e = size_of(dtype);
+    if (!aligned(x, e) || !aligned(w, e) || !aligned(dy, e) || !aligned(dx, e) || !aligned(dw, size_of(dw ? dw_dtype : dtype)) || !aligned(chosen, 4) ||
+        !aligned(workspace, 256))
+        return IWP_EALIGN;
+    if ((tokens == 0 || !dx) && !dw) return IWP_OK;
+    const ProductPlan p = product_plan(z, !readable(w, ld_w, step_w, in, dtype), workspace);
+    if (!workspace || workspace_bytes < p.bytes) return IWP_EWORKSPACE;
+    const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    return with_kind(dtype, [&](auto kind) {
+        typedef decltype(kind) K;
+        constexpr int SIZE = K::E::SIZE;
+        const Packed X{p.x, p.ld_x, in}, D{p.d, p.ld_d, out};
+        int rc = arrange(z, p, chosen, s);
+        if (!rc && dw) rc = gather<SIZE>(z, p, x, ld_x, in, z.by_slot, p.x, p.ld_x, s);
+        if (!rc) rc = gather<SIZE>(z, p, dy, ld_dy, out, true, p.d, p.ld_d, s);
+        if (!rc && dx && tokens) {
+            Matrices W;
+            rc = matrices<SIZE>(z, p, w, ld_w, step_w, &W, s);
+            if (!rc && !p.sums) rc = rows_product<K, K::OUT, true>(z, p, W, D, RowsOut{static_cast<char*>(dx), ld_dx}, s);
+            if (!rc && p.sums) {
+                rc = rows_product<K, OUT_F32, true>(z, p, W, D, RowsOut{reinterpret_cast<char*>(p.sums), (int64_t)p.ld_x}, s);
+                const Spread sp = spread((in + 3) / 4);
+                if (!rc)
+                    rc = in_launches(tokens, sp.rows(), sp.across, 256, [&](uint32_t first, uint32_t blocks) {
+                        IWP_LAUNCH_BLOCK("k_expert_sum", k_expert_sum<K::OUT>, blocks, 256, s, p.sums, p.ld_x, chosen, tokens, slots, experts, in, first, sp,
+                                         dx, ld_dx);
+                        return (int)IWP_OK;
+                    });
+            }
+        }
+        if (!rc && dw)
+            rc = dw_dtype == IWP_F32 ? dw_product<K, OUT_F32>(z, p, X, D, dw, ld_dw, step_dw, s) : dw_product<K, K::OUT>(z, p, X, D, dw, ld_dw, step_dw, s);
+        return rc;
     });
 }
 

@@ -1,0 +1,315 @@
+// Kernels of the experts' products: which rows (slots of tokens) go to which expert, those rows side by side, and the products of every
+// expert's rows with its matrix, one launch for all experts.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/iwp_experts.h"
+#include "iwp_matrix.hpp"
+
+namespace iwp {
+
+constexpr uint32_t NOBODY = 0xffffffffu;
+// An expert's rows begin at a multiple of this, so that whole tiles of summed rows belong to one expert.
+constexpr uint32_t PAD_ROWS = 64;
+
+struct ExpertTile {
+    uint32_t expert, first;                // first: of the expert's rows
+};
+struct ExpertRows {        // experts' rows after each other, in the order of slots; then the slots that nobody got
+    uint32_t* start;       // [experts + 1]
+    uint32_t* count;       // [experts + 1]
+    uint32_t* slot;        // [padded rows] which slot a row is, NOBODY behind an expert's rows
+    ExpertTile* tile;      // the rows in tiles, those of nobody too
+    uint32_t* tiles;       // [1]
+};
+
+// ------------------------------------------------------------------ the rows
+
+// Which of the wavefront's lanes have the same value below 2048; those of `in` alone.
+__device__ __forceinline__ uint64_t same_lanes(uint32_t value, bool in) {
+    uint64_t same = __ballot(in);
+#pragma unroll
+    for (int bit = 0; bit < 11; ++bit) {
+        const bool one = value >> bit & 1;
+        const uint64_t ones = __ballot(one);
+        same &= one ? ones : ~ones;
+    }
+    return same;
+}
+
+// One workgroup: counts every wavefront's part of the slots by expert, where the experts' rows then begin, and puts every slot in its place.
+constexpr uint32_t ARRANGE_WAVES = 16;
+__global__ void __launch_bounds__(ARRANGE_WAVES * 64) k_expert_arrange(const int32_t* __restrict__ chosen, uint32_t n, uint32_t experts,
+                                                                       uint32_t height, ExpertRows R) {
+    __shared__ uint32_t at[ARRANGE_WAVES][IWP_MAX_EXPERTS + 1];
+    __shared__ uint32_t rows_of[ARRANGE_WAVES], tiles_of[ARRANGE_WAVES];
+    const uint32_t thread = threadIdx.x, wave = thread >> 6, lane = thread & 63;
+    const uint32_t part = (n + ARRANGE_WAVES * 64 - 1) / (ARRANGE_WAVES * 64) * 64, from = min(wave * part, n), to = min(from + part, n);
+    for (uint32_t e = lane; e <= experts; e += 64) at[wave][e] = 0;
+    lanes_exchange();
+    auto bucket = [&](uint32_t i) { return min((uint32_t)chosen[i], experts); };
+    for (uint32_t i = from + lane; i < to; i += 64) atomicAdd(&at[wave][bucket(i)], 1u);
+    __syncthreads();
+    // experts' rows and tiles: this thread's expert's, then those before it
+    uint32_t mine = 0;
+    if (thread < experts)
+        for (uint32_t w = 0; w < ARRANGE_WAVES; ++w) mine += at[w][thread];
+    const uint32_t padded = (mine + PAD_ROWS - 1) / PAD_ROWS * PAD_ROWS, tiles = (mine + height - 1) / height;
+    uint32_t rows_to = padded, tiles_to = tiles;
+    for (uint32_t o = 1; o < 64; o <<= 1) {
+        const uint32_t a = __shfl_up(rows_to, o), b = __shfl_up(tiles_to, o);
+        if (lane >= o) rows_to += a, tiles_to += b;
+    }
+    if (lane == 63) rows_of[wave] = rows_to, tiles_of[wave] = tiles_to;
+    __syncthreads();
+    uint32_t all_rows = 0, all_tiles = 0;
+    for (uint32_t w = 0; w < ARRANGE_WAVES; ++w) {
+        if (w < wave) rows_to += rows_of[w], tiles_to += tiles_of[w];
+        all_rows += rows_of[w];
+        all_tiles += tiles_of[w];
+    }
+    auto put = [&](uint32_t e, uint32_t start, uint32_t count, uint32_t first_tile) {
+        R.start[e] = start;
+        R.count[e] = count;
+        for (uint32_t t = 0; t * height < count; ++t) R.tile[first_tile + t] = ExpertTile{e, t * height};
+        for (uint32_t w = 0; w < ARRANGE_WAVES; ++w) {
+            const uint32_t c = at[w][e];
+            at[w][e] = start;
+            start += c;
+        }
+        return start;
+    };
+    if (thread < experts) {
+        const uint32_t start = rows_to - padded;
+        for (uint32_t r = put(thread, start, mine, tiles_to - tiles); r < start + padded; ++r) R.slot[r] = NOBODY;
+    }
+    if (thread == 0) {
+        uint32_t none = 0;
+        for (uint32_t w = 0; w < ARRANGE_WAVES; ++w) none += at[w][experts];
+        put(experts, all_rows, none, all_tiles);
+        *R.tiles = all_tiles + (none + height - 1) / height;
+    }
+    __syncthreads();
+    for (uint32_t base = from; base < to; base += 64) {
+        const uint32_t i = base + lane;
+        const bool in = i < to;
+        const uint32_t e = in ? bucket(i) : 0;
+        const uint64_t same = same_lanes(e, in);
+        const uint32_t rank = __popcll(same & ((1ull << lane) - 1)), first = at[wave][e];
+        lanes_exchange();
+        if (in) {
+            R.slot[first + rank] = i;
+            if (rank == 0) at[wave][e] = first + __popcll(same);
+        }
+        lanes_exchange();
+    }
+}
+
+// Rows of a caller's matrix in the experts' order, zeros behind an expert's rows and past the width.  by_slot: a row for every slot, else one
+// for every token.  16 bytes of four rows a thread.
+constexpr uint32_t GATHER_ROWS = 4;
+template <int SIZE>
+__global__ void __launch_bounds__(256) k_expert_gather(const void* __restrict__ x, int64_t ld, uint32_t dim, uint32_t slots, bool by_slot, uint32_t experts,
+                                                       uint32_t first, Spread spread, ExpertRows R, char* __restrict__ out, uint32_t ld_out) {
+    constexpr uint32_t CHUNK = 16 / SIZE;
+    const uint32_t rows = R.start[experts], c = spread.unit() * CHUNK, r0 = first + spread.row() * GATHER_ROWS;
+    if (c >= ld_out) return;
+    words4 v[GATHER_ROWS];
+#pragma unroll
+    for (uint32_t i = 0; i < GATHER_ROWS; ++i) {
+        v[i] = words4{};
+        const uint32_t slot = r0 + i < rows ? R.slot[r0 + i] : NOBODY;
+        if (slot == NOBODY) continue;
+        const char* p = static_cast<const char*>(x) + ((int64_t)(by_slot ? slot : slot / slots) * ld + c) * SIZE;
+        if (c + CHUNK <= dim) {
+            v[i] = SIZE == 4 ? *reinterpret_cast<const words4*>(p) : (words4)*reinterpret_cast<const words4_any*>(p);
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < CHUNK; ++e)
+                if (c + e < dim) {
+                    if (SIZE == 4) v[i][e % 4] = reinterpret_cast<const uint32_t*>(p)[e];
+                    else v[i][e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[e] << (e % 2 * 16);
+                }
+        }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < GATHER_ROWS; ++i)
+        if (r0 + i < rows) *reinterpret_cast<words4*>(out + ((size_t)(r0 + i) * ld_out + c) * SIZE) = v[i];
+}
+
+// Matrices whose rows cannot be read by 16 bytes where they lie, into rows of ld_out, zeros past the width; of experts that have rows.
+template <int SIZE>
+__global__ void __launch_bounds__(256) k_expert_copy(const void* __restrict__ w, int64_t ld, int64_t step, uint32_t rows, uint32_t dim, uint32_t experts,
+                                                     uint32_t first, Spread spread, ExpertRows R, char* __restrict__ out, uint32_t ld_out) {
+    constexpr uint32_t CHUNK = 16 / SIZE;
+    const uint32_t c = spread.unit() * CHUNK, r0 = first + spread.row() * GATHER_ROWS;
+    if (c >= ld_out) return;
+    words4 v[GATHER_ROWS];
+    bool there[GATHER_ROWS];
+#pragma unroll
+    for (uint32_t i = 0; i < GATHER_ROWS; ++i) {
+        const uint32_t e = (r0 + i) / rows, row = (r0 + i) % rows;
+        v[i] = words4{};
+        there[i] = e < experts && R.count[e];
+        if (!there[i]) continue;
+        const char* p = static_cast<const char*>(w) + (e * step + row * ld + c) * SIZE;
+        if (c + CHUNK <= dim) {
+            v[i] = SIZE == 4 ? *reinterpret_cast<const words4*>(p) : (words4)*reinterpret_cast<const words4_any*>(p);
+        } else {
+#pragma unroll
+            for (uint32_t k = 0; k < CHUNK; ++k)
+                if (c + k < dim) {
+                    if (SIZE == 4) v[i][k % 4] = reinterpret_cast<const uint32_t*>(p)[k];
+                    else v[i][k / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[k] << (k % 2 * 16);
+                }
+        }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < GATHER_ROWS; ++i)
+        if (there[i]) *reinterpret_cast<words4*>(out + ((size_t)(r0 + i) * ld_out + c) * SIZE) = v[i];
+}
+
+// ------------------------------------------------------------------ the products
+
+struct Matrices {          // one for every expert
+    const char* w;
+    int64_t step;          // elements from one to the next
+    uint32_t ld, rows, columns;
+};
+struct Packed {            // gathered rows
+    const char* x;
+    uint32_t ld, dim;
+};
+struct RowsOut {
+    char* y;
+    int64_t ld;            // elements
+};
+
+// Where block `block` of n stands in the work's order: every die has a stretch of it.
+__device__ __forceinline__ uint32_t stretch_place(uint32_t block, uint32_t n) {
+    const uint32_t per = n / 8, more = n % 8, die = block % 8;
+    return die * per + min(die, more) + block / 8;
+}
+
+// A wavefront's part of a tile to memory: row(q) is where the row of entry q begins, or null.
+template <class M, int OUT, int BP, int WP, class F>
+__device__ __forceinline__ void store_tile(const M& mm, char* lds, uint32_t p0, uint32_t columns, F row_of) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    typedef Rows32<OUT == OUT_F32 ? 4 : 2, BP / WP> Out;
+    static_assert(M::WAVES * Out::BYTES <= M::LDS, "a wavefront's rows");
+    char* mine = lds + wave * Out::BYTES;
+    constexpr uint32_t SIZE = OUT == OUT_F32 ? 4 : 2;
+    const uint32_t pw = p0 + M::p_of(wave), qw = M::q_of(wave);
+#pragma unroll
+    for (int b = 0; b < M::FQ; ++b) {
+#pragma unroll
+        for (int a = 0; a < M::FP; ++a)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                f32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = mm.acc[a][b][c * 4 + e];
+                uint64_t four = 0;
+                if (OUT != OUT_F32)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) four |= (uint64_t)(OUT == OUT_BF16 ? Bf16::bits(v[e]) : F16::bits(v[e])) << (16 * e);
+                Out::put(mine, a * 32 + p_in_fragment(c * 4, lane), lane, OUT == OUT_F32 ? (const void*)&v : (const void*)&four);
+            }
+        Out::each(mine, lane, [&](uint32_t row, uint32_t p, quad v) {
+            if (pw + p >= columns) return;
+            char* to = row_of(qw + b * 32 + row);
+            if (!to) return;
+            to += (size_t)(pw + p) * SIZE;
+            if (pw + p + Out::PER_CHUNK <= columns) {
+                *reinterpret_cast<words4_any*>(to) = words4_any{v.x, v.y, v.z, v.w};
+            } else {
+                const uint32_t word[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < Out::PER_CHUNK; ++e)
+                    if (pw + p + e < columns) {
+                        if (OUT == OUT_F32) reinterpret_cast<uint32_t*>(to)[e] = word[e];
+                        else reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(word[e / 2] >> (16 * (e & 1)));
+                    }
+            }
+        });
+    }
+}
+
+// Every expert's rows times its matrix (TRANSPOSED: W, not W^T, as for the rows' gradient), to the slots' rows of the output; zeros for
+// slots of nobody.
+template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool TRANSPOSED>
+__global__ void __launch_bounds__(WP * WQ * 64) k_expert_rows(Matrices W, Packed X, ExpertRows R, uint32_t experts, RowsOut Y) {
+    typedef Product<E, BP, BQ, WP, WQ, TRANSPOSED, false> M;
+    __shared__ __align__(1024) char lds[M::LDS];
+    const uint32_t columns = TRANSPOSED ? W.columns : W.rows, np = (columns + BP - 1) / BP, nq = *R.tiles;
+    if (blockIdx.x >= np * nq) return;
+    const uint32_t at = stretch_place(blockIdx.x, np * nq);
+    constexpr uint32_t TALL = 8;
+    const uint32_t group = at / (np * TALL), rest = at - group * np * TALL, tall = min(TALL, nq - group * TALL);
+    const uint32_t tp = rest / tall;
+    const ExpertTile tile = R.tile[group * TALL + rest % tall];
+    const uint32_t count = R.count[tile.expert], start = R.start[tile.expert];
+    M mm;
+    if (tile.expert < experts) {
+        const uint32_t summed = TRANSPOSED ? W.rows : W.columns;
+        const Operand P{reinterpret_cast<const uint16_t*>(W.w + tile.expert * W.step * E::SIZE), nullptr, W.ld, columns, summed};
+        const Operand Q{reinterpret_cast<const uint16_t*>(X.x + (size_t)start * X.ld * E::SIZE), nullptr, X.ld, count, X.ld};
+        mm.run(P, Q, tp * BP, tile.first, 0, (summed + M::DEEP - 1) / M::DEEP * M::DEEP, lds);
+    } else {
+#pragma unroll
+        for (int a = 0; a < M::FP; ++a)
+#pragma unroll
+            for (int b = 0; b < M::FQ; ++b) mm.acc[a][b] = f32x16{};
+    }
+    constexpr uint32_t SIZE = OUT == OUT_F32 ? 4 : 2;
+    store_tile<M, OUT, BP, WP>(mm, lds, tp * BP, columns, [&](uint32_t q) -> char* {
+        if (tile.first + q >= count) return nullptr;
+        return Y.y + (int64_t)R.slot[start + tile.first + q] * Y.ld * SIZE;
+    });
+}
+
+// Every expert's matrix's gradient: the sum over its rows of dy x^T.
+template <class E, int BP, int BQ, int WP, int WQ, int OUT>
+__global__ void __launch_bounds__(WP * WQ * 64) k_expert_dw(Packed X, Packed D, ExpertRows R, char* __restrict__ dw, int64_t ld, int64_t step) {
+    typedef Product<E, BP, BQ, WP, WQ, true, true> M;
+    __shared__ __align__(1024) char lds[M::LDS];
+    const uint32_t np = (X.dim + BP - 1) / BP, nq = (D.dim + BQ - 1) / BQ;
+    const uint32_t at = stretch_place(blockIdx.x, gridDim.x), expert = at / (np * nq), of = at - expert * np * nq;
+    constexpr uint32_t TALL = 8;
+    const uint32_t group = of / (np * TALL), rest = of - group * np * TALL, tall = min(TALL, nq - group * TALL);
+    const uint32_t tp = rest / tall, tq = group * TALL + rest % tall;
+    const uint32_t rows = (R.count[expert] + PAD_ROWS - 1) / PAD_ROWS * PAD_ROWS, start = R.start[expert];
+    const Operand P{reinterpret_cast<const uint16_t*>(X.x + (size_t)start * X.ld * E::SIZE), nullptr, X.ld, X.dim, rows};
+    const Operand Q{reinterpret_cast<const uint16_t*>(D.x + (size_t)start * D.ld * E::SIZE), nullptr, D.ld, D.dim, rows};
+    M mm;
+    mm.run(P, Q, tp * BP, tq * BQ, 0, rows, lds);
+    constexpr uint32_t SIZE = OUT == OUT_F32 ? 4 : 2;
+    char* mine = dw + (expert * step + (int64_t)tq * BQ * ld) * SIZE;
+    store_tile<M, OUT, BP, WP>(mm, lds, tp * BP, X.dim, [&](uint32_t q) -> char* { return tq * BQ + q < D.dim ? mine + (int64_t)q * ld * SIZE : nullptr; });
+}
+
+// A token's gradient: the sum over its slots' rows, in their order.  Four entries a thread.
+template <int OUT>
+__global__ void __launch_bounds__(256) k_expert_sum(const float* __restrict__ rows, uint32_t ld, const int32_t* __restrict__ chosen, uint32_t tokens,
+                                                    uint32_t slots, uint32_t experts, uint32_t dim, uint32_t first, Spread spread, void* __restrict__ dx,
+                                                    int64_t ld_dx) {
+    const uint32_t token = first + spread.row(), c = spread.unit() * 4;
+    if (token >= tokens || c >= dim) return;
+    f32x4 sum = {};
+    for (uint32_t k = 0; k < slots; ++k) {
+        const size_t slot = (size_t)token * slots + k;
+        if ((uint32_t)chosen[slot] < experts) sum += *reinterpret_cast<const f32x4*>(rows + slot * ld + c);
+    }
+    const int64_t to = token * ld_dx + c;
+    if (c + 4 <= dim && OUT == OUT_F32) {
+        *reinterpret_cast<words4*>(static_cast<float*>(dx) + to) = __builtin_bit_cast(words4, sum);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < dim) iwp::put<OUT>(dx, to + e, sum[e]);
+    }
+}
+
+}  // namespace iwp

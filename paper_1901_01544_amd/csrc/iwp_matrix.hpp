@@ -1,7 +1,7 @@
-// Matrix products on 16-bit operands (bf16, fp16) with binary32 sums, tiled for gfx950's matrix cores.  One tile loop for
-// every product of the head kernels; what differs is which way an operand lies in memory:
+// Matrix products on 16-bit operands (bf16, fp16) or binary32 ones with binary32 sums, tiled for gfx950's matrix cores.  One tile loop
+// for every product of the head's and the experts' kernels; what differs is which way an operand lies in memory:
 //   rows of K     the summed index is contiguous; a lane's fragment is one 128-bit LDS read
-//   columns of K  the other index is contiguous; a lane's fragment is two transposing 64-bit LDS reads
+//   columns of K  the other index is contiguous; a lane's fragment is two transposing 64-bit LDS reads (of binary32: four reads)
 // The tile of P is the matrix instruction's first operand, that of Q its second, so a lane ends up with four consecutive
 // entries of P for one entry of Q: P is the index that is contiguous in the product, Q its row.
 //
@@ -46,6 +46,7 @@ __device__ __forceinline__ void lanes_exchange() {
 }
 
 struct Bf16 {
+    static constexpr int SIZE = 2;
     static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
@@ -53,11 +54,24 @@ struct Bf16 {
     static __device__ __forceinline__ float value(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
 };
 struct F16 {
+    static constexpr int SIZE = 2;
     static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
     }
     static __device__ __forceinline__ uint16_t bits(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
     static __device__ __forceinline__ float value(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }
+};
+
+// Binary32 operands as they are: a fragment's 16 bytes are four summed entries, which take four matrix instructions of two (one of each
+// half of the wavefront).  157 TFLOP/s at most, a sixteenth of bf16's.
+struct F32 {
+    static constexpr int SIZE = 4;
+    static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[k], y[k], c, 0, 0, 0);
+        return c;
+    }
 };
 
 enum OutType { OUT_F32, OUT_BF16, OUT_F16 };
@@ -86,14 +100,15 @@ struct Spread {
     __device__ __forceinline__ uint32_t unit() const { return (blockIdx.x % across << shift) + (threadIdx.x & ((1u << shift) - 1)); }
 };
 
-constexpr uint32_t BK = 64;                        // summed entries per LDS tile: 128 bytes of a row
+constexpr uint32_t BK = 64;                        // summed entries of 16 bits per LDS tile: 128 bytes of a row
+constexpr uint32_t ROW_BYTES = 128;
 
 // An operand as the tile loop reads it.  Binary32 operands come as two planes of fp16 (see split_f32): `lo` is null for
 // operands of 16 bits.
 struct Operand {
     const uint16_t* hi;
     const uint16_t* lo;
-    uint32_t ld;           // elements from row to row; ld * 512 bytes stay below 2^32
+    uint32_t ld;           // elements from row to row; 256 rows stay below 2^32 bytes
     uint32_t extent;       // valid entries of the index that is not summed
     uint32_t summed;       // valid entries of the summed one
 };
@@ -117,7 +132,7 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
 }
 
-// One operand's tile: R entries of its own index, BK of the summed one, WAVES wavefronts loading.
+// One operand's tile: R entries of its own index, 128 bytes of the summed one, WAVES wavefronts loading elements of SIZE bytes.
 //
 // Rows of K: LDS row r holds the 8 chunks (16 bytes) of entry r, chunk c at place c ^ turn(r).
 // Columns of K: LDS row k holds R entries, in pairs of chunks of 64 bytes, pair p at place p ^ turn.
@@ -127,13 +142,13 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 // Entries past the operand's extent are read from a valid one: what they contribute to is never stored.  Summed entries past
 // an operand's end are read from the same row, or from its last row; of the two operands one always reaches to a multiple of BK
 // and holds zeros there.
-template <int R, int WAVES, bool COLUMNS>
+template <int R, int WAVES, bool COLUMNS, int SIZE = 2>
 struct Tile {
-    static constexpr int BYTES = R * BK * 2;
+    static constexpr int BYTES = R * ROW_BYTES, CHUNK = 16 / SIZE;
     static constexpr int LOADS = BYTES / 1024 / WAVES;      // 64 lanes of 16 bytes each
     static_assert(LOADS * WAVES * 1024 == BYTES, "whole loads");
-    static constexpr int PER_ROW = COLUMNS ? R / 8 : BK / 8;
-    static constexpr int TURNS = COLUMNS ? (R / 32 < 8 ? R / 32 : 8) : 8;
+    static constexpr int PER_ROW = COLUMNS ? R / CHUNK : ROW_BYTES / 16;
+    static constexpr int TURNS = !COLUMNS ? 8 : SIZE == 4 ? 1 : R / 32 < 8 ? R / 32 : 8;
 
     uint32_t at[LOADS];        // byte offset of this lane's chunk from the tile's origin
     uint32_t within[LOADS];    // its (first) summed index in the tile
@@ -144,36 +159,44 @@ struct Tile {
         return ((r & 3u) | ((r >> 1) & 4u)) & (TURNS - 1);
     }
     __device__ __forceinline__ void init(const Operand& o, uint32_t first, int wave, int lane) {
-        row_bytes = o.ld * 2;
+        row_bytes = o.ld * SIZE;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const uint32_t slot = (wave * LOADS + i) * 64 + lane, row = slot / PER_ROW, place = slot % PER_ROW;
             if (!COLUMNS) {
                 const uint32_t entry = min(first + row, o.extent - 1) - first, chunk = place ^ turn(row);
-                within[i] = chunk * 8;
+                within[i] = chunk * CHUNK;
                 at[i] = entry * row_bytes + chunk * 16;
             } else {
                 const uint32_t chunk = (((place >> 2) ^ turn(row)) << 2) | (place & 3u);
-                const uint32_t entry = first + chunk * 8 < o.extent ? chunk * 8 : 0u;
+                const uint32_t entry = first + chunk * CHUNK < o.extent ? chunk * CHUNK : 0u;
                 within[i] = row;
-                at[i] = entry * 2 + row * row_bytes;
+                at[i] = entry * SIZE + row * row_bytes;
             }
         }
     }
     // plane + first entry, as bytes: where the tile's entry 0 at summed index k lies
     static __device__ __forceinline__ const char* origin(const uint16_t* plane, const Operand& o, uint32_t first, uint32_t k) {
-        return reinterpret_cast<const char*>(plane) + (COLUMNS ? ((size_t)k * o.ld + first) * 2 : ((size_t)first * o.ld + k) * 2);
+        return reinterpret_cast<const char*>(plane) + (COLUMNS ? ((size_t)k * o.ld + first) * SIZE : ((size_t)first * o.ld + k) * SIZE);
     }
     // The i-th load; left: summed entries from the tile's first on (at least 1)
     __device__ __forceinline__ void load(int i, const char* from, uint32_t left, uint32_t lds, int wave) const {
-        const uint32_t inside = COLUMNS ? at[i] - (within[i] - (left - 1)) * row_bytes : at[i] - within[i] * 2;
+        const uint32_t inside = COLUMNS ? at[i] - (within[i] - (left - 1)) * row_bytes : at[i] - within[i] * SIZE;
         load_to_lds(from, within[i] < left ? at[i] : inside, lds + (wave * LOADS + i) * 1024);
     }
-    // Fragment of the 32 entries from `entry` (a multiple of 32) on, summed indices 16 s to 16 s + 15 of the tile.
+    // Fragment of the 32 entries from `entry` (a multiple of 32) on, bytes 32 s to 32 s + 31 of the summed index: of each half of the
+    // wavefront, 16.
     static __device__ __forceinline__ s16x8 fragment(const char* lds, uint32_t entry, int s, int lane) {
         if (!COLUMNS) {
             const uint32_t row = entry + (lane & 31), chunk = 2 * s + (lane >> 5);
-            return *reinterpret_cast<const s16x8*>(lds + row * (BK * 2) + ((chunk ^ turn(row)) << 4));
+            return *reinterpret_cast<const s16x8*>(lds + row * ROW_BYTES + ((chunk ^ turn(row)) << 4));
+        }
+        if (SIZE == 4) {
+            f32x4 x;
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k)
+                x[k] = *reinterpret_cast<const f32_bytes*>(lds + (8 * s + 4 * (lane >> 5) + k) * (R * 4) + (entry + (lane & 31)) * 4);
+            return __builtin_bit_cast(s16x8, x);
         }
         const uint32_t i = lane & 15, half = lane >> 5;
         const uint32_t k = 16 * s + 8 * half + (i >> 2);
@@ -198,8 +221,9 @@ template <class E, int BP, int BQ, int WP, int WQ, bool P_COLUMNS, bool Q_COLUMN
 struct Product {
     static constexpr int WAVES = WP * WQ;
     static constexpr int FP = BP / WP / 32, FQ = BQ / WQ / 32;     // fragments of 32 per wavefront
-    typedef Tile<BP, WAVES, P_COLUMNS> TP;
-    typedef Tile<BQ, WAVES, Q_COLUMNS> TQ;
+    typedef Tile<BP, WAVES, P_COLUMNS, E::SIZE> TP;
+    typedef Tile<BQ, WAVES, Q_COLUMNS, E::SIZE> TQ;
+    static constexpr uint32_t DEEP = ROW_BYTES / E::SIZE;          // summed entries of a tile
     static constexpr int STAGE = TP::BYTES + TQ::BYTES, LDS = 2 * STAGE;
 
     f32x16 acc[FP][FQ];
@@ -208,7 +232,7 @@ struct Product {
     static __device__ __forceinline__ uint32_t p_of(int wave) { return (wave % WP) * (BP / WP); }
     static __device__ __forceinline__ uint32_t q_of(int wave) { return (wave / WP) * (BQ / WQ); }
 
-    // Sum over summed indices [k_from, k_to), a multiple of BK, of P[p0 ..][k] Q[q0 ..][k].  Operands of two planes x = hi + 2^-11 lo (scaled, see
+    // Sum over summed indices [k_from, k_to), a multiple of DEEP, of P[p0 ..][k] Q[q0 ..][k].  Operands of two planes x = hi + 2^-11 lo (scaled, see
     // split_f32) take three passes, lo hi + hi lo first, then times 2^-11, then hi hi; lo lo lies below binary32.
     __device__ __forceinline__ void run(const Operand& P, const Operand& Q, uint32_t p0, uint32_t q0, uint32_t k_from,
                                         uint32_t k_to, char* lds) {
@@ -222,20 +246,20 @@ struct Product {
         TQ tq;
         tp.init(P, p0, wave, lane);
         tq.init(Q, q0, wave, lane);
-        const uint32_t steps = (k_to - k_from) / BK, passes = P.lo ? 3 : 1, total = steps * passes;
+        const uint32_t steps = (k_to - k_from) / DEEP, passes = P.lo ? 3 : 1, total = steps * passes;
         const uint32_t pw = p_of(wave), qw = q_of(wave);
-        const size_t p_step = (P_COLUMNS ? (size_t)P.ld * BK : BK) * 2, q_step = (Q_COLUMNS ? (size_t)Q.ld * BK : BK) * 2;
+        const size_t p_step = (P_COLUMNS ? (size_t)P.ld * DEEP : DEEP) * E::SIZE, q_step = (Q_COLUMNS ? (size_t)Q.ld * DEEP : DEEP) * E::SIZE;
         const char *pf = nullptr, *qf = nullptr;
         uint32_t step = 0, pass = 0;                                   // of the next tile to be loaded
         const uint32_t lds_at = lds_address(lds);
-        constexpr int LOADS = TP::LOADS + TQ::LOADS, STEPS = BK / 16, PRODUCTS = FP * FQ;
+        constexpr int LOADS = TP::LOADS + TQ::LOADS, STEPS = ROW_BYTES / 32, PRODUCTS = FP * FQ;
         // load i of the tile `step` of `pass`, into a stage; advance() goes on to the next tile
         auto origin = [&]() {
             pf = TP::origin(passes == 3 && pass == 0 ? P.lo : P.hi, P, p0, k_from);
             qf = TQ::origin(passes == 3 && pass == 1 ? Q.lo : Q.hi, Q, q0, k_from);
         };
         auto load = [&](int i, uint32_t stage) {
-            const uint32_t k = k_from + step * BK, to = lds_at + stage * STAGE;
+            const uint32_t k = k_from + step * DEEP, to = lds_at + stage * STAGE;
             if (i < TP::LOADS) tp.load(i, pf, P.summed - k, to, wave);
             else tq.load(i - TP::LOADS, qf, Q.summed - k, to + TP::BYTES, wave);
         };

@@ -114,6 +114,8 @@ def load() -> C.CDLL:
     L.iwp_head_workspace_bytes.restype = C.c_size_t
     L.iwp_balance_workspace_bytes.argtypes = [C.c_uint32, C.c_uint32]
     L.iwp_balance_workspace_bytes.restype = C.c_size_t
+    L.iwp_expert_product_workspace_bytes.argtypes = [C.c_uint32] * 6 + [_vp, C.c_int64, C.c_int64, C.c_uint32, C.c_uint32]
+    L.iwp_expert_product_workspace_bytes.restype = C.c_size_t
     L.iwp_tensors_create.argtypes = [C.POINTER(Layer), C.c_uint32, C.POINTER(_vp)]
     L.iwp_tensors_create.restype = C.c_int
     L.iwp_tensors_destroy.argtypes = [_vp]

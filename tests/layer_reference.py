@@ -87,3 +87,47 @@ class RouteGradient:
 
     def check(self, dx):
         near("dx", dx, self.dx, self.off)
+
+
+class Experts:
+    """y and the gradients of products with every expert's matrix, row by row of the slots."""
+
+    def __init__(self, x, w, chosen, dy=None):
+        T, K = chosen.shape
+        E, F, D = w.shape
+        by_slot = x.dim() == 3
+        X = (x if by_slot else x[:, None].expand(T, K, D)).reshape(T * K, D).double()
+        c = chosen.reshape(-1).long()
+        self.nobody = ((c < 0) | (c >= E)).view(T, K)
+        zeros = lambda *shape: torch.zeros(*shape, dtype=torch.float64, device=x.device)  # noqa: E731
+        y, y_off = zeros(T * K, F), zeros(T * K, F)
+        dx, dx_off, self.dw, self.dw_off = zeros(T * K, D), zeros(T * K, D), zeros(E, F, D), zeros(E, F, D)
+        d = None if dy is None else dy.reshape(T * K, F).double()
+        for e in range(E):
+            rows = (c == e).nonzero().squeeze(1)
+            if not rows.numel():
+                continue
+            W = w[e].double()
+            y[rows] = X[rows] @ W.t()
+            y_off[rows] = 2.0 ** -20 * (X[rows].abs() @ W.abs().t())           # sums in binary32
+            if d is not None:
+                dx[rows] = d[rows] @ W
+                dx_off[rows] = 2.0 ** -20 * (d[rows].abs() @ W.abs())
+                self.dw[e] = d[rows].t() @ X[rows]
+                self.dw_off[e] = 2.0 ** -20 * (d[rows].abs().t() @ X[rows].abs())
+        self.y, self.y_off = y.view(T, K, F), y_off.view(T, K, F)
+        dx, dx_off = dx.view(T, K, D), dx_off.view(T, K, D)
+        if not by_slot:
+            dx_off = dx_off.sum(1) + 2.0 ** -23 * K * dx.abs().sum(1)
+            dx = dx.sum(1)
+        self.dx, self.dx_off = dx, dx_off
+
+    def check(self, y):
+        near("y", y, self.y, self.y_off)
+        assert (y[self.nobody] == 0).all()
+
+    def check_gradient(self, dx, dw):
+        if dx is not None:
+            near("dx", dx, self.dx, self.dx_off)
+        if dw is not None:
+            near("dw", dw, self.dw, self.dw_off)
