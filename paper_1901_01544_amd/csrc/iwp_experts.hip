@@ -34,18 +34,19 @@ int with_type(uint32_t dtype, F f) {
 }
 
 constexpr uint32_t LDS_OF_A_LAUNCH = 65536;
-constexpr uint32_t ROUTE_GROUPS = 4096;
 
 // Launches over tokens: wavefronts of a workgroup (as many of four as LDS has room for) and workgroups.
 struct TokenGrid {
     uint32_t waves = 4, lds, blocks;
-    TokenGrid(uint32_t tokens, uint32_t lanes, uint32_t bytes_per_token) {
-        const uint32_t at_once = 64 / lanes;
-        while (waves > 1 && waves * at_once * bytes_per_token > LDS_OF_A_LAUNCH) waves /= 2;
-        lds = waves * at_once * bytes_per_token;
-        blocks = std::min((tokens + waves * at_once - 1) / (waves * at_once), ROUTE_GROUPS);
+    TokenGrid(uint32_t tokens, uint32_t at_once, uint32_t bytes_per_wave) {
+        while (waves > 1 && waves * bytes_per_wave > LDS_OF_A_LAUNCH) waves /= 2;
+        lds = waves * bytes_per_wave;
+        blocks = (tokens + waves * at_once - 1) / (waves * at_once);
     }
 };
+
+template <class T>
+T round_up(T x, T to) { return (x + to - 1) / to * to; }
 
 // ------------------------------------------------------------------ the products
 
@@ -82,9 +83,6 @@ struct Carver {            // hands out 256-byte aligned parts; at == nullptr: o
         used += (n * sizeof(T) + 255) & ~size_t(255);
     }
 };
-
-template <class T>
-T round_up(T x, T to) { return (x + to - 1) / to * to; }
 
 struct ProductSizes {
     uint32_t tokens, slots, experts, in, out, dtype;
@@ -247,13 +245,21 @@ int iwp_route(const void* x, int64_t ld_x, uint32_t tokens, uint32_t experts, ui
             constexpr int IN = decltype(in)::value, CHUNKS = decltype(chunks)::value;
             const RouteCall r{x, ld_x, tokens, experts, lanes, slots, bias, scores == IWP_SIGMOID, renormalise != 0, groups, top_groups, group_top,
                               scale, keep, chosen, weight};
-            const TokenGrid g(tokens, lanes, (uint32_t)(slots * sizeof(Slot) + (grouped ? (experts + groups) * (by_score ? 8 : 4) : 0)));
+            const uint32_t at_once = 64 / lanes, row = experts + groups;
+            const uint32_t lds = round_up<uint32_t>(std::max({lanes >= 16 ? at_once * CANDIDATES * (uint32_t)sizeof(Candidate) : 0u, by_score ? row * 8 : 0u,
+                                                              grouped ? at_once * row * 4 : 0u}), 16);
+            const TokenGrid g(tokens, at_once, lds + at_once * slots * 4);
             auto launch = [&](auto kernel) {
-                IWP_LAUNCH_AS("k_route", kernel, g.blocks, g.waves * 64, g.lds, s, r);
+                IWP_LAUNCH_AS("k_route", kernel, g.blocks, g.waves * 64, g.lds, s, r, lds);
                 return (int)IWP_OK;
             };
-            if (by_score) return grouped ? launch(k_route<IN, CHUNKS, double, true>) : launch(k_route<IN, CHUNKS, double, false>);
-            return grouped ? launch(k_route<IN, CHUNKS, float, true>) : launch(k_route<IN, CHUNKS, float, false>);
+            auto of_lanes = [&](auto known) {
+                constexpr int LANES = decltype(known)::value;
+                if (by_score) return grouped ? launch(k_route<IN, CHUNKS, LANES, true, true>) : launch(k_route<IN, CHUNKS, LANES, true, false>);
+                return grouped ? launch(k_route<IN, CHUNKS, LANES, false, true>) : launch(k_route<IN, CHUNKS, LANES, false, false>);
+            };
+            if (CHUNKS == 2 || lanes == 16) return of_lanes(std::integral_constant<int, 16>{});
+            return of_lanes(std::integral_constant<int, CHUNKS == 2 ? 16 : 0>{});
         });
     });
 }
@@ -274,7 +280,8 @@ int iwp_route_gradient(const void* x, int64_t ld_x, uint32_t tokens, uint32_t ex
             constexpr int IN = decltype(in)::value, CHUNKS = decltype(chunks)::value;
             const RouteGradient r{x, ld_x, tokens, experts, lanes, slots, chosen, dweight, scores == IWP_SIGMOID, renormalise != 0, scale, keep,
                                   plus, ld_plus, dx, ld_dx};
-            const TokenGrid g(tokens, lanes, (uint32_t)(slots * sizeof(SlotGradient)));
+            const uint32_t at_once = 64 / lanes;
+            const TokenGrid g(tokens, at_once, at_once * (uint32_t)(slots * sizeof(SlotGradient) + (experts + 7) / 8 * 8 * sizeof(float)));
             auto kernel = k_route_gradient<IN, CHUNKS>;
             IWP_LAUNCH_AS("k_route_gradient", kernel, g.blocks, g.waves * 64, g.lds, s, r);
             return (int)IWP_OK;

@@ -1,8 +1,10 @@
 // Kernels of the choice of experts and of its gradient.  A token's experts lie over a part of a wavefront as in the expert balance
 // (TokenLanes), so the logits are read once, and everything about a token happens between its lanes:
-//   c = score + bias in binary64, or the logits themselves where their order is the scores' order (no bias, no sums over groups);
-//   groups: best one or two c of every group by way of LDS, a group's rank by counting;
-//   then slot after slot the largest c that is left, found by every lane among its own and between lanes in log2(lanes) steps.
+//   c = score + bias, or the logits themselves where their order is the scores' order (no bias, no sums over groups);
+//   groups: best one or two c of every group between the lanes that have it, a group's rank by counting;
+//   slots: the largest c that is left, one after the other, or where there are many lanes all at once (see candidates).
+// Scores decide in binary64, but are computed in binary32 first: where no two c that the choice depends on are closer than twice what
+// binary32 may be off, it is the choice.  Else the wavefront does the token again in binary64, value by value in LDS.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -29,153 +31,415 @@ struct RouteCall {
 // e^(min(x, 0) - m) / (1 + e^-|x|) for m >= min(x, 0): a sigmoid over e^m, which does not vanish where all a token's sigmoids are small.
 __device__ __forceinline__ float sigmoid_over(float x, float m) { return expf(fminf(x, 0.0f) - m) / (1.0f + expf(-fabsf(x))); }
 
-// A part of a wavefront that has one token.
-struct Part {
+template <int IN>
+__device__ __forceinline__ float element(const void* x, int64_t at) {
+    if (IN == OUT_F32) return static_cast<const float*>(x)[at];
+    const uint16_t b = static_cast<const uint16_t*>(x)[at];
+    return IN == OUT_BF16 ? Bf16::value(b) : F16::value(b);
+}
+
+// A part of a wavefront that has one token: `lanes`, a power of two.  LANES: that number where it is known to the compiler, else 0.
+template <int LANES>
+struct PartOf {
     uint32_t lanes;
+    __device__ __forceinline__ PartOf(uint32_t lanes) : lanes(LANES ? LANES : lanes) {}
+    template <int CONTROL, class T>
+    static __device__ __forceinline__ T moved(T v) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CONTROL, 0xf, 0xf, true));
+    }
+    // f over all lanes, in every lane: neighbours, pairs, quads (mirrored, whose lanes hold the same by then), rows of 16
     template <class F, class T>
     __device__ __forceinline__ T reduce(T v, F f) const {
-        for (uint32_t o = lanes / 2; o; o >>= 1) v = f(v, __shfl_xor(v, o));
+        if (lanes > 1) v = f(v, moved<0xb1>(v));                                    // quad_perm 1 0 3 2
+        if (lanes > 2) v = f(v, moved<0x4e>(v));                                    // quad_perm 2 3 0 1
+        if (lanes > 4) v = f(v, moved<0x141>(v));                                   // row_half_mirror
+        if (lanes > 8) v = f(v, moved<0x140>(v));                                   // row_mirror
+        if (lanes > 16) v = f(v, (T)__shfl_xor(v, 16));
+        if (lanes > 32) v = f(v, (T)__shfl_xor(v, 32));
         return v;
     }
     __device__ __forceinline__ float sum(float v) const { return reduce(v, [](float a, float b) { return a + b; }); }
-    __device__ __forceinline__ double sum(double v) const { return reduce(v, [](double a, double b) { return a + b; }); }
     __device__ __forceinline__ float max(float v) const { return reduce(v, [](float a, float b) { return fmaxf(a, b); }); }
+    __device__ __forceinline__ uint32_t min(uint32_t v) const { return reduce(v, [](uint32_t a, uint32_t b) { return a < b ? a : b; }); }
     __device__ __forceinline__ bool any(bool v) const { return reduce((int)v, [](int a, int b) { return a | b; }) != 0; }
+    __device__ __forceinline__ double sum(double v) const {
+        for (uint32_t o = lanes / 2; o; o >>= 1) v += __shfl_xor(v, o);
+        return v;
+    }
 };
+typedef PartOf<0> Part;
 
-struct Slot {              // what a slot got, in LDS until the token's weights are known
-    int32_t expert;
-    float x;
-};
+// The best two of two such pairs.
+template <class C>
+__device__ __forceinline__ void best_two(C& first, C& second, C a, C b) {
+    const C low = first < a ? first : a;
+    first = first < a ? a : first;
+    second = second < b ? b : second;
+    second = second < low ? low : second;
+}
 
-// C: the type of c, float where the logits themselves are compared, else double.
-template <int IN, int CHUNKS, class C, bool GROUPS>
-__global__ void __launch_bounds__(256) k_route(RouteCall r) {
-    typedef TokenLanes<IN, CHUNKS> L;
-    constexpr bool BY_SCORE = sizeof(C) == 8;
+template <>
+__device__ __forceinline__ void best_two<float>(float& first, float& second, float a, float b) {
+    second = fmaxf(fmaxf(second, b), fminf(first, a));
+    first = fmaxf(first, a);
+}
+// The best two of `lanes` lanes' two.
+__device__ __forceinline__ void best_two_of(uint32_t lanes, float& first, float& second) {
+    if (lanes > 1) best_two(first, second, Part::moved<0xb1>(first), Part::moved<0xb1>(second));
+    if (lanes > 2) best_two(first, second, Part::moved<0x4e>(first), Part::moved<0x4e>(second));
+    if (lanes > 4) best_two(first, second, Part::moved<0x141>(first), Part::moved<0x141>(second));
+    if (lanes > 8) best_two(first, second, Part::moved<0x140>(first), Part::moved<0x140>(second));
+    if (lanes > 16) best_two(first, second, __shfl_xor(first, 16), __shfl_xor(second, 16));
+    if (lanes > 32) best_two(first, second, __shfl_xor(first, 32), __shfl_xor(second, 32));
+}
+
+// Groups of any size, by way of LDS (row: the token's c by expert, then the groups' values): what is not in one of the top groups becomes
+// NONE in `row`.  *least, *next: the values of the last group that is in and of the first that is not.
+template <class C, class P>
+__device__ __forceinline__ void choose_groups(const RouteCall& r, const P& part, uint32_t lane, C* row, C* least, C* next) {
     constexpr C NONE = -(C)INFINITY;
-    extern __shared__ __align__(16) char shared[];
-    const L l(r.experts, r.lanes);
-    const Part part{r.lanes};
-    const uint32_t wave = threadIdx.x >> 6, at_once = l.tokens(), tokens = (blockDim.x >> 6) * at_once;      // of the workgroup at a time
-    const uint32_t mine = wave * at_once + l.of;
-    Slot* slot = reinterpret_cast<Slot*>(shared) + (size_t)mine * r.slots;
-    C* row = reinterpret_cast<C*>(shared + (size_t)tokens * r.slots * sizeof(Slot)) + (size_t)mine * (r.experts + r.groups);
+    const uint32_t size = r.experts / r.groups;
     C* of_group = row + r.experts;
-    for (uint32_t base = blockIdx.x * tokens; base < r.tokens; base += gridDim.x * tokens) {
-        const uint32_t i = base + mine;
-        const bool in = i < r.tokens && !(r.keep && !r.keep[i]);
-        words4 raw[CHUNKS] = {};
-        if (in) l.load(r.x, (int64_t)i * r.ld, raw);
-        float x[L::N];
-        L::unpack(raw, x);
-        bool nan = false;
-        float m = -INFINITY;
-        C c[L::N];
+    for (uint32_t g = lane; g < r.groups; g += part.lanes) {
+        C first = NONE, second = NONE;
+        for (uint32_t e = 0; e < size; ++e) best_two(first, second, row[g * size + e], NONE);
+        of_group[g] = r.group_top == 2 && second != NONE ? first + second : first;
+    }
+    lanes_exchange();
+    *least = INFINITY;
+    *next = NONE;
+    for (uint32_t g = lane; g < r.groups; g += part.lanes) {
+        const C y = of_group[g];
+        uint32_t better = 0;
+        for (uint32_t o = 0; o < r.groups; ++o) better += of_group[o] > y || (of_group[o] == y && o < g);
+        const bool out = better >= r.top_groups;
+        if (out || y == NONE)
+            for (uint32_t e = 0; e < size; ++e) row[g * size + e] = NONE;
+        if (out && y > *next) *next = y;
+        if (!out && y < *least) *least = y;
+    }
+    lanes_exchange();
+}
+
+// A token in binary64, value by value in LDS.
+template <int IN>
+__device__ __forceinline__ void route_in_binary64(const RouteCall& r, const Part& part, uint32_t lane, uint32_t i, double from, double* row, int32_t* slot) {
+    constexpr double NONE = -INFINITY;
+    double sum = 0.0;
+    for (uint32_t e = lane; e < r.experts; e += part.lanes) {
+        double x = (double)element<IN>(r.x, (int64_t)i * r.ld + e);
+        if (x != x) x = NONE;
+        const double s = r.sigmoid ? 1.0 / (1.0 + exp(-x)) : exp(x - from);
+        row[e] = x == NONE ? NONE : s;
+        if (x != NONE) sum += s;
+    }
+    sum = part.sum(sum);
+    for (uint32_t e = lane; e < r.experts; e += part.lanes) {
+        double s = row[e];
+        if (s == NONE) continue;
+        if (!r.sigmoid) s /= sum;
+        if (r.bias) s += (double)r.bias[e];
+        row[e] = s != s ? NONE : s;
+    }
+    lanes_exchange();
+    double least, next;
+    if (r.top_groups < r.groups) choose_groups(r, part, lane, row, &least, &next);
+    for (uint32_t k = 0; k < r.slots; ++k) {
+        double best = NONE;
+        uint32_t at = 0xffffffffu;
+        for (uint32_t e = lane; e < r.experts; e += part.lanes)
+            if (row[e] > best) best = row[e], at = e;
+        for (uint32_t o = part.lanes / 2; o; o >>= 1) {
+            const double other = __shfl_xor(best, o);
+            const uint32_t other_at = __shfl_xor(at, o);
+            if (other > best || (other == best && other_at < at)) best = other, at = other_at;
+        }
+        lanes_exchange();
+        if (lane == 0) {
+            slot[k] = best == NONE ? -1 : (int32_t)at;
+            if (best != NONE) row[at] = NONE;
+        }
+        lanes_exchange();
+    }
+}
+
+// What binary32 may be off in c = s + bias, relative to 1 + the token's largest |c|.  e^d by way of 2^(d log2 e), two rounded factors and the function's
+// last place: |d| 2^-23.4 + 2^-23 of it.
+//   sigmoid  s (1 - s) of that (|x| s (1 - s) < 0.23), s (2^-24 + 2^-23) for the sum and the reciprocal, 2^-24 |c| for the bias: below 2^-22 (1 + |c|)
+//   softmax  d = x - m is rounded too, |d| 2^-22.6: p |d| < 0.37 of its own, and p times the mean of |d| over the distribution, below 1.8 for 1024 experts,
+//            for the sum; p 2^-21.4 for functions, quotient and product: below 2^-20.4 (1 + |c|)
+constexpr float OFF_SIGMOID = 0x1p-22f, OFF_SOFTMAX = 0x1p-20f;
+
+// At least `wanted` of a token's lanes have a largest c that is not below what this returns.
+template <class P>
+__device__ __forceinline__ float bound_of(const P& part, float best, uint32_t wanted) {
+    uint32_t greater = 0;
+    auto count = [&](float other) { greater += other > best; };
+    if (part.lanes == 16) {
+        count(Part::moved<0x121>(best)), count(Part::moved<0x122>(best)), count(Part::moved<0x123>(best)), count(Part::moved<0x124>(best));   // row_ror
+        count(Part::moved<0x125>(best)), count(Part::moved<0x126>(best)), count(Part::moved<0x127>(best)), count(Part::moved<0x128>(best));
+        count(Part::moved<0x129>(best)), count(Part::moved<0x12a>(best)), count(Part::moved<0x12b>(best)), count(Part::moved<0x12c>(best));
+        count(Part::moved<0x12d>(best)), count(Part::moved<0x12e>(best)), count(Part::moved<0x12f>(best));
+    } else {
+        for (uint32_t o = 1; o < part.lanes; ++o) count(__shfl_xor(best, o));
+    }
+    return -part.max(greater < wanted ? -best : -INFINITY);
+}
+
+// The wavefront's LDS: candidates of its tokens, or their experts and groups, or one token's in binary64.
+constexpr uint32_t CANDIDATES = 64;
+struct Candidate {
+    float c;
+    uint32_t expert;
+};
+
+// BY_SCORE: c is a score and a bias, else the logit.  lds: bytes of a wavefront besides its slots.
+template <int IN, int CHUNKS, int LANES, bool BY_SCORE, bool GROUPS>
+__global__ void __launch_bounds__(256) k_route(RouteCall r, uint32_t lds) {
+    typedef TokenLanes<IN, CHUNKS> L;
+    constexpr float NONE = -INFINITY;
+    extern __shared__ __align__(16) char shared[];
+    if (LANES) r.lanes = LANES;
+    const L l(r.experts, r.lanes);
+    const PartOf<LANES> part(r.lanes);
+    const uint32_t wave = threadIdx.x >> 6, at_once = l.tokens(), tokens = (blockDim.x >> 6) * at_once;      // of the workgroup
+    const uint32_t mine = wave * at_once + l.of, of_group = r.experts / r.groups;
+    char* own = shared + wave * lds;
+    int32_t* slot = reinterpret_cast<int32_t*>(shared + (blockDim.x >> 6) * lds) + mine * r.slots;
+    // groups that are whole runs of lanes: `per` of them
+    const uint32_t per = of_group / L::WIDTH;           // (at least WIDTH experts each: no more groups than CHUNKS a lane)
+    const bool by_lanes = GROUPS && of_group % L::WIDTH == 0 && (per & (per - 1)) == 0 && per <= r.lanes;
+    const uint32_t per_shift = by_lanes ? 31 - __clz(per) : 0;
+    const bool at_a_time = r.lanes >= 16 && r.slots < r.lanes;
+    const uint32_t base = blockIdx.x * tokens;
+    const uint32_t i = base + mine;
+    const bool in = i < r.tokens && !(r.keep && !r.keep[i]);
+    words4 raw[CHUNKS];
+    if (in) {
+        l.load(r.x, (int64_t)i * r.ld, raw);
+    } else {
+        constexpr uint32_t none = IN == OUT_F32 ? 0xff800000u : IN == OUT_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) raw[k] = words4{none, none, none, none};
+    }
+    float c[L::N];
+    L::unpack(raw, c);
+    bool nan = false;
+#pragma unroll
+    for (int v = 0; v < L::N; v += 2) nan |= __builtin_isunordered(c[v], c[v + 1]);
+    if (__any(nan)) {
+#pragma unroll
+        for (int v = 0; v < L::N; ++v) c[v] = c[v] != c[v] ? NONE : c[v];
+    }
+    float m = NONE;
+#pragma unroll
+    for (int v = 0; v < L::N; ++v) {
+        c[v] = __builtin_canonicalizef(c[v]);                                       // known to be no signalling NaN, which costs maxima nothing then
+        m = fmaxf(m, c[v]);
+    }
+    m = part.max(m);
+    nan = part.any(nan) || (!r.sigmoid && m == INFINITY);
+    const float from = m == NONE ? 0.0f : m;
+    float by = 1.0f;                                                            // softmax: 1 / sum of e^(x - m)
+    bool close = false;
+    float off = 0.0f;
+    if (BY_SCORE) {
+        if (!r.sigmoid) {
+            double sum = 0.0;
+#pragma unroll
+            for (int v = 0; v < L::N; ++v) sum += (double)exp_of(c[v] - from);
+            by = (float)(1.0 / part.sum(sum));
+        }
+float bias[L::N];
+#pragma unroll
+        for (int v = 0; v < L::N; ++v) bias[v] = 0.0f;
+        if (r.bias) {
+#pragma unroll
+            for (int v = 0; v < L::N; v += 4) {
+                if (l.expert(v) + 4 <= r.experts) {
+                    const words4 four = *reinterpret_cast<const words4*>(r.bias + l.expert(v));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) bias[v + e] = __uint_as_float(four[e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (l.expert(v) + e < r.experts) bias[v + e] = r.bias[l.expert(v) + e];
+                }
+            }
+        }
 #pragma unroll
         for (int v = 0; v < L::N; ++v) {
-            if (!in || l.expert(v) >= r.experts) x[v] = -INFINITY;
-            nan |= x[v] != x[v];
-            if (x[v] != x[v]) x[v] = -INFINITY;
-            m = fmaxf(m, x[v]);
+            const float s = (r.sigmoid ? __builtin_amdgcn_rcpf(1.0f + exp_of(-c[v])) : exp_of(c[v] - from) * by) + bias[v];
+            c[v] = ((c[v] == NONE) | (s != s)) ? NONE : s;
+            off = fmaxf(off, c[v] == NONE ? 0.0f : fabsf(c[v]));
         }
-        m = part.max(m);
-        nan = part.any(nan) || (!r.sigmoid && m == INFINITY);
-        const float from = m == -INFINITY ? 0.0f : m;
-        float by = 1.0f;                                                            // softmax: 1 / sum of e^(x - m)
-        if (BY_SCORE) {
-            double e[L::N], sum = 0.0;
+        off = (r.sigmoid ? OFF_SIGMOID : OFF_SOFTMAX) * (1.0f + part.max(off));
+    } else if (!r.sigmoid && !r.renormalise) {
+        float sum = 0.0f;
 #pragma unroll
-            for (int v = 0; v < L::N; ++v) {
-                e[v] = r.sigmoid ? 1.0 / (1.0 + exp(-(double)x[v])) : exp((double)x[v] - (double)from);
-                sum += e[v];
+        for (int v = 0; v < L::N; ++v) sum += expf(c[v] - from);
+        by = 1.0f / part.sum(sum);
+    }
+    if (GROUPS) {
+        float least, next;
+        if (by_lanes) {
+            float* values = reinterpret_cast<float*>(own) + l.of * r.groups;
+#pragma unroll
+            for (int k = 0; k < CHUNKS; ++k) {
+                float first = NONE, second = NONE;
+#pragma unroll
+                for (int w = 0; w < L::WIDTH; ++w) best_two(first, second, c[k * L::WIDTH + w], NONE);
+                best_two_of(per, first, second);
+                const uint32_t g = (k * r.lanes + l.lane) >> per_shift;
+                if (g < r.groups) values[g] = r.group_top == 2 && second != NONE ? first + second : first;
             }
-            sum = part.sum(sum);
-            by = (float)(1.0 / sum);
+            lanes_exchange();
+            least = INFINITY;
+            next = NONE;
+            uint64_t out = 0;                                                       // of this lane's groups: as many as it has chunks at most
+            for (uint32_t g = l.lane, j = 0; g < r.groups; g += r.lanes, ++j) {
+                const float y = values[g];
+                uint32_t better = 0;
+#pragma unroll 4
+                for (uint32_t o = 0; o < r.groups; ++o) {
+                    const float other = values[o];
+                    better += (other > y) | ((other == y) & (o < g));
+                }
+                if (better < r.top_groups) {
+                    least = fminf(least, y);
+                } else {
+                    next = fmaxf(next, y);
+                    out |= 1ull << j;
+                }
+            }
+            lanes_exchange();
+            for (uint32_t g = l.lane, j = 0; g < r.groups; g += r.lanes, ++j)
+                if (out >> j & 1) values[g] = NAN;
+            lanes_exchange();
 #pragma unroll
-            for (int v = 0; v < L::N; ++v) {
-                const uint32_t ex = l.expert(v);
-                double s = r.sigmoid ? e[v] : e[v] / sum;
-                if (r.bias && ex < r.experts) s += (double)r.bias[ex];
-                c[v] = x[v] == -INFINITY || s != s ? NONE : (C)s;
+            for (int k = 0; k < CHUNKS; ++k) {
+                const uint32_t g = (k * r.lanes + l.lane) >> per_shift;
+                const float y = values[min(g, r.groups - 1)];
+#pragma unroll
+                for (int w = 0; w < L::WIDTH; ++w) c[k * L::WIDTH + w] = y != y ? NONE : c[k * L::WIDTH + w];
             }
         } else {
-            if (!r.sigmoid && !r.renormalise) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int v = 0; v < L::N; ++v) sum += expf(x[v] - from);
-                by = 1.0f / part.sum(sum);
-            }
-#pragma unroll
-            for (int v = 0; v < L::N; ++v) c[v] = (C)x[v];
-        }
-        if (GROUPS) {
-            const uint32_t size = r.experts / r.groups;
+            float* row = reinterpret_cast<float*>(own) + l.of * (r.experts + r.groups);
 #pragma unroll
             for (int v = 0; v < L::N; ++v)
                 if (l.expert(v) < r.experts) row[l.expert(v)] = c[v];
             lanes_exchange();
-            for (uint32_t g = l.lane; g < r.groups; g += r.lanes) {
-                C first = NONE, second = NONE;
-                for (uint32_t e = 0; e < size; ++e) {
-                    const C y = row[g * size + e];
-                    second = y > first ? first : y > second ? y : second;
-                    first = y > first ? y : first;
-                }
-                of_group[g] = r.group_top == 2 && second != NONE ? first + second : first;
-            }
-            lanes_exchange();
-            for (uint32_t g = l.lane; g < r.groups; g += r.lanes) {
-                const C y = of_group[g];
-                uint32_t better = 0;
-                for (uint32_t o = 0; o < r.groups; ++o) better += of_group[o] > y || (of_group[o] == y && o < g);
-                if (better >= r.top_groups || y == NONE)
-                    for (uint32_t e = 0; e < size; ++e) row[g * size + e] = NONE;
-            }
-            lanes_exchange();
+            choose_groups(r, part, l.lane, row, &least, &next);
 #pragma unroll
             for (int v = 0; v < L::N; ++v) c[v] = l.expert(v) < r.experts ? row[l.expert(v)] : NONE;
+        }
+        lanes_exchange();
+        if (BY_SCORE) {
+            least = -part.max(-least);
+            next = part.max(next);
+            close |= least != NONE && !(least - next > 4.0f * off);             // sums of two, each off; infinities are close
+        }
+    }
+    // All slots at once: the slots' lanes' largest c bound what can be chosen, and few c are not below that; each of those finds its
+    // place by comparing with the others.  (With a score one more than the slots, which must not be close to the last.)
+    constexpr uint32_t MORE = BY_SCORE ? 1 : 0;
+    bool done = false;
+    if (at_a_time) {
+        float best = NONE;
+#pragma unroll
+        for (int v = 0; v < L::N; ++v) best = fmaxf(best, c[v]);
+        const float bound = fmaxf(bound_of(part, best, r.slots + MORE), -3.4028235e38f);
+        uint32_t count = 0;
+#pragma unroll
+        for (int v = 0; v < L::N; ++v) count += c[v] >= bound;
+        uint32_t to = count;
+        for (uint32_t o = 1; o < r.lanes; o <<= 1) {
+            const uint32_t other = __shfl_up(to, o);
+            if (l.lane >= o) to += other;
+        }
+        const uint32_t n = __shfl(to, (threadIdx.x & 63) | (r.lanes - 1));
+        to -= count;
+        done = !__any(n > CANDIDATES);
+        if (done) {
+            Candidate* list = reinterpret_cast<Candidate*>(own) + l.of * CANDIDATES;
+#pragma unroll
+            for (int v = 0; v < L::N; ++v)
+                if (c[v] >= bound) list[to++] = Candidate{c[v], l.expert(v)};
+            for (uint32_t k = l.lane; k < r.slots; k += r.lanes) slot[k] = -1;
+            lanes_exchange();
+            for (uint32_t k = l.lane; k < n; k += r.lanes) {
+                const Candidate me = list[k];
+                uint32_t before = 0;
+                bool near = false;
+                for (uint32_t o = 0; o < n; ++o) {
+                    const Candidate other = list[o];
+                    before += (other.c > me.c) | ((other.c == me.c) & (other.expert < me.expert));
+                    if (BY_SCORE) near |= (o != k) & !(fabsf(other.c - me.c) > 2.0f * off);
+                }
+                if (before < r.slots) {
+                    slot[before] = (int32_t)me.expert;
+                    close |= near;
+                }
+            }
+            close = part.any(close);
             lanes_exchange();
         }
-        // the slots: of equal c the lower expert, which is also the lower v of a lane
-        float most = -INFINITY;                                                     // of the chosen logits (sigmoid: at most 0)
-        for (uint32_t k = 0; k < r.slots; ++k) {
-            C best = NONE;
-            uint32_t at = 0xffffffffu;
-            float logit = 0.0f;
+    }
+    if (!done) {                        // of equal c the lower expert, which is also the lower v of a lane
+        float before = INFINITY;
+        for (uint32_t k = 0; k < r.slots + MORE; ++k) {
+            float best = NONE;
 #pragma unroll
-            for (int v = 0; v < L::N; ++v)
-                if (c[v] > best) best = c[v], at = l.expert(v), logit = x[v];
-            for (uint32_t o = r.lanes / 2; o; o >>= 1) {
-                const C other = __shfl_xor(best, o);
-                const uint32_t other_at = __shfl_xor(at, o);
-                const float other_logit = __shfl_xor(logit, o);
-                if (other > best || (other == best && other_at < at)) best = other, at = other_at, logit = other_logit;
+            for (int v = 0; v < L::N; ++v) best = fmaxf(best, c[v]);
+            best = part.max(best);
+            if (BY_SCORE) {
+                close |= k && best != NONE && !(before - best > 2.0f * off);
+                before = best;
+                if (k == r.slots) break;
             }
+            uint32_t at = 0xffffffffu;
 #pragma unroll
-            for (int v = 0; v < L::N; ++v)
-                if (l.expert(v) == at) c[v] = NONE;
-            const bool some = best != NONE;
-            if (some) most = fmaxf(most, r.sigmoid ? fminf(logit, 0.0f) : logit);
-            if (l.lane == 0) slot[k] = Slot{some ? (int32_t)at : -1, logit};
+            for (int v = L::N; v-- > 0;) at = c[v] == best ? l.expert(v) : at;
+            at = part.min(at);
+#pragma unroll
+            for (int v = 0; v < L::N; ++v) c[v] = l.expert(v) == at ? NONE : c[v];
+            if (l.lane == 0) slot[k] = best == NONE ? -1 : (int32_t)at;
         }
         lanes_exchange();
-        float all = 0.0f;
-        auto share = [&](const Slot& s, float m) { return s.expert < 0 ? 0.0f : r.sigmoid ? sigmoid_over(s.x, m) : expf(s.x - m); };
+    }
+    if (BY_SCORE) {
+        for (uint64_t again = __ballot(close && in && l.lane == 0); again; again &= again - 1) {
+            const uint32_t lane = __ffsll((unsigned long long)again) - 1, token = wave * at_once + lane / r.lanes;
+            route_in_binary64<IN>(r, Part(64), threadIdx.x & 63, base + token, (double)__shfl(from, lane), reinterpret_cast<double*>(own),
+                                  slot + ((int32_t)token - (int32_t)mine) * (int32_t)r.slots);
+        }
+    }
+    if (i < r.tokens) {
+        // a lane's slots: the first's logit is at hand, more than one are read again
+        auto logit = [&](int32_t e) { return element<IN>(r.x, (int64_t)i * r.ld + e); };
+        const int32_t mine0 = l.lane < r.slots ? slot[l.lane] : -1;
+        const float x0 = mine0 >= 0 ? logit(mine0) : NONE;
+        auto x_of = [&](uint32_t k, int32_t e) { return k == l.lane ? x0 : logit(e); };
+        auto share = [&](float x, float m) { return r.sigmoid ? sigmoid_over(x, m) : expf(x - m); };
+        float all = 1.0f, most = r.sigmoid ? 0.0f : m;
         if (r.renormalise) {
-            for (uint32_t k = l.lane; k < r.slots; k += r.lanes) all += share(slot[k], most);
+            most = r.sigmoid && mine0 >= 0 ? fminf(x0, 0.0f) : x0;
+            for (uint32_t k = l.lane + r.lanes; k < r.slots; k += r.lanes)
+                if (slot[k] >= 0) most = fmaxf(most, r.sigmoid ? fminf(logit(slot[k]), 0.0f) : logit(slot[k]));
+            most = part.max(most);
+            all = mine0 >= 0 ? share(x0, most) : 0.0f;
+            for (uint32_t k = l.lane + r.lanes; k < r.slots; k += r.lanes)
+                if (slot[k] >= 0) all += share(logit(slot[k]), most);
             all = part.sum(all);
         }
-        if (i < r.tokens)
-            for (uint32_t k = l.lane; k < r.slots; k += r.lanes) {
-                const Slot s = slot[k];
-                float y = r.renormalise ? share(s, most) / all : r.sigmoid ? share(s, 0.0f) : share(s, m) * by;
-                y = s.expert < 0 ? 0.0f : y * r.scale;
-                const size_t to = (size_t)i * r.slots + k;
-                r.chosen[to] = s.expert;
-                r.weight[to] = nan ? NAN : y;
-            }
-        lanes_exchange();
+        for (uint32_t k = l.lane; k < r.slots; k += r.lanes) {
+            const int32_t e = slot[k];
+            float y = 0.0f;
+            if (e >= 0) y = share(x_of(k, e), most) * (r.renormalise || r.sigmoid ? 1.0f : by) / all * r.scale;
+            const size_t to = (size_t)i * r.slots + k;
+            r.chosen[to] = e;
+            r.weight[to] = nan ? NAN : y;
+        }
     }
 }
 
@@ -199,22 +463,17 @@ struct SlotGradient {
     float d;
 };
 
-template <int IN>
-__device__ __forceinline__ float element(const void* x, int64_t at) {
-    if (IN == OUT_F32) return static_cast<const float*>(x)[at];
-    const uint16_t b = static_cast<const uint16_t*>(x)[at];
-    return IN == OUT_BF16 ? Bf16::value(b) : F16::value(b);
-}
-
 template <int IN, int CHUNKS>
 __global__ void __launch_bounds__(256) k_route_gradient(RouteGradient r) {
     typedef TokenLanes<IN, CHUNKS> L;
     extern __shared__ __align__(16) char shared[];
     const L l(r.experts, r.lanes);
-    const Part part{r.lanes};
+    const Part part(r.lanes);
     const uint32_t wave = threadIdx.x >> 6, at_once = l.tokens(), tokens = (blockDim.x >> 6) * at_once;
     const uint32_t mine = wave * at_once + l.of;
     SlotGradient* slot = reinterpret_cast<SlotGradient*>(shared) + (size_t)mine * r.slots;
+    const uint32_t units = (r.experts + L::WIDTH - 1) / L::WIDTH * L::WIDTH;
+    f32_bytes* row = reinterpret_cast<f32_bytes*>(shared + (size_t)tokens * r.slots * sizeof(SlotGradient)) + (size_t)mine * units;
     const bool dense = !r.sigmoid && !r.renormalise;
     for (uint32_t base = blockIdx.x * tokens; base < r.tokens; base += gridDim.x * tokens) {
         const uint32_t i = base + mine;
@@ -271,14 +530,31 @@ __global__ void __launch_bounds__(256) k_route_gradient(RouteGradient r) {
             }
             slot[k] = SlotGradient{e, d};
         }
+        // by expert: the slots' parts in their order, so that the sum of an expert's is the same every time
+#pragma unroll
+        for (int v = 0; v < L::N; v += 4)
+            if (l.expert(v) < units) *reinterpret_cast<f32x4_bytes*>(row + l.expert(v)) = f32x4{};
+        lanes_exchange();
+        for (uint32_t k = l.lane; k < r.slots; k += r.lanes) {
+            const SlotGradient s = slot[k];
+            if (s.expert >= r.experts) continue;
+            bool first = true;
+            float sum = s.d;
+            for (uint32_t o = 0; o < r.slots; ++o) {
+                if (o == k || slot[o].expert != s.expert) continue;
+                first &= o > k;
+                sum += slot[o].d;
+            }
+            if (first) row[s.expert] = sum;
+        }
         lanes_exchange();
         float d[L::N];
 #pragma unroll
-        for (int v = 0; v < L::N; ++v) d[v] = 0.0f;
-        for (uint32_t k = 0; k < r.slots; ++k) {
-            const SlotGradient s = slot[k];
+        for (int v = 0; v < L::N; v += 4) {
+            f32x4 four = {};
+            if (l.expert(v) < units) four = *reinterpret_cast<const f32x4_bytes*>(row + l.expert(v));
 #pragma unroll
-            for (int v = 0; v < L::N; ++v) d[v] += l.expert(v) == s.expert ? s.d : 0.0f;
+            for (int e = 0; e < 4; ++e) d[v + e] = four[e];
         }
         lanes_exchange();
         if (i >= r.tokens) continue;

@@ -32,4 +32,4 @@ def test_casts_of_pointers():
     text = "".join(open(os.path.join(CSRC, n)).read() for n in ("iwp_tokens.hpp", "iwp_route.hpp", "iwp_grouped.hpp", "iwp_experts.hip", "iwp_clip.hip"))
     alias = set(re.findall(r"typedef \w+ (\w+) __attribute__\(\([^;]*\bmay_alias\b[^;]*\)\);", shared + text))
     casts = set(re.findall(r"reinterpret_cast<(?:const )?(\w+)\s*\*>", text)) - alias
-    assert casts == {"char", "uint16_t", "uint32_t", "f32x4", "T", "C", "Slot", "SlotGradient"}
+    assert casts == {"char", "uint16_t", "uint32_t", "f32x4", "T", "Candidate", "SlotGradient"}
