@@ -27,9 +27,9 @@ def test_waits_around_the_loads(tmp_path):
 
 def test_casts_of_pointers():
     """Only to types that may alias any other, to char, or to an element's own type where a caller's row is at hand as char or what a kernel's
-    own LDS or workspace holds is of that type throughout."""
+    own LDS or workspace holds is of that type throughout, or from one fence to the next (the routing's LDS)."""
     shared = open(os.path.join(CSRC, "iwp_matrix.hpp")).read()
     text = "".join(open(os.path.join(CSRC, n)).read() for n in ("iwp_tokens.hpp", "iwp_route.hpp", "iwp_grouped.hpp", "iwp_experts.hip", "iwp_clip.hip"))
     alias = set(re.findall(r"typedef \w+ (\w+) __attribute__\(\([^;]*\bmay_alias\b[^;]*\)\);", shared + text))
     casts = set(re.findall(r"reinterpret_cast<(?:const )?(\w+)\s*\*>", text)) - alias
-    assert casts == {"char", "uint16_t", "uint32_t", "f32x4", "T", "Candidate", "SlotGradient"}
+    assert casts == {"char", "uint16_t", "uint32_t", "f32x4", "T", "Candidate", "SlotGradient", "float", "double", "int32_t"}
