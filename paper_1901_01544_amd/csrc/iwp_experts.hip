@@ -100,6 +100,7 @@ struct ProductPlan {
     uint32_t deep, ld_x, ld_d;             // elements in 128 bytes; widths rounded up to that
     TileKind rows_tile, dw_tile;
     uint32_t height, max_tiles;
+    uint32_t arrangers, per_wave;          // workgroups that arrange the slots, slots of a wavefront
     ExpertRows R;
     char *x, *d, *w;                       // gathered rows, gathered gradients, copied matrices
     float* sums;
@@ -111,6 +112,9 @@ bool readable(const void* w, int64_t ld, int64_t step, uint32_t in, uint32_t dty
     return aligned(w, 16) && ld % chunk == 0 && step % chunk == 0 && in % chunk == 0;
 }
 
+// A workgroup arranges 4096 slots, four rounds of its wavefronts, up to 64 of them, each of which reads all the others' counts.
+constexpr uint32_t ARRANGE_SLOTS = 4096, ARRANGE_MOST = 64;
+
 ProductPlan product_plan(const ProductSizes& z, bool copy_w, void* workspace) {
     ProductPlan p{};
     p.deep = ROW_BYTES / (uint32_t)size_of(z.dtype);
@@ -121,7 +125,10 @@ ProductPlan product_plan(const ProductSizes& z, bool copy_w, void* workspace) {
     p.dw_tile = tile_for(z.in, z.out, z.experts);
     p.height = p.rows_tile == BIG ? Big::BQ : p.rows_tile == MID ? Mid::BQ : Few::BQ;
     p.max_tiles = n / p.height + many + 1;
+    p.arrangers = std::max(1u, std::min((n + ARRANGE_SLOTS - 1) / ARRANGE_SLOTS, ARRANGE_MOST));
+    p.per_wave = round_up((n + p.arrangers * ARRANGE_WAVES - 1) / (p.arrangers * ARRANGE_WAVES), 64u);
     Carver c{static_cast<char*>(workspace)};
+    if (p.arrangers > 1) c.take(p.R.counts, (size_t)p.arrangers * (z.experts + 1));
     c.take(p.R.start, z.experts + 1);
     c.take(p.R.count, z.experts + 1);
     c.take(p.R.slot, (size_t)z.padded() + n);
@@ -156,7 +163,8 @@ int with_kind(uint32_t dtype, F f) {
 }
 
 int arrange(const ProductSizes& z, const ProductPlan& p, const int32_t* chosen, hipStream_t s) {
-    IWP_LAUNCH_BLOCK("k_expert_arrange", k_expert_arrange, 1, ARRANGE_WAVES * 64, s, chosen, z.rows(), z.experts, p.height, p.R);
+    if (p.arrangers > 1) IWP_LAUNCH_BLOCK("k_expert_count", k_expert_count, p.arrangers, ARRANGE_THREADS, s, chosen, z.rows(), p.per_wave, z.experts, p.R);
+    IWP_LAUNCH_BLOCK("k_expert_arrange", k_expert_arrange, p.arrangers, ARRANGE_THREADS, s, chosen, z.rows(), p.per_wave, z.experts, p.height, p.R);
     return IWP_OK;
 }
 

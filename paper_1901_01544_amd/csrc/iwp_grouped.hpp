@@ -23,6 +23,7 @@ struct ExpertRows {        // experts' rows after each other, in the order of sl
     uint32_t* slot;        // [padded rows] which slot a row is, NOBODY behind an expert's rows
     ExpertTile* tile;      // the rows in tiles, those of nobody too
     uint32_t* tiles;       // [1]
+    uint32_t* counts;      // [workgroups that arrange, experts + 1]: slots of each one's part
 };
 
 // ------------------------------------------------------------------ the rows
@@ -39,23 +40,64 @@ __device__ __forceinline__ uint64_t same_lanes(uint32_t value, bool in) {
     return same;
 }
 
-// One workgroup: counts every wavefront's part of the slots by expert, where the experts' rows then begin, and puts every slot in its place.
-constexpr uint32_t ARRANGE_WAVES = 16;
-__global__ void __launch_bounds__(ARRANGE_WAVES * 64) k_expert_arrange(const int32_t* __restrict__ chosen, uint32_t n, uint32_t experts,
-                                                                       uint32_t height, ExpertRows R) {
+// Which slots go where.  Every workgroup has a part of the slots, every wavefront a part of that; slots of an expert stay in order.
+constexpr uint32_t ARRANGE_WAVES = 16, ARRANGE_THREADS = ARRANGE_WAVES * 64;
+struct SlotPart {
+    uint32_t from, to;
+    __device__ __forceinline__ SlotPart(uint32_t n, uint32_t per_wave) {
+        const uint32_t wave = blockIdx.x * ARRANGE_WAVES + (threadIdx.x >> 6);
+        from = min(wave * per_wave, n);
+        to = min(from + per_wave, n);
+    }
+};
+__device__ __forceinline__ uint32_t bucket_of(const int32_t* chosen, uint32_t i, uint32_t experts) { return min((uint32_t)chosen[i], experts); }
+
+// Slots of every expert in each workgroup's part (where there is more than one).
+__global__ void __launch_bounds__(ARRANGE_THREADS) k_expert_count(const int32_t* __restrict__ chosen, uint32_t n, uint32_t per_wave, uint32_t experts,
+                                                                  ExpertRows R) {
+    __shared__ uint32_t of[IWP_MAX_EXPERTS + 1];
+    for (uint32_t e = threadIdx.x; e <= experts; e += ARRANGE_THREADS) of[e] = 0;
+    __syncthreads();
+    const SlotPart part(n, per_wave);
+    for (uint32_t i = part.from + (threadIdx.x & 63); i < part.to; i += 64) atomicAdd(&of[bucket_of(chosen, i, experts)], 1u);
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e <= experts; e += ARRANGE_THREADS) R.counts[blockIdx.x * (experts + 1) + e] = of[e];
+}
+
+// Counts the wavefronts' parts, finds where the experts' rows begin and puts every slot in its place.  Every workgroup adds up the others'
+// counts itself; the first one writes what is one for all.  us for 32768 slots, 64 experts: one workgroup alone 52, counting and placing by 8
+// workgroups 6 and 8.
+__global__ void __launch_bounds__(ARRANGE_THREADS) k_expert_arrange(const int32_t* __restrict__ chosen, uint32_t n, uint32_t per_wave, uint32_t experts,
+                                                                    uint32_t height, ExpertRows R) {
     __shared__ uint32_t at[ARRANGE_WAVES][IWP_MAX_EXPERTS + 1];
-    __shared__ uint32_t rows_of[ARRANGE_WAVES], tiles_of[ARRANGE_WAVES];
+    __shared__ uint32_t rows_of[ARRANGE_WAVES], tiles_of[ARRANGE_WAVES], nobody_of[2];
     const uint32_t thread = threadIdx.x, wave = thread >> 6, lane = thread & 63;
-    const uint32_t part = (n + ARRANGE_WAVES * 64 - 1) / (ARRANGE_WAVES * 64) * 64, from = min(wave * part, n), to = min(from + part, n);
+    const SlotPart part(n, per_wave);
     for (uint32_t e = lane; e <= experts; e += 64) at[wave][e] = 0;
     lanes_exchange();
-    auto bucket = [&](uint32_t i) { return min((uint32_t)chosen[i], experts); };
-    for (uint32_t i = from + lane; i < to; i += 64) atomicAdd(&at[wave][bucket(i)], 1u);
+    for (uint32_t i = part.from + lane; i < part.to; i += 64) atomicAdd(&at[wave][bucket_of(chosen, i, experts)], 1u);
     __syncthreads();
-    // experts' rows and tiles: this thread's expert's, then those before it
-    uint32_t mine = 0;
-    if (thread < experts)
-        for (uint32_t w = 0; w < ARRANGE_WAVES; ++w) mine += at[w][thread];
+    // slots of this thread's expert (the thread after the experts': nobody's) in all parts and in those before this workgroup's
+    auto count = [&](uint32_t e, uint32_t* all, uint32_t* before) {
+        *all = *before = 0;
+        if (gridDim.x == 1) {
+            for (uint32_t w = 0; w < ARRANGE_WAVES; ++w) *all += at[w][e];
+            return;
+        }
+#pragma unroll 8
+        for (uint32_t b = 0; b < gridDim.x; ++b) {
+            const uint32_t c = R.counts[b * (experts + 1) + e];
+            *all += c;
+            if (b < blockIdx.x) *before += c;
+        }
+    };
+    uint32_t mine = 0, before = 0, none = 0, none_before = 0;
+    if (thread < experts) count(thread, &mine, &before);
+    if (thread == ARRANGE_THREADS - 1) {
+        count(experts, &none, &none_before);
+        nobody_of[0] = none;
+        nobody_of[1] = none_before;
+    }
     const uint32_t padded = (mine + PAD_ROWS - 1) / PAD_ROWS * PAD_ROWS, tiles = (mine + height - 1) / height;
     uint32_t rows_to = padded, tiles_to = tiles;
     for (uint32_t o = 1; o < 64; o <<= 1) {
@@ -70,32 +112,36 @@ __global__ void __launch_bounds__(ARRANGE_WAVES * 64) k_expert_arrange(const int
         all_rows += rows_of[w];
         all_tiles += tiles_of[w];
     }
-    auto put = [&](uint32_t e, uint32_t start, uint32_t count, uint32_t first_tile) {
-        R.start[e] = start;
-        R.count[e] = count;
-        for (uint32_t t = 0; t * height < count; ++t) R.tile[first_tile + t] = ExpertTile{e, t * height};
+    none = nobody_of[0];
+    // what this thread's expert has, from `start` on
+    auto put = [&](uint32_t e, uint32_t start, uint32_t count, uint32_t first_tile, uint32_t before) {
+        if (blockIdx.x == 0) {
+            R.start[e] = start;
+            R.count[e] = count;
+            for (uint32_t t = 0; t * height < count; ++t) R.tile[first_tile + t] = ExpertTile{e, t * height};
+        }
+        uint32_t to = start + before;
         for (uint32_t w = 0; w < ARRANGE_WAVES; ++w) {
             const uint32_t c = at[w][e];
-            at[w][e] = start;
-            start += c;
+            at[w][e] = to;
+            to += c;
         }
-        return start;
     };
     if (thread < experts) {
         const uint32_t start = rows_to - padded;
-        for (uint32_t r = put(thread, start, mine, tiles_to - tiles); r < start + padded; ++r) R.slot[r] = NOBODY;
+        put(thread, start, mine, tiles_to - tiles, before);
+        if (blockIdx.x == 0)
+            for (uint32_t r = start + mine; r < start + padded; ++r) R.slot[r] = NOBODY;
     }
     if (thread == 0) {
-        uint32_t none = 0;
-        for (uint32_t w = 0; w < ARRANGE_WAVES; ++w) none += at[w][experts];
-        put(experts, all_rows, none, all_tiles);
-        *R.tiles = all_tiles + (none + height - 1) / height;
+        put(experts, all_rows, none, all_tiles, nobody_of[1]);
+        if (blockIdx.x == 0) *R.tiles = all_tiles + (none + height - 1) / height;
     }
     __syncthreads();
-    for (uint32_t base = from; base < to; base += 64) {
+    for (uint32_t base = part.from; base < part.to; base += 64) {
         const uint32_t i = base + lane;
-        const bool in = i < to;
-        const uint32_t e = in ? bucket(i) : 0;
+        const bool in = i < part.to;
+        const uint32_t e = in ? bucket_of(chosen, i, experts) : 0;
         const uint64_t same = same_lanes(e, in);
         const uint32_t rank = __popcll(same & ((1ull << lane) - 1)), first = at[wave][e];
         lanes_exchange();

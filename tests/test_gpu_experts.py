@@ -221,3 +221,22 @@ def test_same_bytes_on_another_stream_and_in_a_graph(experts, size):
         torch.cuda.synchronize()
         for a, b, c in zip(first, second, third):
             assert torch.equal(a, b) and torch.equal(a, c)
+
+
+@pytest.mark.parametrize("T,K,E", [(4096, 1, 3), (4097, 1, 1024), (20000, 3, 17), (9000, 8, 64), (300_000, 1, 5)])
+def test_many_slots(experts, T, K, E):
+    """Several workgroups arrange them; rows so narrow that the products are nothing.  Whole numbers, so every sum is exact."""
+    gen = torch.Generator(device=DEV).manual_seed(T)
+    x = torch.randint(-8, 9, (T, K, 8), generator=gen, device=DEV).to(torch.bfloat16)
+    w = torch.randint(-4, 5, (E, 8, 8), generator=gen, device=DEV).to(torch.bfloat16)
+    chosen = torch.randint(-1, E + 1, (T, K), generator=gen, device=DEV, dtype=torch.int32)
+    inside = (chosen >= 0) & (chosen < E)
+    of = w.float()[torch.where(inside, chosen, 0).long()]
+    want = torch.where(inside[:, :, None], (of * x.float()[:, :, None, :]).sum(3), 0.0)
+    assert torch.equal(product(experts, x, w, chosen), want.to(torch.bfloat16))
+    dy = torch.randint(-2, 3, (T, K, 8), generator=gen, device=DEV).to(torch.bfloat16)
+    dx, dw = gradient(experts, x, w, chosen, dy, dw_kind=torch.float32)
+    assert torch.equal(dx, torch.where(inside[:, :, None], (of * dy.float()[:, :, :, None]).sum(2), 0.0).to(torch.bfloat16))
+    outer = dy.double()[inside][:, :, None] * x.double()[inside][:, None, :]
+    want = torch.zeros(E, 8, 8, dtype=torch.float64, device=DEV).index_add_(0, chosen[inside].long(), outer)
+    assert torch.equal(dw.double(), want)
