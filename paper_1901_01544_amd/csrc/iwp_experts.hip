@@ -69,7 +69,8 @@ uint64_t tiles_of(uint64_t np, uint64_t nq) { return (np + T::BP - 1) / T::BP * 
 
 constexpr uint64_t ENOUGH_TILES = 160;
 // `each`: entries of Q that one expert has; `many`: experts that have that many
-TileKind tile_for(uint64_t np, uint64_t each, uint64_t many) {
+TileKind tile_for(uint64_t np, uint64_t each, uint64_t many, uint32_t dtype) {
+    if (dtype == IWP_F32) return FEW;
     if (many * tiles_of<Big>(np, each) >= ENOUGH_TILES && each > Mid::BQ) return BIG;
     return many * tiles_of<Mid>(np, each) >= ENOUGH_TILES && each > Few::BQ ? MID : FEW;
 }
@@ -121,8 +122,8 @@ ProductPlan product_plan(const ProductSizes& z, bool copy_w, void* workspace) {
     p.ld_x = round_up(z.in, p.deep);
     p.ld_d = round_up(z.out, p.deep);
     const uint32_t n = z.rows(), many = std::max(1u, std::min(z.experts, n)), each = (n + many - 1) / many;
-    p.rows_tile = tile_for(z.gradient ? z.in : z.out, each, many);
-    p.dw_tile = tile_for(z.in, z.out, z.experts);
+    p.rows_tile = tile_for(z.gradient ? z.in : z.out, each, many, z.dtype);
+    p.dw_tile = tile_for(z.in, z.out, z.experts, z.dtype);
     p.height = p.rows_tile == BIG ? Big::BQ : p.rows_tile == MID ? Mid::BQ : Few::BQ;
     p.max_tiles = n / p.height + many + 1;
     p.arrangers = std::max(1u, std::min((n + ARRANGE_SLOTS - 1) / ARRANGE_SLOTS, ARRANGE_MOST));
@@ -194,7 +195,8 @@ template <class K, int OUT, bool TRANSPOSED>
 int rows_product(const ProductSizes& z, const ProductPlan& p, const Matrices& W, const Packed& X, const RowsOut& Y, hipStream_t s) {
     return with_tile(p.rows_tile, [&](auto tile) {
         typedef decltype(tile) T;
-        auto kernel = k_expert_rows<typename K::E, T::BP, T::BQ, T::WP, T::WQ, OUT, TRANSPOSED>;
+        auto kernel = X.slots ? k_expert_rows<typename K::E, T::BP, T::BQ, T::WP, T::WQ, OUT, TRANSPOSED, false>
+                              : k_expert_rows<typename K::E, T::BP, T::BQ, T::WP, T::WQ, OUT, TRANSPOSED, true>;
         const uint32_t np = ((TRANSPOSED ? z.in : z.out) + T::BP - 1) / T::BP;
         IWP_LAUNCH_BLOCK("k_expert_rows", kernel, np * p.max_tiles, T::THREADS, s, W, X, p.R, z.experts, Y);
         return (int)IWP_OK;
@@ -220,6 +222,12 @@ bool launches_fit(const ProductSizes& z, const ProductPlan& p) {
         typedef decltype(tile) T;
         return (int)(z.experts * tiles_of<T>(z.in, z.out) * T::THREADS <= MOST_THREADS);
     });
+}
+
+// Can a product read these rows where they lie?  By 16 bytes, whole tiles of the summed index, within what 32 bits count.
+bool in_place(const void* x, int64_t ld, uint32_t dim, uint64_t rows, uint32_t dtype) {
+    const uint64_t size = size_of(dtype);
+    return aligned(x, 16) && ld * size % 16 == 0 && dim * size % ROW_BYTES == 0 && rows * ld * size < (uint64_t)1 << 32;
 }
 
 // What both calls check: sizes, x, w and chosen.
@@ -322,10 +330,12 @@ int iwp_expert_product(const void* x, int64_t ld_x, uint32_t x_by_slot, const vo
         typedef decltype(kind) K;
         constexpr int SIZE = K::E::SIZE;
         Matrices W;
+        Packed X{p.x, p.ld_x, in, 0};
         int rc = arrange(z, p, chosen, s);
-        if (!rc) rc = gather<SIZE>(z, p, x, ld_x, in, z.by_slot, p.x, p.ld_x, s);
+        if (in_place(x, ld_x, in, z.by_slot ? z.rows() : tokens, dtype)) X = Packed{static_cast<const char*>(x), (uint32_t)ld_x, in, z.by_slot ? 1 : slots};
+        else if (!rc) rc = gather<SIZE>(z, p, x, ld_x, in, z.by_slot, p.x, p.ld_x, s);
         if (!rc) rc = matrices<SIZE>(z, p, w, ld_w, step_w, &W, s);
-        if (!rc) rc = rows_product<K, K::OUT, false>(z, p, W, Packed{p.x, p.ld_x, in}, RowsOut{static_cast<char*>(y), ld_y}, s);
+        if (!rc) rc = rows_product<K, K::OUT, false>(z, p, W, X, RowsOut{static_cast<char*>(y), ld_y}, s);
         return rc;
     });
 }
@@ -352,10 +362,13 @@ int iwp_expert_product_gradient(const void* x, int64_t ld_x, uint32_t x_by_slot,
     return with_kind(dtype, [&](auto kind) {
         typedef decltype(kind) K;
         constexpr int SIZE = K::E::SIZE;
-        const Packed X{p.x, p.ld_x, in}, D{p.d, p.ld_d, out};
+        const Packed X{p.x, p.ld_x, in, 0};
+        Packed D{p.d, p.ld_d, out, 0};
         int rc = arrange(z, p, chosen, s);
         if (!rc && dw) rc = gather<SIZE>(z, p, x, ld_x, in, z.by_slot, p.x, p.ld_x, s);
-        if (!rc) rc = gather<SIZE>(z, p, dy, ld_dy, out, true, p.d, p.ld_d, s);
+        // without the matrices' gradient, dy's rows may do where they lie
+        if (!dw && in_place(dy, ld_dy, out, z.rows(), dtype)) D = Packed{static_cast<const char*>(dy), (uint32_t)ld_dy, out, 1};
+        else if (!rc) rc = gather<SIZE>(z, p, dy, ld_dy, out, true, p.d, p.ld_d, s);
         if (!rc && dx && tokens) {
             Matrices W;
             rc = matrices<SIZE>(z, p, w, ld_w, step_w, &W, s);

@@ -224,9 +224,16 @@ struct Matrices {          // one for every expert
     int64_t step;          // elements from one to the next
     uint32_t ld, rows, columns;
 };
-struct Packed {            // gathered rows
+struct Packed {            // gathered rows, or where they lie: a slot's own, or its token's
     const char* x;
     uint32_t ld, dim;
+    uint32_t slots;        // of a token whose row is read where it lies (1: a row for every slot); 0: gathered
+};
+struct SlotRows {
+    static constexpr bool ANYWHERE = true;
+    const uint32_t* slot;
+    uint32_t slots;
+    __device__ __forceinline__ uint32_t operator()(uint32_t q) const { return slots == 1 ? slot[q] : slot[q] / slots; }
 };
 struct RowsOut {
     char* y;
@@ -285,7 +292,7 @@ __device__ __forceinline__ void store_tile(const M& mm, char* lds, uint32_t p0, 
 
 // Every expert's rows times its matrix (TRANSPOSED: W, not W^T, as for the rows' gradient), to the slots' rows of the output; zeros for
 // slots of nobody.
-template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool TRANSPOSED>
+template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool TRANSPOSED, bool GATHERED>
 __global__ void __launch_bounds__(WP * WQ * 64) k_expert_rows(Matrices W, Packed X, ExpertRows R, uint32_t experts, RowsOut Y) {
     typedef Product<E, BP, BQ, WP, WQ, TRANSPOSED, false> M;
     __shared__ __align__(1024) char lds[M::LDS];
@@ -301,8 +308,10 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_expert_rows(Matrices W, Packed
     if (tile.expert < experts) {
         const uint32_t summed = TRANSPOSED ? W.rows : W.columns;
         const Operand P{reinterpret_cast<const uint16_t*>(W.w + tile.expert * W.step * E::SIZE), nullptr, W.ld, columns, summed};
-        const Operand Q{reinterpret_cast<const uint16_t*>(X.x + (size_t)start * X.ld * E::SIZE), nullptr, X.ld, count, X.ld};
-        mm.run(P, Q, tp * BP, tile.first, 0, (summed + M::DEEP - 1) / M::DEEP * M::DEEP, lds);
+        const uint32_t to = (summed + M::DEEP - 1) / M::DEEP * M::DEEP;
+        const Operand Q{reinterpret_cast<const uint16_t*>(GATHERED ? X.x + (size_t)start * X.ld * E::SIZE : X.x), nullptr, X.ld, count, to};
+        if constexpr (GATHERED) mm.run(P, Q, tp * BP, tile.first, 0, to, lds);
+        else mm.run(P, Q, tp * BP, tile.first, 0, to, lds, SlotRows{R.slot + start, X.slots});
     } else {
 #pragma unroll
         for (int a = 0; a < M::FP; ++a)

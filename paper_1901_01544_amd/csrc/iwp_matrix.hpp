@@ -132,6 +132,12 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
 }
 
+// Rows of Q that lie anywhere in its matrix: row(q) is where entry q is.  All rows within 2^32 bytes.
+struct InOrder {
+    static constexpr bool ANYWHERE = false;
+    __device__ __forceinline__ uint32_t operator()(uint32_t q) const { return q; }
+};
+
 // One operand's tile: R entries of its own index, 128 bytes of the summed one, WAVES wavefronts loading elements of SIZE bytes.
 //
 // Rows of K: LDS row r holds the 8 chunks (16 bytes) of entry r, chunk c at place c ^ turn(r).
@@ -173,6 +179,18 @@ struct Tile {
                 within[i] = row;
                 at[i] = entry * SIZE + row * row_bytes;
             }
+        }
+    }
+    // The same of rows that lie anywhere, from the matrix's first one on
+    template <class Rows>
+    __device__ __forceinline__ void init_anywhere(const Operand& o, uint32_t first, int wave, int lane, const Rows& row_of) {
+        static_assert(!COLUMNS, "rows");
+        row_bytes = o.ld * SIZE;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t slot = (wave * LOADS + i) * 64 + lane, row = slot / PER_ROW, place = slot % PER_ROW, chunk = place ^ turn(row);
+            within[i] = chunk * CHUNK;
+            at[i] = row_of(min(first + row, o.extent - 1)) * row_bytes + chunk * 16;
         }
     }
     // plane + first entry, as bytes: where the tile's entry 0 at summed index k lies
@@ -234,8 +252,9 @@ struct Product {
 
     // Sum over summed indices [k_from, k_to), a multiple of DEEP, of P[p0 ..][k] Q[q0 ..][k].  Operands of two planes x = hi + 2^-11 lo (scaled, see
     // split_f32) take three passes, lo hi + hi lo first, then times 2^-11, then hi hi; lo lo lies below binary32.
+    template <class Rows = InOrder>
     __device__ __forceinline__ void run(const Operand& P, const Operand& Q, uint32_t p0, uint32_t q0, uint32_t k_from,
-                                        uint32_t k_to, char* lds) {
+                                        uint32_t k_to, char* lds, const Rows& row_of = Rows{}) {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
         for (int a = 0; a < FP; ++a)
@@ -245,7 +264,8 @@ struct Product {
         TP tp;
         TQ tq;
         tp.init(P, p0, wave, lane);
-        tq.init(Q, q0, wave, lane);
+        if constexpr (Rows::ANYWHERE) tq.init_anywhere(Q, q0, wave, lane, row_of);
+        else tq.init(Q, q0, wave, lane);
         const uint32_t steps = (k_to - k_from) / DEEP, passes = P.lo ? 3 : 1, total = steps * passes;
         const uint32_t pw = p_of(wave), qw = q_of(wave);
         const size_t p_step = (P_COLUMNS ? (size_t)P.ld * DEEP : DEEP) * E::SIZE, q_step = (Q_COLUMNS ? (size_t)Q.ld * DEEP : DEEP) * E::SIZE;
@@ -256,7 +276,7 @@ struct Product {
         // load i of the tile `step` of `pass`, into a stage; advance() goes on to the next tile
         auto origin = [&]() {
             pf = TP::origin(passes == 3 && pass == 0 ? P.lo : P.hi, P, p0, k_from);
-            qf = TQ::origin(passes == 3 && pass == 1 ? Q.lo : Q.hi, Q, q0, k_from);
+            qf = TQ::origin(passes == 3 && pass == 1 ? Q.lo : Q.hi, Q, Rows::ANYWHERE ? 0 : q0, k_from);
         };
         auto load = [&](int i, uint32_t stage) {
             const uint32_t k = k_from + step * DEEP, to = lds_at + stage * STAGE;
