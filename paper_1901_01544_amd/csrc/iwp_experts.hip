@@ -153,9 +153,9 @@ Spread spread(uint32_t units) {
     return s;
 }
 
-struct KindF32 { typedef F32 E; static constexpr int OUT = OUT_F32; };
-struct KindBf16 { typedef Bf16 E; static constexpr int OUT = OUT_BF16; };
-struct KindF16 { typedef F16 E; static constexpr int OUT = OUT_F16; };
+struct KindF32 { typedef F32 E; typedef FewF32 FEW_E; static constexpr int OUT = OUT_F32; };
+struct KindBf16 { typedef Bf16 E; typedef FewBf16 FEW_E; static constexpr int OUT = OUT_BF16; };
+struct KindF16 { typedef F16 E; typedef FewF16 FEW_E; static constexpr int OUT = OUT_F16; };
 
 template <class F>
 int with_kind(uint32_t dtype, F f) {
@@ -222,6 +222,14 @@ bool launches_fit(const ProductSizes& z, const ProductPlan& p) {
         typedef decltype(tile) T;
         return (int)(z.experts * tiles_of<T>(z.in, z.out) * T::THREADS <= MOST_THREADS);
     });
+}
+
+// Products of few rows an expert need no arrangement.  us here and by tiles, mean rows of an expert that has any: bf16 1 token x 8 of 64 experts x 2048 x 1024
+// 10 and 33, 16 tokens 42 and 53 (2 rows), 32 x 4 of 16 x 2048 x 2048 34 and 42 (8), 64 x 4 of 16 50 and 42 (16); binary32 60 x 2 of 8 x 1024 x 1024
+// 16 and 29 (15).
+bool few_rows(const ProductSizes& z) {
+    const uint32_t n = z.rows();
+    return n <= FEW_SLOTS && n <= (z.dtype == IWP_F32 ? FEW_ROWS : FEW_ROWS / 2) * std::min(z.experts, n);
 }
 
 // Can a product read these rows where they lie?  By 16 bytes, whole tiles of the summed index, within what 32 bits count.
@@ -329,6 +337,15 @@ int iwp_expert_product(const void* x, int64_t ld_x, uint32_t x_by_slot, const vo
     return with_kind(dtype, [&](auto kind) {
         typedef decltype(kind) K;
         constexpr int SIZE = K::E::SIZE;
+        if (few_rows(z)) {
+            const bool by_slot = z.rows() <= experts;
+            const uint32_t blocks = (out + FEW_ROWS - 1) / FEW_ROWS * (by_slot ? z.rows() : experts + 1);
+            IWP_LAUNCH_BLOCK("k_expert_few", (k_expert_few<typename K::FEW_E, K::OUT>), blocks, 256, s,
+                             (Matrices{static_cast<const char*>(w), step_w, (uint32_t)ld_w, out, in}),
+                             (Packed{static_cast<const char*>(x), (uint32_t)ld_x, in, z.by_slot ? 1 : slots}), chosen, z.rows(), experts, by_slot,
+                             (RowsOut{static_cast<char*>(y), ld_y}));
+            return (int)IWP_OK;
+        }
         Matrices W;
         Packed X{p.x, p.ld_x, in, 0};
         int rc = arrange(z, p, chosen, s);

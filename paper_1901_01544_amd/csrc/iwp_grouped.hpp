@@ -325,6 +325,102 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_expert_rows(Matrices W, Packed
     });
 }
 
+// Products of few rows, in one launch, without arranging anything: a workgroup has 16 rows of an expert's matrix, each of its wavefronts a
+// quarter of their width; it finds the expert's slots by itself and takes 16 of them at a time, so a matrix is read once as long as its
+// expert has no more.  Loads go straight to registers, whatever rows' alignment, eight steps of 16 rows by 64 bytes on their way.
+struct FewF32 {
+    static constexpr int SIZE = 4;
+    static __device__ __forceinline__ f32x4 mfma(words4 a, words4 b, f32x4 c) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[k]), __uint_as_float(b[k]), c, 0, 0, 0);
+        return c;
+    }
+};
+struct FewBf16 {
+    static constexpr int SIZE = 2;
+    static __device__ __forceinline__ f32x4 mfma(words4 a, words4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+struct FewF16 {
+    static constexpr int SIZE = 2;
+    static __device__ __forceinline__ f32x4 mfma(words4 a, words4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+};
+
+// 16 bytes of a row from element c on: zeros past its width
+template <int SIZE>
+__device__ __forceinline__ words4 row_chunk(const char* row, uint32_t c, uint32_t dim) {
+    constexpr uint32_t CHUNK = 16 / SIZE;
+    const char* p = row + (size_t)c * SIZE;
+    if (c + CHUNK <= dim) return SIZE == 4 ? *reinterpret_cast<const words4*>(p) : (words4)*reinterpret_cast<const words4_any*>(p);
+    words4 v = {};
+#pragma unroll
+    for (uint32_t e = 0; e < CHUNK; ++e)
+        if (c + e < dim) {
+            if (SIZE == 4) v[e % 4] = reinterpret_cast<const uint32_t*>(p)[e];
+            else v[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[e] << (e % 2 * 16);
+        }
+    return v;
+}
+
+constexpr uint32_t FEW_SLOTS = 1024, FEW_ROWS = 16;
+// by_slot: a workgroup for every slot and 16 rows, of which the first slot of an expert does them all; else one for every expert, and one for nobody.
+template <class E, int OUT>
+__global__ void __launch_bounds__(256) k_expert_few(Matrices W, Packed X, const int32_t* __restrict__ chosen, uint32_t n, uint32_t experts, bool by_slot,
+                                                    RowsOut Y) {
+    constexpr uint32_t CHUNK = 16 / E::SIZE, STEP = 4 * CHUNK;
+    __shared__ uint32_t list[FEW_SLOTS], found;
+    __shared__ float sums[4][FEW_ROWS][FEW_ROWS + 1];
+    const uint32_t np = (W.rows + FEW_ROWS - 1) / FEW_ROWS, p0 = blockIdx.x % np * FEW_ROWS, which = blockIdx.x / np;
+    const uint32_t thread = threadIdx.x, lane = thread & 63, wave = thread >> 6;
+    const uint32_t expert = by_slot ? bucket_of(chosen, which, experts) : which;
+    if (thread == 0) found = 0;
+    __syncthreads();
+    bool earlier = false;
+    for (uint32_t i = thread; i < n; i += 256) {
+        if (bucket_of(chosen, i, experts) != expert || (by_slot && expert == experts && i != which)) continue;
+        earlier |= i < which;
+        list[atomicAdd(&found, 1u)] = i;
+    }
+    if (__syncthreads_or(by_slot && earlier)) return;
+    const uint32_t count = found;
+    if (expert == experts) {
+        for (uint32_t i = thread; i < count * FEW_ROWS; i += 256)
+            if (p0 + i % FEW_ROWS < W.rows) put<OUT>(Y.y, (int64_t)list[i / FEW_ROWS] * Y.ld + p0 + i % FEW_ROWS, 0.0f);
+        return;
+    }
+    const uint32_t steps = (W.columns + STEP - 1) / STEP, each = (steps + 3) / 4, from = min(wave * each, steps), to = min(from + each, steps);
+    const uint32_t whole = min(to, max(from, W.columns / STEP));
+    const char* w = W.w + (expert * W.step + (int64_t)min(p0 + (lane & 15), W.rows - 1) * W.ld) * E::SIZE;
+    const uint32_t c0 = (lane >> 4) * CHUNK;
+    for (uint32_t r0 = 0; r0 < count; r0 += FEW_ROWS) {
+        const uint32_t slot = list[min(r0 + (lane & 15), count - 1)];
+        const char* x = X.x + (int64_t)(X.slots == 1 ? slot : slot / X.slots) * X.ld * E::SIZE;
+        f32x4 acc = {};
+        constexpr uint32_t AHEAD = 8;
+        uint32_t s = from;
+        for (; s + AHEAD <= whole; s += AHEAD) {
+            words4 a[AHEAD], b[AHEAD];
+#pragma unroll
+            for (uint32_t k = 0; k < AHEAD; ++k) a[k] = row_chunk<E::SIZE>(w, (s + k) * STEP + c0, ~0u);
+#pragma unroll
+            for (uint32_t k = 0; k < AHEAD; ++k) b[k] = row_chunk<E::SIZE>(x, (s + k) * STEP + c0, ~0u);
+#pragma unroll
+            for (uint32_t k = 0; k < AHEAD; ++k) acc = E::mfma(a[k], b[k], acc);
+        }
+        for (; s < to; ++s) acc = E::mfma(row_chunk<E::SIZE>(w, s * STEP + c0, W.columns), row_chunk<E::SIZE>(x, s * STEP + c0, W.columns), acc);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sums[wave][(lane >> 4) * 4 + j][lane & 15] = acc[j];
+        __syncthreads();
+        const uint32_t p = thread & 15, q = thread >> 4;
+        if (p0 + p < W.rows && r0 + q < count)
+            put<OUT>(Y.y, (int64_t)list[r0 + q] * Y.ld + p0 + p, (sums[0][p][q] + sums[1][p][q]) + (sums[2][p][q] + sums[3][p][q]));
+        __syncthreads();
+    }
+}
+
 // Every expert's matrix's gradient: the sum over its rows of dy x^T.
 template <class E, int BP, int BQ, int WP, int WQ, int OUT>
 __global__ void __launch_bounds__(WP * WQ * 64) k_expert_dw(Packed X, Packed D, ExpertRows R, char* __restrict__ dw, int64_t ld, int64_t step) {
