@@ -151,3 +151,18 @@ def test_same_bytes_on_another_stream_and_in_a_graph(clipping, rows):
         assert torch.equal(first[1], second[1]) and torch.equal(first[1], norm)
         for a, b, c in zip(first[0], second[0], out):
             assert torch.equal(a[:n], b[:n]) and torch.equal(a[:n], c[:n])
+
+
+def test_workers_beyond_the_cache(clipping):
+    """Gradients that are clipped a worker at a time; the last one as it is."""
+    rows = [(0, 20_000_001), (20_000_100, 25_000_003)]
+    g = gradients(rows, 3, seed=5)
+    g[2] *= 1e-3
+    before = [torch.zeros_like(x) for x in g]
+    out = [x.clone() for x in before]
+    norm = call(clipping, rows, g, out, max_norm=100.0)
+    check(rows, g, out, before, norm, 100.0)
+    assert torch.equal(call(clipping, rows, g, None, max_norm=100.0), norm) or (norm - call(clipping, rows, g, None)).abs().max() <= HALF * norm.max()
+    onto = [x.clone() for x in g]
+    call(clipping, rows, onto, onto, max_norm=100.0)
+    check(rows, g, onto, g, norm, 100.0)
