@@ -421,13 +421,15 @@ __global__ void __launch_bounds__(256) k_expert_few(Matrices W, Packed X, const 
     }
 }
 
-// Every expert's matrix's gradient: the sum over its rows of dy x^T.
+// Every expert's matrix's gradient: the sum over its rows of dy x^T.  Experts have more and fewer rows, so the dies take neighbouring tiles in turn: with
+// a stretch of the experts each, the die with the liked ones is the last (8 experts of 2048 x 4096, 16384 rows: 411 us instead of 275; 64 of 2048 x 1024,
+// 65536 rows: 458 and 400).
 template <class E, int BP, int BQ, int WP, int WQ, int OUT>
 __global__ void __launch_bounds__(WP * WQ * 64) k_expert_dw(Packed X, Packed D, ExpertRows R, char* __restrict__ dw, int64_t ld, int64_t step) {
     typedef Product<E, BP, BQ, WP, WQ, true, true> M;
     __shared__ __align__(1024) char lds[M::LDS];
     const uint32_t np = (X.dim + BP - 1) / BP, nq = (D.dim + BQ - 1) / BQ;
-    const uint32_t at = stretch_place(blockIdx.x, gridDim.x), expert = at / (np * nq), of = at - expert * np * nq;
+    const uint32_t expert = blockIdx.x / (np * nq), of = blockIdx.x - expert * np * nq;
     constexpr uint32_t TALL = 8;
     const uint32_t group = of / (np * TALL), rest = of - group * np * TALL, tall = min(TALL, nq - group * TALL);
     const uint32_t tp = rest / tall, tq = group * TALL + rest % tall;
