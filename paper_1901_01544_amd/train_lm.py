@@ -1,11 +1,14 @@
 """A small language model with routed experts, trained by several emulated workers whose gradients go through the compression step.
 
     python -m paper_1901_01544_amd.train_lm --steps 60
+    python -m paper_1901_01544_amd.train_lm --steps 60 --scores sigmoid --width 64 --clip 1.0
 
 Every worker runs the model on its own tokens; the losses' kernels (``losses.head_distill``, ``losses.head_cross_entropy``,
 ``losses.balance``) give the loss and the gradients of the hidden states, of the router's logits and, written straight into the
 worker's flat gradient buffer, of the head; torch's autograd takes the former two through the model's body.  Then
-``iwp.step_segmented`` accumulates, selects, exchanges and updates.  The text is synthetic: a token's successor is a fixed one
+``iwp.step_segmented`` accumulates, selects, exchanges and updates.  With ``width`` the experts are matrices, up to that width and back, instead
+of scales: ``experts.route`` chooses them, by softmax or sigmoid scores, ``experts.product`` takes the tokens through them, and their gradients go
+straight into the flat buffer too.  With ``clip`` the workers' gradients are clipped to that norm (``clipping.clip``).  The text is synthetic: a token's successor is a fixed one
 four times out of five, and a teacher knows it.
 """
 from __future__ import annotations
@@ -14,15 +17,19 @@ import argparse
 
 import torch
 
-from paper_1901_01544_amd import iwp, losses
+from paper_1901_01544_amd import clipping, experts as layer, iwp, losses
 
 
 class Model:
-    """Weights in one flat buffer, the layout that the compression step takes: embedding, router, experts' scales, head."""
+    """Weights in one flat buffer, the layout that the compression step takes: embedding, router, experts' scales, head; with a width, the
+    experts' matrices up and down in place of the scales, one below the other."""
 
-    def __init__(self, vocab: int, dim: int, experts: int, keep: float, device, seed: int):
+    def __init__(self, vocab: int, dim: int, experts: int, keep: float, device, seed: int, width: int = 0):
         gen = torch.Generator().manual_seed(seed)
-        self.shapes = [(vocab, dim), (experts, dim), (experts, dim), (vocab, dim)]
+        middle = [(experts * width, dim), (experts * dim, width)] if width else [(experts, dim)]
+        scales = [1.0, 0.3] + ([dim ** -0.5, width ** -0.5] if width else [0.1]) + [0.1]
+        self.shapes = [(vocab, dim), (experts, dim), *middle, (vocab, dim)]
+        self.experts = experts
         self.rows, off, out = [], 0, 0
         for rows, columns in self.shapes:
             n = rows * columns
@@ -31,7 +38,7 @@ class Model:
             off, out = (off + n + 63) // 64 * 64, out + k
         self.flat, self.pairs = off, out
         weights = torch.zeros(self.flat)
-        for (start, n, _, _), scale in zip(self.rows, (1.0, 0.3, 0.1, 0.1)):
+        for (start, n, _, _), scale in zip(self.rows, scales):
             weights[start:start + n] = scale * torch.randn(n, generator=gen)
         self.weights = weights.to(device)
 
@@ -46,6 +53,57 @@ def body(embedding, router, scales, tokens, slots: int):
     chosen = logits.detach().topk(slots, dim=1).indices
     gates = torch.softmax(logits, 1).gather(1, chosen)
     return x * (1.0 + (gates[:, :, None] * scales[chosen]).sum(1)), logits, chosen.to(torch.int32)
+
+
+class Route(torch.autograd.Function):
+    """Experts and their weights; the gradient of the logits from the weights'."""
+
+    @staticmethod
+    def forward(ctx, logits, slots: int, scores: str, keep):
+        chosen = torch.empty(logits.shape[0], slots, dtype=torch.int32, device=logits.device)
+        weight = torch.empty(logits.shape[0], slots, device=logits.device)
+        layer.route(logits, chosen, weight, scores=scores, renormalise=True, keep=keep)
+        ctx.save_for_backward(logits, chosen, keep)
+        ctx.scores = scores
+        ctx.mark_non_differentiable(chosen)
+        return chosen, weight
+
+    @staticmethod
+    def backward(ctx, _, dweight):
+        logits, chosen, keep = ctx.saved_tensors
+        dx = torch.empty_like(logits)
+        layer.route_gradient(logits, chosen, dweight.contiguous(), dx, scores=ctx.scores, renormalise=True, keep=keep)
+        return dx, None, None, None
+
+
+class Product(torch.autograd.Function):
+    """Rows through the experts' matrices w, whose gradient is written into ``into``."""
+
+    @staticmethod
+    def forward(ctx, x, w, chosen, into):
+        y = torch.empty(*chosen.shape, w.shape[1], device=x.device)
+        workspace = torch.empty(layer.product_workspace_bytes(x, w, chosen), dtype=torch.uint8, device=x.device)
+        layer.product(x, w, chosen, y, workspace)
+        ctx.save_for_backward(x, w, chosen)
+        ctx.into = into
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, w, chosen = ctx.saved_tensors
+        dx = torch.empty_like(x)
+        workspace = torch.empty(layer.product_workspace_bytes(x, w, chosen, gradient=True), dtype=torch.uint8, device=x.device)
+        layer.product_gradient(x, w, chosen, dy.contiguous(), dx, ctx.into, workspace)
+        return dx, None, None, None
+
+
+def routed_body(embedding, router, up, down, into_up, into_down, tokens, slots: int, scores: str, keep):
+    """Hidden states, the router's logits and its choice, with matrices for experts; up, down and their gradients: [experts, ...]."""
+    x = embedding[tokens]
+    logits = x @ router.t()
+    chosen, weight = Route.apply(logits, slots, scores, keep)
+    y = Product.apply(torch.nn.functional.silu(Product.apply(x, up, chosen, into_up)), down, chosen, into_down)
+    return x + (weight[:, :, None] * y).sum(1), logits, chosen
 
 
 class Text:
@@ -68,10 +126,47 @@ class Text:
         return now, target.to(torch.int32), index.to(torch.int32), logit
 
 
+class Worker:
+    """What a worker's pass takes besides the model: outputs and workspaces of the losses."""
+
+    def __init__(self, model: Model, tokens: int, dim: int, top: int, slots: int, scores: str, device):
+        self.model, self.slots, self.scores, self.counted = model, slots, scores, tokens - tokens // 8
+        head = model.views(model.weights)[-1]
+        self.loss, self.dh = torch.empty(tokens, device=device), torch.empty(tokens, dim, device=device)
+        self.balance, self.counts = torch.empty(2, device=device), torch.empty(model.experts, dtype=torch.int32, device=device)
+        self.dlogits = torch.empty(tokens, model.experts, device=device)
+        self.head_workspace = torch.empty(losses.head_workspace_bytes(self.dh, head, top=top), dtype=torch.uint8, device=device)
+        self.balance_workspace = torch.empty(losses.balance_workspace_bytes(tokens, model.experts), dtype=torch.uint8, device=device)
+
+    def gradient(self, batch, into, taught: bool) -> None:
+        """The gradient of every weight into the flat buffer whose views are ``into``; the tokens' losses."""
+        now, target, index, logit = batch
+        weights = self.model.views(self.model.weights)
+        through = 2 if len(weights) == 5 else 3                       # tensors whose gradients come from autograd
+        leaves = [x.detach().requires_grad_() for x in weights[:through]]
+        keep_mask = (target >= 0).to(torch.uint8)
+        if len(weights) == 5:
+            matrices = [x.unflatten(0, (self.model.experts, -1)) for x in weights[2:4] + into[2:4]]
+            hidden, logits, chosen = routed_body(*leaves, *matrices, now, self.slots, self.scores, keep_mask)
+        else:
+            hidden, logits, chosen = body(*leaves, now, self.slots)
+        h, x, scale = hidden.detach(), logits.detach(), 1.0 / self.counted
+        if taught:
+            losses.head_distill(h, weights[-1], index, logit, self.loss, self.dh, into[-1], self.head_workspace, temperature=2.0, soft=0.5, target=target,
+                                hard=0.5, scale=scale)
+        else:
+            losses.head_cross_entropy(h, weights[-1], target, self.loss, self.dh, into[-1], self.head_workspace, scale=scale)
+        losses.balance(x, chosen, self.balance, self.counts, self.dlogits, self.balance_workspace, balance=0.01, z=0.001, keep=keep_mask)
+        for to, g in zip(into[:through], torch.autograd.grad([hidden, logits], leaves, [self.dh, self.dlogits])):
+            to.copy_(g)
+
+
 def train(steps: int = 60, workers: int = 4, tokens: int = 200, vocab: int = 300, dim: int = 48, experts: int = 8, slots: int = 2,
-          top: int = 8, keep: float = 1 / 8, rate: float = 8.0, device="cuda:0", seed: int = 0, report=None):
-    """Mean loss per counted token of every step, and the experts' counts of the last one."""
-    model, text = Model(vocab, dim, experts, keep, device, seed), Text(vocab, top, seed + 1)
+          top: int = 8, keep: float = 1 / 8, rate: float = 8.0, device="cuda:0", seed: int = 0, report=None, width: int = 0,
+          scores: str = "softmax", clip: float = 0.0):
+    """Mean loss per counted token of every step, and the experts' counts of the last one.  width: of the experts' matrices, 0 for scales;
+    scores: by which experts are chosen then; clip: largest norm of a worker's gradient, 0 for none."""
+    model, text = Model(vocab, dim, experts, keep, device, seed, width), Text(vocab, top, seed + 1)
     plan = iwp.Plan(model.rows)
     gradients = [torch.zeros(model.flat, device=device) for _ in range(workers)]
     residuals = [torch.zeros(model.flat, device=device) for _ in range(workers)]
@@ -79,47 +174,36 @@ def train(steps: int = 60, workers: int = 4, tokens: int = 200, vocab: int = 300
     value_out, sum_out = torch.empty(model.pairs, device=device), torch.empty(model.pairs, device=device)
     thresholds = [torch.zeros(3 * len(model.rows), dtype=torch.int32, device=device) for _ in range(2)]
     step_workspace = torch.empty(max(1, plan.step_workspace_bytes(workers)), dtype=torch.uint8, device=device)
-    head = model.views(model.weights)[3]
-    loss, dh = torch.empty(tokens, device=device), torch.empty(tokens, dim, device=device)
-    balance, counts = torch.empty(2, device=device), torch.empty(experts, dtype=torch.int32, device=device)
-    dlogits = torch.empty(tokens, experts, device=device)
-    head_workspace = torch.empty(losses.head_workspace_bytes(dh, head, top=top), dtype=torch.uint8, device=device)
-    balance_workspace = torch.empty(losses.balance_workspace_bytes(tokens, experts), dtype=torch.uint8, device=device)
+    worker = Worker(model, tokens, dim, top, slots, scores, device)
+    if clip:
+        tensors, norm = clipping.Tensors(model.rows), torch.empty(workers, device=device)
+        clip_workspace = torch.empty(tensors.workspace_bytes(workers), dtype=torch.uint8, device=device)
     history = []
     for t in range(steps):
         total = 0.0
-        for p in range(workers):
-            now, target, index, logit = (x.to(device) for x in text.batch(tokens))
-            counted = tokens - tokens // 8
-            weights, into = model.views(model.weights), model.views(gradients[p])
-            leaves = [x.detach().requires_grad_() for x in weights[:3]]
-            hidden, logits, chosen = body(*leaves, now, slots)
-            h, x = hidden.detach(), logits.detach()
-            if p % 2 == 0:                                            # half of the workers have a teacher
-                losses.head_distill(h, weights[3], index, logit, loss, dh, into[3], head_workspace, temperature=2.0, soft=0.5, target=target,
-                                    hard=0.5, scale=1.0 / counted)
-            else:
-                losses.head_cross_entropy(h, weights[3], target, loss, dh, into[3], head_workspace, scale=1.0 / counted)
-            keep_mask = (target >= 0).to(torch.uint8)
-            losses.balance(x, chosen, balance, counts, dlogits, balance_workspace, balance=0.01, z=0.001, keep=keep_mask)
-            for to, g in zip(into[:3], torch.autograd.grad([hidden, logits], leaves, [dh, dlogits])):
-                to.copy_(g)
-            total += loss.sum().item() / counted
+        for p in range(workers):                                      # half of the workers have a teacher
+            worker.gradient([x.to(device) for x in text.batch(tokens)], model.views(gradients[p]), taught=p % 2 == 0)
+            total += worker.loss.sum().item() / worker.counted
+        if clip:
+            clipping.clip(tensors, gradients, gradients, norm, clip_workspace, max_norm=clip)
         leader = torch.tensor([(t + j) % workers for j in range(len(model.rows))], dtype=torch.int32, device=device)
         iwp.step_segmented(plan, model.weights, gradients, residuals, leader, 1e-8, -rate / workers, index_out, value_out, sum_out,
                            thresholds[t % 2], step_workspace, thr_hint=thresholds[(t + 1) % 2] if t else None)
         history.append(total / workers)
         if report:
-            report(t, history[-1], counts)
-    return history, counts.cpu()
+            report(t, history[-1], worker.counts)
+    return history, worker.counts.cpu()
 
 
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--steps", type=int, default=60)
     ap.add_argument("--workers", type=int, default=4)
+    ap.add_argument("--width", type=int, default=0, help="experts are matrices up to this width and back (0: scales)")
+    ap.add_argument("--scores", choices=["softmax", "sigmoid"], default="softmax", help="by which experts with matrices are chosen")
+    ap.add_argument("--clip", type=float, default=0.0, help="largest norm of a worker's gradient (0: as it is)")
     a = ap.parse_args()
-    train(a.steps, a.workers, report=lambda t, loss, counts: t % 10 == 0 and print("step %3d  loss %.4f  experts %s" % (t, loss, counts.tolist()), flush=True))
+    train(a.steps, a.workers, width=a.width, scores=a.scores, clip=a.clip, report=lambda t, loss, counts: t % 10 == 0 and print("step %3d  loss %.4f  experts %s" % (t, loss, counts.tolist()), flush=True))
 
 
 if __name__ == "__main__":
