@@ -11,6 +11,8 @@ from __future__ import annotations
 import ctypes as C
 from typing import Optional, Sequence
 
+import torch
+
 from . import iwp
 
 
@@ -45,10 +47,10 @@ class Tensors:
             pass
 
 
-def _flat(t, what: str, end: int):
-    import torch
-    if t is not None and (t.dtype != torch.float32 or t.dim() != 1 or t.numel() < end):
-        raise ValueError("%s: flat float32 buffers of at least %d elements are wanted, not %s of %s" % (what, end, t.dtype, tuple(t.shape)))
+def _flat(buffers, what: str, end: int):
+    for t in buffers:
+        if t is not None and (t.dtype is not torch.float32 or len(t.shape) != 1 or len(t) < end):
+            raise ValueError("%s: flat float32 buffers of at least %d elements are wanted, not %s of %s" % (what, end, t.dtype, tuple(t.shape)))
 
 
 def clip(tensors: Tensors, g: Sequence, out: Optional[Sequence], norm, workspace, max_norm: float = float("inf"), scale: float = 1.0,
@@ -57,15 +59,13 @@ def clip(tensors: Tensors, g: Sequence, out: Optional[Sequence], norm, workspace
 
     g: one flat buffer a worker, None for a worker without a gradient.  out: likewise, out[p] may be g[p]; None: norms alone.  norm: [W].
     workspace: ``tensors.workspace_bytes(W)`` bytes."""
-    import torch
     W = len(g)
     out = [None] * W if out is None else out
     if len(out) != W:
         raise ValueError("out: %d buffers are wanted, not %d" % (W, len(out)))
-    if norm.dtype != torch.float32 or tuple(norm.shape) != (W,):
+    if norm.dtype != torch.float32 or norm.shape != (W,):
         raise ValueError("norm: float32 of shape %s is wanted, not %s of %s" % ((W,), norm.dtype, tuple(norm.shape)))
-    for a, b in zip(g, out):
-        _flat(a, "g", tensors.end)
-        _flat(b, "out", tensors.end)
+    _flat(g, "g", tensors.end)
+    _flat(out, "out", tensors.end)
     iwp._check(iwp._hot().iwp_clip(tensors._address, g, out, W, scale, max_norm, norm, workspace, iwp._bytes(workspace), iwp._stream(stream)),
                "clip")

@@ -30,21 +30,22 @@ def _dtype(t, what: str) -> int:
 
 def _matrix(t, what: str, rows: int, columns: int, dtype=None):
     """(address, elements from row to row) of a device matrix whose rows lie together."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != columns:
+    if t.shape != (rows, columns):
         raise ValueError("%s: a matrix of %d x %d is wanted, not %s" % (what, rows, columns, tuple(t.shape)))
     if dtype is not None and t.dtype != dtype:
         raise ValueError("%s: %s is wanted, not %s" % (what, dtype, t.dtype))
     if not t.is_cuda:
         raise ValueError("%s: a device tensor is wanted" % what)
-    if t.stride(1) != 1 and columns > 1:
+    ld, step = t.stride()
+    if step != 1 and columns > 1:
         raise ValueError("%s: the elements of a row have to lie together" % what)
-    return t.data_ptr(), max(t.stride(0), columns) if rows <= 1 else t.stride(0)
+    return t.data_ptr(), max(ld, columns) if rows <= 1 else ld
 
 
 def _packed(t, what: str, shape, dtype) -> Optional[int]:
     if t is None:
         return None
-    if tuple(t.shape) != shape or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError("%s: %s of shape %s is wanted, not %s of %s" % (what, dtype, shape, t.dtype, tuple(t.shape)))
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError("%s: a contiguous device tensor is wanted" % what)
