@@ -47,9 +47,12 @@ class Tensors:
             pass
 
 
+_F32 = torch.float32
+
+
 def _flat(buffers, what: str, end: int):
     for t in buffers:
-        if t is not None and (t.dtype is not torch.float32 or len(t.shape) != 1 or len(t) < end):
+        if t is not None and (t.dtype is not _F32 or t.numel() < end):
             raise ValueError("%s: flat float32 buffers of at least %d elements are wanted, not %s of %s" % (what, end, t.dtype, tuple(t.shape)))
 
 
@@ -63,9 +66,10 @@ def clip(tensors: Tensors, g: Sequence, out: Optional[Sequence], norm, workspace
     out = [None] * W if out is None else out
     if len(out) != W:
         raise ValueError("out: %d buffers are wanted, not %d" % (W, len(out)))
-    if norm.dtype != torch.float32 or norm.shape != (W,):
+    if norm.dtype is not _F32 or norm.shape != (W,):
         raise ValueError("norm: float32 of shape %s is wanted, not %s of %s" % ((W,), norm.dtype, tuple(norm.shape)))
     _flat(g, "g", tensors.end)
-    _flat(out, "out", tensors.end)
+    if out is not g:
+        _flat(out, "out", tensors.end)
     iwp._check(iwp._hot().iwp_clip(tensors._address, g, out, W, scale, max_norm, norm, workspace, iwp._bytes(workspace), iwp._stream(stream)),
                "clip")

@@ -64,6 +64,13 @@ int with_tile(TileKind kind, F f) {
     }
 }
 
+// Of a kind of operands: binary32 takes the small tiles alone.
+template <class K, class F>
+int with_tile_of(TileKind kind, F f) {
+    if constexpr (K::OUT == OUT_F32) return f(Few{});
+    else return with_tile(kind, f);
+}
+
 template <class T>
 uint64_t tiles_of(uint64_t np, uint64_t nq) { return (np + T::BP - 1) / T::BP * ((nq + T::BQ - 1) / T::BQ); }
 
@@ -99,7 +106,7 @@ struct ProductSizes {
 
 struct ProductPlan {
     uint32_t deep, ld_x, ld_d;             // elements in 128 bytes; widths rounded up to that
-    TileKind rows_tile, dw_tile;
+    TileKind tile;
     uint32_t height, max_tiles;
     uint32_t arrangers, per_wave;          // workgroups that arrange the slots, slots of a wavefront
     ExpertRows R;
@@ -122,9 +129,8 @@ ProductPlan product_plan(const ProductSizes& z, bool copy_w, void* workspace) {
     p.ld_x = round_up(z.in, p.deep);
     p.ld_d = round_up(z.out, p.deep);
     const uint32_t n = z.rows(), many = std::max(1u, std::min(z.experts, n)), each = (n + many - 1) / many;
-    p.rows_tile = tile_for(z.gradient ? z.in : z.out, each, many, z.dtype);
-    p.dw_tile = tile_for(z.in, z.out, z.experts, z.dtype);
-    p.height = p.rows_tile == BIG ? Big::BQ : p.rows_tile == MID ? Mid::BQ : Few::BQ;
+    p.tile = tile_for(z.gradient ? z.in : z.out, each, many, z.dtype);
+    p.height = p.tile == BIG ? Big::BQ : p.tile == MID ? Mid::BQ : Few::BQ;
     p.max_tiles = n / p.height + many + 1;
     p.arrangers = std::max(1u, std::min((n + ARRANGE_SLOTS - 1) / ARRANGE_SLOTS, ARRANGE_MOST));
     p.per_wave = round_up((n + p.arrangers * ARRANGE_WAVES - 1) / (p.arrangers * ARRANGE_WAVES), 64u);
@@ -163,65 +169,41 @@ int with_kind(uint32_t dtype, F f) {
     return dtype == IWP_BF16 ? f(KindBf16{}) : f(KindF16{});
 }
 
-int arrange(const ProductSizes& z, const ProductPlan& p, const int32_t* chosen, hipStream_t s) {
+// Arranges the slots and, where the products cannot read the matrices where they lie, copies them.
+template <int SIZE>
+int arrange(const ProductSizes& z, const ProductPlan& p, const int32_t* chosen, const void* w, int64_t ld, int64_t step, bool wanted, Matrices* W, hipStream_t s) {
+    *W = Matrices{static_cast<const char*>(w), step, (uint32_t)ld, z.out, z.in};
+    MatrixCopy copy{static_cast<const char*>(w), ld, step, z.out, z.in, Units{1, 0}, p.w};
+    if (p.w && wanted) {
+        *W = Matrices{p.w, (int64_t)z.out * p.ld_x, p.ld_x, z.out, z.in};
+        copy.of = Units{p.ld_x * SIZE / 16, z.experts * z.out};
+    }
+    const uint32_t copiers = (uint32_t)((copy.of.threads() + ARRANGE_THREADS - 1) / ARRANGE_THREADS);
     if (p.arrangers > 1) IWP_LAUNCH_BLOCK("k_expert_count", k_expert_count, p.arrangers, ARRANGE_THREADS, s, chosen, z.rows(), p.per_wave, z.experts, p.R);
-    IWP_LAUNCH_BLOCK("k_expert_arrange", k_expert_arrange, p.arrangers, ARRANGE_THREADS, s, chosen, z.rows(), p.per_wave, z.experts, p.height, p.R);
+    IWP_LAUNCH_BLOCK("k_expert_arrange", k_expert_arrange<SIZE>, p.arrangers + copiers, ARRANGE_THREADS, s, chosen, z.rows(), p.per_wave, z.experts, p.height,
+                     p.arrangers, p.R, copy);
     return IWP_OK;
 }
 
+RowsGather gather_of(const ProductSizes& z, const void* x, int64_t ld, uint32_t dim, uint32_t slots, char* out, uint32_t ld_out) {
+    return RowsGather{static_cast<const char*>(x), ld, dim, slots, Units{(uint32_t)(ld_out * size_of(z.dtype) / 16), z.padded()}, out};
+}
 template <int SIZE>
-int gather(const ProductSizes& z, const ProductPlan& p, const void* x, int64_t ld, uint32_t dim, bool by_slot, char* out, uint32_t ld_out, hipStream_t s) {
-    const Spread sp = spread(ld_out * SIZE / 16);
-    return in_launches(z.padded(), sp.rows() * GATHER_ROWS, sp.across, 256, [&](uint32_t first, uint32_t blocks) {
-        IWP_LAUNCH_BLOCK("k_expert_gather", k_expert_gather<SIZE>, blocks, 256, s, x, ld, dim, z.slots, by_slot, z.experts, first, sp, p.R, out, ld_out);
-        return (int)IWP_OK;
-    });
-}
-
-// The matrices where the products read them: where they lie, or copied.
-template <int SIZE>
-int matrices(const ProductSizes& z, const ProductPlan& p, const void* w, int64_t ld, int64_t step, Matrices* W, hipStream_t s) {
-    *W = Matrices{static_cast<const char*>(w), step, (uint32_t)ld, z.out, z.in};
-    if (!p.w) return IWP_OK;
-    *W = Matrices{p.w, (int64_t)z.out * p.ld_x, p.ld_x, z.out, z.in};
-    const Spread sp = spread(p.ld_x * SIZE / 16);
-    return in_launches(z.experts * z.out, sp.rows() * GATHER_ROWS, sp.across, 256, [&](uint32_t first, uint32_t blocks) {
-        IWP_LAUNCH_BLOCK("k_expert_copy", k_expert_copy<SIZE>, blocks, 256, s, w, ld, step, z.out, z.in, z.experts, first, sp, p.R, p.w, p.ld_x);
-        return (int)IWP_OK;
-    });
-}
-
-template <class K, int OUT, bool TRANSPOSED>
-int rows_product(const ProductSizes& z, const ProductPlan& p, const Matrices& W, const Packed& X, const RowsOut& Y, hipStream_t s) {
-    return with_tile(p.rows_tile, [&](auto tile) {
-        typedef decltype(tile) T;
-        auto kernel = X.slots ? k_expert_rows<typename K::E, T::BP, T::BQ, T::WP, T::WQ, OUT, TRANSPOSED, false>
-                              : k_expert_rows<typename K::E, T::BP, T::BQ, T::WP, T::WQ, OUT, TRANSPOSED, true>;
-        const uint32_t np = ((TRANSPOSED ? z.in : z.out) + T::BP - 1) / T::BP;
-        IWP_LAUNCH_BLOCK("k_expert_rows", kernel, np * p.max_tiles, T::THREADS, s, W, X, p.R, z.experts, Y);
-        return (int)IWP_OK;
-    });
-}
-
-template <class K, int OUT>
-int dw_product(const ProductSizes& z, const ProductPlan& p, const Packed& X, const Packed& D, void* dw, int64_t ld, int64_t step, hipStream_t s) {
-    return with_tile(p.dw_tile, [&](auto tile) {
-        typedef decltype(tile) T;
-        auto kernel = k_expert_dw<typename K::E, T::BP, T::BQ, T::WP, T::WQ, OUT>;
-        IWP_LAUNCH_BLOCK("k_expert_dw", kernel, (uint32_t)(z.experts * tiles_of<T>(z.in, z.out)), T::THREADS, s, X, D, p.R, static_cast<char*>(dw), ld, step);
-        return (int)IWP_OK;
-    });
+int gather(const ProductSizes& z, const ProductPlan& p, const RowsGather& A, const RowsGather& B, hipStream_t s) {
+    const uint32_t a = (uint32_t)((A.of.threads() + 255) / 256), b = (uint32_t)((B.of.threads() + 255) / 256);
+    if (a + b) IWP_LAUNCH_BLOCK("k_expert_gather", k_expert_gather<SIZE>, a + b, 256, s, A, B, a, z.experts, p.R);
+    return IWP_OK;
 }
 
 // HIP counts a launch's threads in 32 bits.  More rows by columns than this allows fit no memory.
 bool launches_fit(const ProductSizes& z, const ProductPlan& p) {
-    return with_tile(p.rows_tile, [&](auto tile) {
-        typedef decltype(tile) T;
-        return (int)((uint64_t)(std::max(z.in, z.out) + T::BP - 1) / T::BP * p.max_tiles * T::THREADS <= MOST_THREADS);
-    }) && with_tile(p.dw_tile, [&](auto tile) {
-        typedef decltype(tile) T;
-        return (int)(z.experts * tiles_of<T>(z.in, z.out) * T::THREADS <= MOST_THREADS);
-    });
+    const uint64_t widest = round_up(std::max(z.in, z.out), 64u), units = widest * size_of(z.dtype) / 16;
+    return 2 * units * (z.padded() / GATHER_ROWS + 1) <= MOST_THREADS && units * z.experts * z.out / GATHER_ROWS + (ARRANGE_MOST + 2) * ARRANGE_THREADS <= MOST_THREADS &&
+           with_tile(p.tile, [&](auto tile) {
+               typedef decltype(tile) T;
+               const uint64_t rows = (widest + T::BP - 1) / T::BP * p.max_tiles, matrices = z.gradient ? z.experts * tiles_of<T>(z.in, z.out) : 0;
+               return (int)((rows + matrices + 16) * T::THREADS <= MOST_THREADS);
+           });
 }
 
 // Products of few rows an expert need no arrangement.  us here and by tiles, mean rows of an expert that has any: bf16 1 token x 8 of 64 experts x 2048 x 1024
@@ -337,23 +319,28 @@ int iwp_expert_product(const void* x, int64_t ld_x, uint32_t x_by_slot, const vo
     return with_kind(dtype, [&](auto kind) {
         typedef decltype(kind) K;
         constexpr int SIZE = K::E::SIZE;
+        const RowsOut Y{static_cast<char*>(y), ld_y};
         if (few_rows(z)) {
             const bool by_slot = z.rows() <= experts;
             const uint32_t blocks = (out + FEW_ROWS - 1) / FEW_ROWS * (by_slot ? z.rows() : experts + 1);
             IWP_LAUNCH_BLOCK("k_expert_few", (k_expert_few<typename K::FEW_E, K::OUT>), blocks, 256, s,
                              (Matrices{static_cast<const char*>(w), step_w, (uint32_t)ld_w, out, in}),
-                             (Packed{static_cast<const char*>(x), (uint32_t)ld_x, in, z.by_slot ? 1 : slots}), chosen, z.rows(), experts, by_slot,
-                             (RowsOut{static_cast<char*>(y), ld_y}));
+                             (Packed{static_cast<const char*>(x), (uint32_t)ld_x, in, z.by_slot ? 1 : slots}), chosen, z.rows(), experts, by_slot, Y);
             return (int)IWP_OK;
         }
         Matrices W;
         Packed X{p.x, p.ld_x, in, 0};
-        int rc = arrange(z, p, chosen, s);
+        int rc = arrange<SIZE>(z, p, chosen, w, ld_w, step_w, true, &W, s);
         if (in_place(x, ld_x, in, z.by_slot ? z.rows() : tokens, dtype)) X = Packed{static_cast<const char*>(x), (uint32_t)ld_x, in, z.by_slot ? 1 : slots};
-        else if (!rc) rc = gather<SIZE>(z, p, x, ld_x, in, z.by_slot, p.x, p.ld_x, s);
-        if (!rc) rc = matrices<SIZE>(z, p, w, ld_w, step_w, &W, s);
-        if (!rc) rc = rows_product<K, K::OUT, false>(z, p, W, X, RowsOut{static_cast<char*>(y), ld_y}, s);
-        return rc;
+        else if (!rc) rc = gather<SIZE>(z, p, gather_of(z, x, ld_x, in, z.by_slot ? 1 : slots, p.x, p.ld_x), RowsGather{}, s);
+        if (rc) return rc;
+        return with_tile_of<K>(p.tile, [&](auto tile) {
+            typedef decltype(tile) T;
+            auto kernel = X.slots ? k_expert_rows<typename K::E, T::BP, T::BQ, T::WP, T::WQ, K::OUT, false>
+                                  : k_expert_rows<typename K::E, T::BP, T::BQ, T::WP, T::WQ, K::OUT, true>;
+            IWP_LAUNCH_BLOCK("k_expert_rows", kernel, (out + T::BP - 1) / T::BP * p.max_tiles, T::THREADS, s, W, X, p.R, experts, Y);
+            return (int)IWP_OK;
+        });
     });
 }
 
@@ -379,31 +366,35 @@ int iwp_expert_product_gradient(const void* x, int64_t ld_x, uint32_t x_by_slot,
     return with_kind(dtype, [&](auto kind) {
         typedef decltype(kind) K;
         constexpr int SIZE = K::E::SIZE;
-        const Packed X{p.x, p.ld_x, in, 0};
-        Packed D{p.d, p.ld_d, out, 0};
-        int rc = arrange(z, p, chosen, s);
-        if (!rc && dw) rc = gather<SIZE>(z, p, x, ld_x, in, z.by_slot, p.x, p.ld_x, s);
-        // without the matrices' gradient, dy's rows may do where they lie
-        if (!dw && in_place(dy, ld_dy, out, z.rows(), dtype)) D = Packed{static_cast<const char*>(dy), (uint32_t)ld_dy, out, 1};
-        else if (!rc) rc = gather<SIZE>(z, p, dy, ld_dy, out, true, p.d, p.ld_d, s);
-        if (!rc && dx && tokens) {
-            Matrices W;
-            rc = matrices<SIZE>(z, p, w, ld_w, step_w, &W, s);
-            if (!rc && !p.sums) rc = rows_product<K, K::OUT, true>(z, p, W, D, RowsOut{static_cast<char*>(dx), ld_dx}, s);
-            if (!rc && p.sums) {
-                rc = rows_product<K, OUT_F32, true>(z, p, W, D, RowsOut{reinterpret_cast<char*>(p.sums), (int64_t)p.ld_x}, s);
-                const Spread sp = spread((in + 3) / 4);
-                if (!rc)
-                    rc = in_launches(tokens, sp.rows(), sp.across, 256, [&](uint32_t first, uint32_t blocks) {
-                        IWP_LAUNCH_BLOCK("k_expert_sum", k_expert_sum<K::OUT>, blocks, 256, s, p.sums, p.ld_x, chosen, tokens, slots, experts, in, first, sp,
-                                         dx, ld_dx);
-                        return (int)IWP_OK;
-                    });
-            }
-        }
-        if (!rc && dw)
-            rc = dw_dtype == IWP_F32 ? dw_product<K, OUT_F32>(z, p, X, D, dw, ld_dw, step_dw, s) : dw_product<K, K::OUT>(z, p, X, D, dw, ld_dw, step_dw, s);
-        return rc;
+        const Packed X{p.x, p.ld_x, in, 0}, D{p.d, p.ld_d, out, 0};
+        Matrices W;
+        int rc = arrange<SIZE>(z, p, chosen, w, ld_w, step_w, dx && tokens, &W, s);
+        if (!rc)
+            rc = gather<SIZE>(z, p, gather_of(z, dy, ld_dy, out, 1, p.d, p.ld_d), dw ? gather_of(z, x, ld_x, in, z.by_slot ? 1 : slots, p.x, p.ld_x) : RowsGather{}, s);
+        if (rc) return rc;
+        // out_x, out_w: constants with the types of what the kernel writes
+        auto products = [&](auto out_x, auto out_w) {
+            return with_tile_of<K>(p.tile, [&](auto tile) {
+                typedef decltype(tile) T;
+                auto kernel = k_expert_gradients<typename K::E, T::BP, T::BQ, T::WP, T::WQ, decltype(out_x)::value, decltype(out_w)::value>;
+                const RowsOut rows = p.sums ? RowsOut{reinterpret_cast<char*>(p.sums), (int64_t)p.ld_x} : RowsOut{static_cast<char*>(dx), ld_dx};
+                const uint32_t tiles = dx ? (in + T::BP - 1) / T::BP * p.max_tiles : 0, matrices = dw ? (uint32_t)(experts * tiles_of<T>(in, out)) : 0;
+                IWP_LAUNCH_BLOCK("k_expert_gradients", kernel, ((tiles + 7) / 8 + (matrices + 7) / 8) * 8, T::THREADS, s, W, X, D, p.R, experts, rows,
+                                 dx && tokens, (MatricesOut{static_cast<char*>(dw), ld_dw, step_dw}), matrices);
+                return (int)IWP_OK;
+            });
+        };
+        constexpr std::integral_constant<int, K::OUT> own{};
+        constexpr std::integral_constant<int, OUT_F32> wide{};
+        const bool wide_w = dw && dw_dtype == IWP_F32;
+        if (p.sums) rc = wide_w ? products(wide, wide) : products(wide, own);
+        else rc = wide_w ? products(own, wide) : products(own, own);
+        if (rc || !dx || !p.sums) return rc;
+        const Spread sp = spread((in + 3) / 4);
+        return in_launches(tokens, sp.rows(), sp.across, 256, [&](uint32_t first, uint32_t blocks) {
+            IWP_LAUNCH_BLOCK("k_expert_sum", k_expert_sum<K::OUT>, blocks, 256, s, p.sums, p.ld_x, chosen, tokens, slots, experts, in, first, sp, dx, ld_dx);
+            return (int)IWP_OK;
+        });
     });
 }
 
