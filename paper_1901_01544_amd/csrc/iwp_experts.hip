@@ -169,19 +169,20 @@ int with_kind(uint32_t dtype, F f) {
     return dtype == IWP_BF16 ? f(KindBf16{}) : f(KindF16{});
 }
 
-// Arranges the slots and, where the products cannot read the matrices where they lie, copies them.
+// Arranges the slots, and copies the matrices (if they are wanted and cannot be read where they lie) and `rows`.
 template <int SIZE>
-int arrange(const ProductSizes& z, const ProductPlan& p, const int32_t* chosen, const void* w, int64_t ld, int64_t step, bool wanted, Matrices* W, hipStream_t s) {
+int arrange(const ProductSizes& z, const ProductPlan& p, const int32_t* chosen, const void* w, int64_t ld, int64_t step, bool wanted, Matrices* W,
+            const MatrixCopy& rows, hipStream_t s) {
     *W = Matrices{static_cast<const char*>(w), step, (uint32_t)ld, z.out, z.in};
     MatrixCopy copy{static_cast<const char*>(w), ld, step, z.out, z.in, Units{1, 0}, p.w};
     if (p.w && wanted) {
         *W = Matrices{p.w, (int64_t)z.out * p.ld_x, p.ld_x, z.out, z.in};
         copy.of = Units{p.ld_x * SIZE / 16, z.experts * z.out};
     }
-    const uint32_t copiers = (uint32_t)((copy.of.threads() + ARRANGE_THREADS - 1) / ARRANGE_THREADS);
+    const uint32_t copiers = (uint32_t)((copy.of.threads() + rows.of.threads() + ARRANGE_THREADS - 1) / ARRANGE_THREADS);
     if (p.arrangers > 1) IWP_LAUNCH_BLOCK("k_expert_count", k_expert_count, p.arrangers, ARRANGE_THREADS, s, chosen, z.rows(), p.per_wave, z.experts, p.R);
     IWP_LAUNCH_BLOCK("k_expert_arrange", k_expert_arrange<SIZE>, p.arrangers + copiers, ARRANGE_THREADS, s, chosen, z.rows(), p.per_wave, z.experts, p.height,
-                     p.arrangers, p.R, copy);
+                     p.arrangers, p.R, copy, rows);
     return IWP_OK;
 }
 
@@ -198,7 +199,8 @@ int gather(const ProductSizes& z, const ProductPlan& p, const RowsGather& A, con
 // HIP counts a launch's threads in 32 bits.  More rows by columns than this allows fit no memory.
 bool launches_fit(const ProductSizes& z, const ProductPlan& p) {
     const uint64_t widest = round_up(std::max(z.in, z.out), 64u), units = widest * size_of(z.dtype) / 16;
-    return 2 * units * (z.padded() / GATHER_ROWS + 1) <= MOST_THREADS && units * z.experts * z.out / GATHER_ROWS + (ARRANGE_MOST + 2) * ARRANGE_THREADS <= MOST_THREADS &&
+    return 2 * units * (z.padded() / GATHER_ROWS + 1) <= MOST_THREADS &&
+           units * ((uint64_t)z.experts * z.out / GATHER_ROWS + z.rows() / GATHER_ROWS + 2) + (ARRANGE_MOST + 2) * ARRANGE_THREADS <= MOST_THREADS &&
            with_tile(p.tile, [&](auto tile) {
                typedef decltype(tile) T;
                const uint64_t rows = (widest + T::BP - 1) / T::BP * p.max_tiles, matrices = z.gradient ? z.experts * tiles_of<T>(z.in, z.out) : 0;
@@ -328,11 +330,16 @@ int iwp_expert_product(const void* x, int64_t ld_x, uint32_t x_by_slot, const vo
                              (Packed{static_cast<const char*>(x), (uint32_t)ld_x, in, z.by_slot ? 1 : slots}), chosen, z.rows(), experts, by_slot, Y);
             return (int)IWP_OK;
         }
+        // rows where they lie, else copied side by side, or gathered where 32 bits do not reach all of them
+        const uint32_t per_row = z.by_slot ? 1 : slots, rows = z.rows() / per_row;
         Matrices W;
-        Packed X{p.x, p.ld_x, in, 0};
-        int rc = arrange<SIZE>(z, p, chosen, w, ld_w, step_w, true, &W, s);
-        if (in_place(x, ld_x, in, z.by_slot ? z.rows() : tokens, dtype)) X = Packed{static_cast<const char*>(x), (uint32_t)ld_x, in, z.by_slot ? 1 : slots};
-        else if (!rc) rc = gather<SIZE>(z, p, gather_of(z, x, ld_x, in, z.by_slot ? 1 : slots, p.x, p.ld_x), RowsGather{}, s);
+        Packed X{static_cast<const char*>(x), (uint32_t)ld_x, in, per_row};
+        MatrixCopy copy{static_cast<const char*>(x), ld_x, 0, rows, in, Units{1, 0}, p.x};
+        const bool lies = in_place(x, ld_x, in, rows, dtype), copied = !lies && in_place(p.x, p.ld_x, p.ld_x, rows, dtype);
+        if (copied) copy.of = Units{p.ld_x * SIZE / 16, rows};
+        if (!lies) X = Packed{p.x, p.ld_x, in, copied ? per_row : 0};
+        int rc = arrange<SIZE>(z, p, chosen, w, ld_w, step_w, true, &W, copy, s);
+        if (!rc && !X.slots) rc = gather<SIZE>(z, p, gather_of(z, x, ld_x, in, per_row, p.x, p.ld_x), RowsGather{}, s);
         if (rc) return rc;
         return with_tile_of<K>(p.tile, [&](auto tile) {
             typedef decltype(tile) T;
@@ -368,7 +375,7 @@ int iwp_expert_product_gradient(const void* x, int64_t ld_x, uint32_t x_by_slot,
         constexpr int SIZE = K::E::SIZE;
         const Packed X{p.x, p.ld_x, in, 0}, D{p.d, p.ld_d, out, 0};
         Matrices W;
-        int rc = arrange<SIZE>(z, p, chosen, w, ld_w, step_w, dx && tokens, &W, s);
+        int rc = arrange<SIZE>(z, p, chosen, w, ld_w, step_w, dx && tokens, &W, MatrixCopy{}, s);
         if (!rc)
             rc = gather<SIZE>(z, p, gather_of(z, dy, ld_dy, out, 1, p.d, p.ld_d), dw ? gather_of(z, x, ld_x, in, z.by_slot ? 1 : slots, p.x, p.ld_x) : RowsGather{}, s);
         if (rc) return rc;

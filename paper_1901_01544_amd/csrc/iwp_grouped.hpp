@@ -173,9 +173,9 @@ __device__ __forceinline__ words4 row_chunk(const char* row, uint32_t c, uint32_
 constexpr uint32_t GATHER_ROWS = 4;
 struct Units {
     uint32_t units, rows;
-    __host__ __device__ uint64_t threads() const { return (uint64_t)units * ((rows + GATHER_ROWS - 1) / GATHER_ROWS); }
-    __device__ __forceinline__ uint32_t unit(uint64_t thread) const { return (uint32_t)(thread % units); }
-    __device__ __forceinline__ uint32_t row(uint64_t thread) const { return (uint32_t)(thread / units) * GATHER_ROWS; }
+    __host__ __device__ uint32_t threads() const { return units * ((rows + GATHER_ROWS - 1) / GATHER_ROWS); }      // (launches_fit)
+    __device__ __forceinline__ uint32_t unit(uint32_t thread) const { return thread % units; }
+    __device__ __forceinline__ uint32_t row(uint32_t thread) const { return thread / units * GATHER_ROWS; }
 };
 
 // Matrices whose rows cannot be read by 16 bytes where they lie, into rows of whole units, zeros past the width.
@@ -187,7 +187,7 @@ struct MatrixCopy {
     char* out;
 };
 template <int SIZE>
-__device__ __forceinline__ void copy_matrices(const MatrixCopy& m, uint64_t thread) {
+__device__ __forceinline__ void copy_matrices(const MatrixCopy& m, uint32_t thread) {
     constexpr uint32_t CHUNK = 16 / SIZE;
     const uint32_t u = m.of.unit(thread), r0 = m.of.row(thread);
     words4 v[GATHER_ROWS];
@@ -201,16 +201,18 @@ __device__ __forceinline__ void copy_matrices(const MatrixCopy& m, uint64_t thre
         if (r0 + i < m.of.rows) *reinterpret_cast<words4*>(m.out + ((size_t)(r0 + i) * m.of.units + u) * 16) = v[i];
 }
 
-// The first `arrangers` workgroups arrange the slots, the others copy matrices, which has to be done anyway and does not wait for that.
+// The first `arrangers` workgroups arrange the slots, the others copy matrices and rows that cannot be read where they lie, which does not
+// wait for that.
 template <int SIZE>
 __global__ void __launch_bounds__(ARRANGE_THREADS) k_expert_arrange(const int32_t* __restrict__ chosen, uint32_t n, uint32_t per_wave, uint32_t experts,
-                                                                    uint32_t height, uint32_t arrangers, ExpertRows R, MatrixCopy copy) {
+                                                                    uint32_t height, uint32_t arrangers, ExpertRows R, MatrixCopy A, MatrixCopy B) {
     if (blockIdx.x < arrangers) {
         arrange_slots(chosen, n, per_wave, experts, height, arrangers, R);
         return;
     }
-    const uint64_t thread = (uint64_t)(blockIdx.x - arrangers) * ARRANGE_THREADS + threadIdx.x;
-    if (thread < copy.of.threads()) copy_matrices<SIZE>(copy, thread);
+    const uint32_t thread = (blockIdx.x - arrangers) * ARRANGE_THREADS + threadIdx.x, first = A.of.threads();
+    if (thread < first) copy_matrices<SIZE>(A, thread);
+    else if (thread - first < B.of.threads()) copy_matrices<SIZE>(B, thread - first);
 }
 
 // Rows of a caller's matrix in the experts' order, zeros behind an expert's rows and past the width.  slots: of a token, whose row each of
@@ -223,7 +225,7 @@ struct RowsGather {
     char* out;
 };
 template <int SIZE>
-__device__ __forceinline__ void gather_rows(const RowsGather& g, const ExpertRows& R, uint32_t rows, uint64_t thread) {
+__device__ __forceinline__ void gather_rows(const RowsGather& g, const ExpertRows& R, uint32_t rows, uint32_t thread) {
     constexpr uint32_t CHUNK = 16 / SIZE;
     const uint32_t u = g.of.unit(thread), r0 = g.of.row(thread);
     words4 v[GATHER_ROWS];
@@ -241,7 +243,7 @@ __device__ __forceinline__ void gather_rows(const RowsGather& g, const ExpertRow
 template <int SIZE>
 __global__ void __launch_bounds__(256) k_expert_gather(RowsGather A, RowsGather B, uint32_t first, uint32_t experts, ExpertRows R) {
     const bool second = blockIdx.x >= first;
-    const uint64_t thread = (uint64_t)(second ? blockIdx.x - first : blockIdx.x) * 256 + threadIdx.x;
+    const uint32_t thread = (second ? blockIdx.x - first : blockIdx.x) * 256 + threadIdx.x;
     if (thread < (second ? B : A).of.threads()) gather_rows<SIZE>(second ? B : A, R, R.start[experts], thread);
 }
 
