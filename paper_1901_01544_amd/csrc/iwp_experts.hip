@@ -256,7 +256,7 @@ int iwp_route(const void* x, int64_t ld_x, uint32_t tokens, uint32_t experts, ui
             const uint32_t at_once = 64 / lanes, row = experts + groups;
             const uint32_t lds = round_up<uint32_t>(std::max({lanes >= 16 ? at_once * CANDIDATES * (uint32_t)sizeof(Candidate) : 0u, by_score ? row * 8 : 0u,
                                                               grouped ? at_once * row * 4 : 0u}), 16);
-            const TokenGrid g(tokens, at_once, lds + at_once * slots * 4);
+            const TokenGrid g(tokens, at_once, lds + at_once * (by_score ? 2 * slots + 1 : slots) * 4);
             auto launch = [&](auto kernel) {
                 IWP_LAUNCH_AS("k_route", kernel, g.blocks, g.waves * 64, g.lds, s, r, lds);
                 return (int)IWP_OK;

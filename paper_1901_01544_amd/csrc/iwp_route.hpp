@@ -193,7 +193,7 @@ struct Candidate {
     uint32_t expert;
 };
 
-// BY_SCORE: c is a score and a bias, else the logit.  lds: bytes of a wavefront besides its slots.
+// BY_SCORE: c is a score and a bias, else the logit.  lds: bytes of a wavefront besides its slots (and their c).
 template <int IN, int CHUNKS, int LANES, bool BY_SCORE, bool GROUPS>
 __global__ void __launch_bounds__(256) k_route(RouteCall r, uint32_t lds) {
     typedef TokenLanes<IN, CHUNKS> L;
@@ -206,6 +206,7 @@ __global__ void __launch_bounds__(256) k_route(RouteCall r, uint32_t lds) {
     const uint32_t mine = wave * at_once + l.of, of_group = r.experts / r.groups;
     char* own = shared + wave * lds;
     int32_t* slot = reinterpret_cast<int32_t*>(shared + (blockDim.x >> 6) * lds) + mine * r.slots;
+    float* in_order = reinterpret_cast<float*>(shared + (blockDim.x >> 6) * lds) + tokens * r.slots + mine * (r.slots + 1);      // (BY_SCORE) the slots' c and the next
     // groups that are whole runs of lanes: `per` of them
     const uint32_t per = of_group / L::WIDTH;           // (at least WIDTH experts each: no more groups than CHUNKS a lane)
     const bool by_lanes = GROUPS && of_group % L::WIDTH == 0 && (per & (per - 1)) == 0 && per <= r.lanes;
@@ -365,24 +366,26 @@ float bias[L::N];
 #pragma unroll
             for (int v = 0; v < L::N; ++v)
                 if (c[v] >= bound) list[to++] = Candidate{c[v], l.expert(v)};
-            for (uint32_t k = l.lane; k < r.slots; k += r.lanes) slot[k] = -1;
+            for (uint32_t k = l.lane; k < r.slots + MORE; k += r.lanes) {
+                if (k < r.slots) slot[k] = -1;
+                if (BY_SCORE) in_order[k] = NONE;
+            }
             lanes_exchange();
             for (uint32_t k = l.lane; k < n; k += r.lanes) {
                 const Candidate me = list[k];
                 uint32_t before = 0;
-                bool near = false;
                 for (uint32_t o = 0; o < n; ++o) {
                     const Candidate other = list[o];
                     before += (other.c > me.c) | ((other.c == me.c) & (other.expert < me.expert));
-                    if (BY_SCORE) near |= (o != k) & !(fabsf(other.c - me.c) > 2.0f * off);
                 }
-                if (before < r.slots) {
-                    slot[before] = (int32_t)me.expert;
-                    close |= near;
-                }
+                if (before < r.slots) slot[before] = (int32_t)me.expert;
+                if (BY_SCORE && before <= r.slots) in_order[before] = me.c;
             }
-            close = part.any(close);
             lanes_exchange();
+            if (BY_SCORE) {
+                for (uint32_t k = l.lane; k < r.slots; k += r.lanes) close |= in_order[k + 1] != NONE && !(in_order[k] - in_order[k + 1] > 2.0f * off);
+                close = part.any(close);
+            }
         }
     }
     if (!done) {                        // of equal c the lower expert, which is also the lower v of a lane
@@ -419,23 +422,25 @@ float bias[L::N];
         auto logit = [&](int32_t e) { return element<IN>(r.x, (int64_t)i * r.ld + e); };
         const int32_t mine0 = l.lane < r.slots ? slot[l.lane] : -1;
         const float x0 = mine0 >= 0 ? logit(mine0) : NONE;
-        auto x_of = [&](uint32_t k, int32_t e) { return k == l.lane ? x0 : logit(e); };
         auto share = [&](float x, float m) { return r.sigmoid ? sigmoid_over(x, m) : expf(x - m); };
-        float all = 1.0f, most = r.sigmoid ? 0.0f : m;
+        float all = 1.0f, most = r.sigmoid ? 0.0f : m, q0 = 0.0f;
         if (r.renormalise) {
             most = r.sigmoid && mine0 >= 0 ? fminf(x0, 0.0f) : x0;
             for (uint32_t k = l.lane + r.lanes; k < r.slots; k += r.lanes)
                 if (slot[k] >= 0) most = fmaxf(most, r.sigmoid ? fminf(logit(slot[k]), 0.0f) : logit(slot[k]));
             most = part.max(most);
-            all = mine0 >= 0 ? share(x0, most) : 0.0f;
+            q0 = mine0 >= 0 ? share(x0, most) : 0.0f;
+            all = q0;
             for (uint32_t k = l.lane + r.lanes; k < r.slots; k += r.lanes)
                 if (slot[k] >= 0) all += share(logit(slot[k]), most);
             all = part.sum(all);
+        } else if (mine0 >= 0) {
+            q0 = share(x0, most);
         }
         for (uint32_t k = l.lane; k < r.slots; k += r.lanes) {
             const int32_t e = slot[k];
             float y = 0.0f;
-            if (e >= 0) y = share(x_of(k, e), most) * (r.renormalise || r.sigmoid ? 1.0f : by) / all * r.scale;
+            if (e >= 0) y = (k == l.lane ? q0 : share(logit(e), most)) * (r.renormalise || r.sigmoid ? 1.0f : by) / all * r.scale;
             const size_t to = (size_t)i * r.slots + k;
             r.chosen[to] = e;
             r.weight[to] = nan ? NAN : y;

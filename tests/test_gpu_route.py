@@ -263,3 +263,29 @@ def test_same_bytes_on_another_stream_and_in_a_graph(experts, size):
         torch.cuda.synchronize()
         for a, b, c in zip(first, second, third):
             assert torch.equal(a, b) and torch.equal(a, c)
+
+
+@pytest.mark.parametrize("kind", TYPES, ids=str)
+@pytest.mark.parametrize("E", [8, 100, 256, 1024])
+def test_all_alike_and_masked_by_the_lowest_value(experts, kind, E):
+    """More equal logits than a token's candidates have room for; masks of the type's lowest value instead of -inf, for some and for all."""
+    x = torch.zeros(70, E, dtype=kind, device=DEV)
+    gen = torch.Generator(device=DEV).manual_seed(12)
+    lowest = torch.finfo(kind).min
+    x[20:] = torch.randn(50, E, generator=gen, device=DEV).to(kind)
+    x[20:40, E // 4:] = lowest
+    x[40:60, 3:] = lowest
+    x[60:] = lowest
+    x[65:, E // 2] = torch.finfo(kind).max
+    K = 4
+    for how in (dict(), dict(renormalise=True), dict(scores="sigmoid"), dict(bias=torch.zeros(E, device=DEV)),
+                dict(bias=torch.zeros(E, device=DEV), scores="sigmoid", groups=4, top_groups=2, group_top=2)):
+        chosen, weight = route(experts, x, K, **how)
+        ref = Route(x, K, **how)
+        assert torch.equal(chosen, ref.chosen)
+        assert (chosen[:20] == torch.arange(K, device=DEV)).all()
+        # differences to the lowest value round to it, and its exponential is 0 either way: the bound of the values that are ordinary ones
+        small = 2.0 ** -19 * 8 * ref.weight.abs() + 2.0 ** -140
+        assert ((weight.double() - ref.weight).abs() <= small).all()
+        dx = gradient(experts, x, chosen, torch.ones(70, K, device=DEV), **{k: v for k, v in how.items() if k in ("scores", "renormalise")})
+        assert torch.isfinite(dx).all()
