@@ -74,6 +74,10 @@ int with_tile_of(TileKind kind, F f) {
 template <class T>
 uint64_t tiles_of(uint64_t np, uint64_t nq) { return (np + T::BP - 1) / T::BP * ((nq + T::BQ - 1) / T::BQ); }
 
+// The largest tile of which the experts' rows make enough for most of the 256 compute units and that they fill.  us of a call with large tiles, middling
+// and small ones, bf16: 2048 x 2 rows of 8 experts x 2048 x 4096 (512 rows each) 119, 111, 130; 8192 x 8 of 32 x 1024 x 512 (2048 each) 145, 141, 164; 512 x 2
+// of 8 x 2048 x 4096 (128 each) 58, 44, 55; 64 x 4 of 16 x 2048 x 2048 (16 each) 52, 36, 31.  Binary32 is bound by the matrix cores in any tile and
+// wants them small: 4096 x 2 of 8 x 1024 x 1024 272, 288, 183.
 constexpr uint64_t ENOUGH_TILES = 160;
 // `each`: entries of Q that one expert has; `many`: experts that have that many
 TileKind tile_for(uint64_t np, uint64_t each, uint64_t many, uint32_t dtype) {
@@ -120,8 +124,10 @@ bool readable(const void* w, int64_t ld, int64_t step, uint32_t in, uint32_t dty
     return aligned(w, 16) && ld % chunk == 0 && step % chunk == 0 && in % chunk == 0;
 }
 
-// A workgroup arranges 4096 slots, four rounds of its wavefronts, up to 64 of them, each of which reads all the others' counts.
-constexpr uint32_t ARRANGE_SLOTS = 4096, ARRANGE_MOST = 64;
+// One workgroup arranges up to 2048 slots; more are counted first and arranged by up to 64, each of which reads all the others' counts, 1024
+// slots or more each.  us of counting and arranging: 2042 slots by one 10, by two 16; 4096 by one 13, by four 16 (a call with small products 14.5 and
+// 13.8); 16384 of 8 experts by 4 21, by 16 17.  Beside a copy of the matrices, which takes longer, one workgroup is enough for more.
+constexpr uint32_t ARRANGE_ONE = 2048, ARRANGE_SLOTS = 1024, ARRANGE_MOST = 64;
 
 ProductPlan product_plan(const ProductSizes& z, bool copy_w, void* workspace) {
     ProductPlan p{};
@@ -132,7 +138,7 @@ ProductPlan product_plan(const ProductSizes& z, bool copy_w, void* workspace) {
     p.tile = tile_for(z.gradient ? z.in : z.out, each, many, z.dtype);
     p.height = p.tile == BIG ? Big::BQ : p.tile == MID ? Mid::BQ : Few::BQ;
     p.max_tiles = n / p.height + many + 1;
-    p.arrangers = std::max(1u, std::min((n + ARRANGE_SLOTS - 1) / ARRANGE_SLOTS, ARRANGE_MOST));
+    p.arrangers = n <= (copy_w ? 4 * ARRANGE_ONE : ARRANGE_ONE) ? 1 : std::min((n + ARRANGE_SLOTS - 1) / ARRANGE_SLOTS, ARRANGE_MOST);
     p.per_wave = round_up((n + p.arrangers * ARRANGE_WAVES - 1) / (p.arrangers * ARRANGE_WAVES), 64u);
     Carver c{static_cast<char*>(workspace)};
     if (p.arrangers > 1) c.take(p.R.counts, (size_t)p.arrangers * (z.experts + 1));
