@@ -129,6 +129,14 @@ bool readable(const void* w, int64_t ld, int64_t step, uint32_t in, uint32_t dty
 // 13.8); 16384 of 8 experts by 4 21, by 16 17.  Beside a copy of the matrices, which takes longer, one workgroup is enough for more.
 constexpr uint32_t ARRANGE_ONE = 2048, ARRANGE_SLOTS = 1024, ARRANGE_MOST = 64;
 
+// Products of few rows an expert need no arrangement.  us here and by tiles, mean rows of an expert that has any: bf16 1 token x 8 of 64 experts x 2048 x 1024
+// 10 and 33, 16 tokens 42 and 53 (2 rows), 32 x 4 of 16 x 2048 x 2048 34 and 42 (8), 64 x 4 of 16 50 and 42 (16); binary32 60 x 2 of 8 x 1024 x 1024
+// 16 and 29 (15).
+bool few_rows(const ProductSizes& z) {
+    const uint32_t n = z.rows();
+    return n <= FEW_SLOTS && n <= (z.dtype == IWP_F32 ? FEW_ROWS : FEW_ROWS / 2) * std::min(z.experts, n);
+}
+
 ProductPlan product_plan(const ProductSizes& z, bool copy_w, void* workspace) {
     ProductPlan p{};
     p.deep = ROW_BYTES / (uint32_t)size_of(z.dtype);
@@ -140,6 +148,10 @@ ProductPlan product_plan(const ProductSizes& z, bool copy_w, void* workspace) {
     p.max_tiles = n / p.height + many + 1;
     p.arrangers = n <= (copy_w ? 4 * ARRANGE_ONE : ARRANGE_ONE) ? 1 : std::min((n + ARRANGE_SLOTS - 1) / ARRANGE_SLOTS, ARRANGE_MOST);
     p.per_wave = round_up((n + p.arrangers * ARRANGE_WAVES - 1) / (p.arrangers * ARRANGE_WAVES), 64u);
+    if (!z.gradient && few_rows(z)) {
+        p.bytes = 256;                     // none is used
+        return p;
+    }
     Carver c{static_cast<char*>(workspace)};
     if (p.arrangers > 1) c.take(p.R.counts, (size_t)p.arrangers * (z.experts + 1));
     c.take(p.R.start, z.experts + 1);
@@ -212,14 +224,6 @@ bool launches_fit(const ProductSizes& z, const ProductPlan& p) {
                const uint64_t rows = (widest + T::BP - 1) / T::BP * p.max_tiles, matrices = z.gradient ? z.experts * tiles_of<T>(z.in, z.out) : 0;
                return (int)((rows + matrices + 16) * T::THREADS <= MOST_THREADS);
            });
-}
-
-// Products of few rows an expert need no arrangement.  us here and by tiles, mean rows of an expert that has any: bf16 1 token x 8 of 64 experts x 2048 x 1024
-// 10 and 33, 16 tokens 42 and 53 (2 rows), 32 x 4 of 16 x 2048 x 2048 34 and 42 (8), 64 x 4 of 16 50 and 42 (16); binary32 60 x 2 of 8 x 1024 x 1024
-// 16 and 29 (15).
-bool few_rows(const ProductSizes& z) {
-    const uint32_t n = z.rows();
-    return n <= FEW_SLOTS && n <= (z.dtype == IWP_F32 ? FEW_ROWS : FEW_ROWS / 2) * std::min(z.experts, n);
 }
 
 // Can a product read these rows where they lie?  By 16 bytes, whole tiles of the summed index, within what 32 bits count.

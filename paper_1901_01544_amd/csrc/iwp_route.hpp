@@ -4,7 +4,12 @@
 //   groups: best one or two c of every group between the lanes that have it, a group's rank by counting;
 //   slots: the largest c that is left, one after the other, or where there are many lanes all at once (see candidates).
 // Scores decide in binary64, but are computed in binary32 first: where no two c that the choice depends on are closer than twice what
-// binary32 may be off, it is the choice.  Else the wavefront does the token again in binary64, value by value in LDS.
+// binary32 may be off, it is the choice.  Else the wavefront does the token again in binary64, value by value in LDS (6 of 10000 tokens of the
+// case below).
+//
+// Bound by instructions where experts are many.  131072 tokens x 256 experts in binary32, 8 slots: by logits alone 30 us, which is reading them (134 MB,
+// 4.5 TB/s); sigmoid scores with a bias 53; of 4 of 8 groups by their best two 75, some 1250 vector instructions a wavefront of four tokens.  In
+// binary64 throughout 264; slots one after the other instead of all at once 120.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -251,7 +256,7 @@ __global__ void __launch_bounds__(256) k_route(RouteCall r, uint32_t lds) {
             for (int v = 0; v < L::N; ++v) sum += (double)exp_of(c[v] - from);
             by = (float)(1.0 / part.sum(sum));
         }
-float bias[L::N];
+        float bias[L::N];
 #pragma unroll
         for (int v = 0; v < L::N; ++v) bias[v] = 0.0f;
         if (r.bias) {
@@ -476,9 +481,9 @@ __global__ void __launch_bounds__(256) k_route_gradient(RouteGradient r) {
     const Part part(r.lanes);
     const uint32_t wave = threadIdx.x >> 6, at_once = l.tokens(), tokens = (blockDim.x >> 6) * at_once;
     const uint32_t mine = wave * at_once + l.of;
-    SlotGradient* slot = reinterpret_cast<SlotGradient*>(shared) + (size_t)mine * r.slots;
     const uint32_t units = (r.experts + L::WIDTH - 1) / L::WIDTH * L::WIDTH;
-    f32_bytes* row = reinterpret_cast<f32_bytes*>(shared + (size_t)tokens * r.slots * sizeof(SlotGradient)) + (size_t)mine * units;
+    f32_bytes* row = reinterpret_cast<f32_bytes*>(shared) + (size_t)mine * units;
+    SlotGradient* slot = reinterpret_cast<SlotGradient*>(shared + (size_t)tokens * units * sizeof(float)) + (size_t)mine * r.slots;
     const bool dense = !r.sigmoid && !r.renormalise;
     for (uint32_t base = blockIdx.x * tokens; base < r.tokens; base += gridDim.x * tokens) {
         const uint32_t i = base + mine;

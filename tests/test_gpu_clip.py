@@ -166,3 +166,21 @@ def test_workers_beyond_the_cache(clipping):
     onto = [x.clone() for x in g]
     call(clipping, rows, onto, onto, max_norm=100.0)
     check(rows, g, onto, g, norm, 100.0)
+
+
+def test_tensors_beyond_32_bits(clipping):
+    """The last of a flat buffer of as many elements as one may have."""
+    end = 0xFFFF0000
+    rows = [(5, 1000), (end - 70_001, 70_001)]
+    flat = torch.zeros(end, device=DEV)
+    gen = torch.Generator(device=DEV).manual_seed(6)
+    for o, n in rows:
+        flat[o:o + n] = torch.randn(n, generator=gen, device=DEV)
+    before = [flat[o:o + n].clone() for o, n in rows]
+    norm = call(clipping, rows, [flat], [flat], max_norm=10.0)
+    want = torch.cat(before).double().norm()
+    assert abs(norm[0].double() - want) <= 1.01 * HALF * want
+    for (o, n), x in zip(rows, before):
+        y = x.double() * (10.0 / want)
+        assert ((flat[o:o + n].double() - y).abs() <= 1.01 * HALF * y.abs() + 2.0 ** -150).all()
+    assert not flat[1005:end - 70_001].any()

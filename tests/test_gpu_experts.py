@@ -89,8 +89,9 @@ def test_no_rows_at_all(experts, kind, by_slot):
 
 @pytest.mark.parametrize("kind", TYPES, ids=str)
 @pytest.mark.parametrize("by_slot", [False, True])
-def test_nan_and_infinity_stay_with_their_rows(experts, kind, by_slot):
-    T, K, E, D, F = 150, 2, 5, 72, 136
+@pytest.mark.parametrize("T,D", [(150, 72), (150, 128), (20, 72)])
+def test_nan_and_infinity_stay_with_their_rows(experts, kind, by_slot, T, D):
+    K, E, F = 2, 5, 136
     x, w, chosen, dy = inputs(T, K, E, D, F, kind, by_slot, nobody=0.2)
     chosen[chosen == 4] = 3                                             # nobody's matrix
     clean = Experts(x, w, chosen, dy)
@@ -112,9 +113,10 @@ def test_nan_and_infinity_stay_with_their_rows(experts, kind, by_slot):
 
 @pytest.mark.parametrize("kind", TYPES, ids=str)
 @pytest.mark.parametrize("shift,more", [(0, 8), (1, 3), (8, 16), (4, 5)])
-def test_strides_and_alignments(experts, kind, shift, more):
+@pytest.mark.parametrize("T", [10, 90])
+def test_strides_and_alignments(experts, kind, shift, more, T):
     """Rows of every matrix a stretch of longer ones, matrices apart from each other; what lies around the outputs stays."""
-    T, K, E, D, F = 90, 3, 4, 96, 56
+    K, E, D, F = 3, 4, 96, 56
     for by_slot in (False, True):
         x0, w0, chosen, dy0 = inputs(T, K, E, D, F, kind, by_slot)
 
@@ -240,3 +242,31 @@ def test_many_slots(experts, T, K, E):
     outer = dy.double()[inside][:, :, None] * x.double()[inside][:, None, :]
     want = torch.zeros(E, 8, 8, dtype=torch.float64, device=DEV).index_add_(0, chosen[inside].long(), outer)
     assert torch.equal(dw.double(), want)
+
+
+@pytest.mark.parametrize("T,K,E", [(700, 2, 3), (9, 2, 3)])
+def test_rows_and_matrices_far_apart(experts, T, K, E):
+    """Offsets that 32 bits do not hold: rows 8 MB apart, matrices 2^31 elements."""
+    D, F = 128, 64
+    x0, w0, chosen, dy0 = inputs(T, K, E, D, F, torch.bfloat16, False)
+    ref = Experts(x0, w0, chosen, dy0)
+    far = 1 << 22
+
+    def rows(t):
+        n = t.numel() // t.shape[-1]
+        part = torch.zeros(n * far, dtype=t.dtype, device=DEV).view(n, far)[:, 64:64 + t.shape[-1]]
+        part.copy_(t.reshape(n, -1))
+        return part.unflatten(0, t.shape[:-1]) if t.dim() == 3 else part
+
+    def matrices(kind):
+        return torch.empty((E - 1) * (1 << 31) + F * D, dtype=kind, device=DEV).as_strided((E, F, D), (1 << 31, D, 1))
+
+    x, w = rows(x0), matrices(torch.bfloat16)
+    w.copy_(w0)
+    y = rows(torch.zeros_like(dy0))
+    product(experts, x, w, chosen, y)
+    ref.check(y.contiguous())
+    y.copy_(dy0)
+    dx, dw = rows(torch.zeros_like(x0)), matrices(torch.float32)
+    gradient(experts, x, w, chosen, y, dx=dx, dw=dw)
+    ref.check_gradient(dx.contiguous(), dw.contiguous())

@@ -289,3 +289,18 @@ def test_all_alike_and_masked_by_the_lowest_value(experts, kind, E):
         assert ((weight.double() - ref.weight).abs() <= small).all()
         dx = gradient(experts, x, chosen, torch.ones(70, K, device=DEV), **{k: v for k, v in how.items() if k in ("scores", "renormalise")})
         assert torch.isfinite(dx).all()
+
+
+def test_rows_beyond_32_bits(experts):
+    """2^20 tokens, rows 16 KB apart: checked at both ends."""
+    T, E = 1 << 20, 48
+    x = torch.empty(T * 8192, dtype=torch.bfloat16, device=DEV).view(T, 8192)[:, 100:100 + E]
+    x0, gen = logits(T, E, torch.bfloat16, seed=13)
+    x.copy_(x0)
+    dweight = torch.randn(T, 3, generator=gen, device=DEV)
+    bias = 0.1 * torch.randn(E, generator=gen, device=DEV)
+    chosen, weight = route(experts, x, 3, bias=bias)
+    experts.route_gradient(x, chosen, dweight, x, plus=x)
+    for part in (slice(0, 100), slice(T - 100, T)):
+        Route(x0[part], 3, bias).check(chosen[part], weight[part])
+        RouteGradient(x0[part], chosen[part], dweight[part], plus=x0[part]).check(x[part].contiguous())

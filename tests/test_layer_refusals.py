@@ -15,7 +15,7 @@ GOOD_ROUTE = dict(x=AT, ld_x=16, tokens=10, experts=16, dtype=0, bias=None, scor
                   keep=None, chosen=AT, weight=AT, slots=4)
 GOOD_GRADIENT = dict(x=AT, ld_x=16, tokens=10, experts=16, dtype=1, chosen=AT, dweight=AT, slots=4, scores=0, renormalise=0, scale=1.0, keep=None,
                      plus=AT, ld_plus=16, dx=AT, ld_dx=16)
-GOOD_PRODUCT = dict(x=AT, ld_x=64, by_slot=0, w=AT, ld_w=64, step_w=2048, tokens=10, slots=2, experts=4, width=64, out=32, dtype=1, chosen=AT, y=AT,
+GOOD_PRODUCT = dict(x=AT, ld_x=64, by_slot=0, w=AT, ld_w=64, step_w=2048, tokens=100, slots=2, experts=4, width=64, out=32, dtype=1, chosen=AT, y=AT,
                     ld_y=32, ws=AT, bytes=1 << 40)
 GOOD_BACK = dict(x=AT, ld_x=64, by_slot=0, w=AT, ld_w=64, step_w=2048, tokens=10, slots=2, experts=4, width=64, out=32, dtype=1, chosen=AT, dy=AT,
                  ld_dy=32, dx=AT, ld_dx=64, dw=AT, ld_dw=64, step_dw=2048, dw_dtype=0, ws=AT, bytes=1 << 40)
@@ -84,10 +84,14 @@ def test_workspace_sizes():
     assert size() > 0 and size(tokens=0) > 0 and size(gradient=1) > size()
     assert 0 == size(slots=9) == size(tokens=(1 << 20) + 1) == size(experts=0) == size(width=0) == size(out=0) == size(dtype=3) == size(experts=1025)
     # matrices that cannot be read by 16 bytes where they lie are copied
-    many = dict(experts=64, width=1000, out=1000)
+    many = dict(tokens=1000, experts=64, width=1000, out=1000)
     for other in (dict(w=AT + 2), dict(ld=1001), dict(width=1001), dict(step=1000 * 1000 + 4)):
         assert size(**dict(many, **other)) >= size(**many) + 64 * 1000 * 1000 * 2
     assert size(gradient=1, tokens=4096) > size(gradient=1, tokens=4096, by_slot=1)
+    # few rows need none; sizes that no launch takes are refused by the calls too
+    assert size(tokens=4, width=1001, out=1000, experts=64) == 256
+    assert size(tokens=1 << 20, slots=16, experts=16, width=1 << 16) == 0
+    assert code("iwp_expert_product", GOOD_PRODUCT, tokens=1 << 20, slots=16, experts=16, width=1 << 16, ld_x=1 << 16, ld_w=1 << 16, step_w=1 << 30) == INVALID
 
 
 def test_every_declared_call_is_exported():
