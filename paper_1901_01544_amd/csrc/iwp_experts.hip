@@ -222,7 +222,7 @@ bool launches_fit(const ProductSizes& z, const ProductPlan& p) {
            with_tile(p.tile, [&](auto tile) {
                typedef decltype(tile) T;
                const uint64_t rows = (widest + T::BP - 1) / T::BP * p.max_tiles, matrices = z.gradient ? z.experts * tiles_of<T>(z.in, z.out) : 0;
-               return (int)((rows + matrices + 16) * T::THREADS <= MOST_THREADS);
+               return (int)((rows + matrices + TILES_AT_A_TIME) * T::THREADS <= MOST_THREADS);
            });
 }
 
@@ -355,7 +355,8 @@ int iwp_expert_product(const void* x, int64_t ld_x, uint32_t x_by_slot, const vo
             typedef decltype(tile) T;
             auto kernel = X.slots ? k_expert_rows<typename K::E, T::BP, T::BQ, T::WP, T::WQ, K::OUT, false>
                                   : k_expert_rows<typename K::E, T::BP, T::BQ, T::WP, T::WQ, K::OUT, true>;
-            IWP_LAUNCH_BLOCK("k_expert_rows", kernel, (out + T::BP - 1) / T::BP * p.max_tiles, T::THREADS, s, W, X, p.R, experts, Y);
+            const uint32_t more = T::BQ == Big::BQ ? MOST_HALVES : 0;
+            IWP_LAUNCH_BLOCK("k_expert_rows", kernel, (out + T::BP - 1) / T::BP * p.max_tiles + more, T::THREADS, s, W, X, p.R, experts, Y);
             return (int)IWP_OK;
         });
     });

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "../../include/iwp_experts.h"
+#include "iwp_halves.hpp"
 #include "iwp_matrix.hpp"
 
 namespace iwp {
@@ -332,15 +333,16 @@ __device__ __forceinline__ void store_tile(const M& mm, char* lds, uint32_t p0, 
 // slots of nobody.  at: which of the np x nq tiles, in an order in which some dozens in a row share few rows and columns.
 template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool TRANSPOSED, bool GATHERED>
 __device__ __forceinline__ void rows_tile(const Matrices& W, const Packed& X, const ExpertRows& R, uint32_t experts, const RowsOut& Y, uint32_t at, uint32_t np,
-                                          uint32_t nq, char* lds) {
+                                          uint32_t nq, char* lds, uint32_t down = 0) {
     typedef Product<E, BP, BQ, WP, WQ, TRANSPOSED, false> M;
     const uint32_t columns = TRANSPOSED ? W.columns : W.rows;
     constexpr uint32_t TALL = 8;
     const uint32_t group = at / (np * TALL), rest = at - group * np * TALL, tall = min(TALL, nq - group * TALL);
     const uint32_t tp = rest / tall;
     ExpertTile tile = R.tile[group * TALL + rest % tall];
-    tile = ExpertTile{uniform(tile.expert), uniform(tile.first)};
+    tile = ExpertTile{uniform(tile.expert), uniform(tile.first) + down};
     const uint32_t count = uniform(R.count[tile.expert]), start = uniform(R.start[tile.expert]);
+    if (tile.first >= count) return;                       // (a lower part of the tile)
     M mm;
     if (tile.expert < experts) {
         const uint32_t summed = TRANSPOSED ? W.rows : W.columns;
@@ -365,8 +367,18 @@ template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool GATHERED>
 __global__ void __launch_bounds__(WP * WQ * 64) k_expert_rows(Matrices W, Packed X, ExpertRows R, uint32_t experts, RowsOut Y) {
     __shared__ __align__(1024) char lds[Product<E, BP, BQ, WP, WQ, false, false>::LDS];
     const uint32_t np = (W.rows + BP - 1) / BP, nq = uniform(*R.tiles);
-    if (blockIdx.x < np * nq)
+    if constexpr (BQ == 256) {                             // large tiles fill a compute unit each
+        TilePart part;
+        uint32_t whole;
+        if (!part_of(blockIdx.x, np * nq, &part, &whole)) return;
+        if (part.half) {
+            rows_tile<E, BP, BQ / 2, 4, 2, OUT, false, GATHERED>(W, X, R, experts, Y, part.tile, np, nq, lds, (part.half - 1) * (BQ / 2));
+            return;
+        }
+        rows_tile<E, BP, BQ, WP, WQ, OUT, false, GATHERED>(W, X, R, experts, Y, stretch_place(part.tile, whole), np, nq, lds);
+    } else if (blockIdx.x < np * nq) {
         rows_tile<E, BP, BQ, WP, WQ, OUT, false, GATHERED>(W, X, R, experts, Y, stretch_place(blockIdx.x, np * nq), np, nq, lds);
+    }
 }
 
 // Products of few rows, in one launch, without arranging anything: a workgroup has 16 rows of an expert's matrix, each of its wavefronts a

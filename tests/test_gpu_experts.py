@@ -9,7 +9,8 @@ DEV = "cuda:0"
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
 # tokens, slots, experts, in, out
 SIZES = [(1, 1, 1, 1, 1), (1, 2, 8, 64, 128), (1, 8, 64, 256, 192), (7, 3, 5, 33, 17), (63, 2, 4, 100, 70), (64, 1, 1, 128, 256), (65, 1, 1, 129, 257),
-         (200, 2, 8, 48, 96), (333, 2, 8, 513, 640), (300, 4, 100, 72, 40), (1000, 3, 4, 320, 200), (129, 6, 1024, 16, 24), (2048, 2, 4, 512, 1024)]
+         (200, 2, 8, 48, 96), (333, 2, 8, 513, 640), (300, 4, 100, 72, 40), (1000, 3, 4, 320, 200), (129, 6, 1024, 16, 24), (2048, 2, 4, 512, 1024),
+         (2600, 2, 4, 192, 4096), (2300, 2, 4, 4096, 200)]
 
 
 @pytest.fixture(scope="module")
