@@ -115,21 +115,38 @@ __device__ __forceinline__ double factor(const ClipCall& c, double square, float
     return c.scale * (n <= c.max_norm ? 1.0 : c.max_norm / n);
 }
 
-// The last chunks first: they are what the memory-side cache still has of the pass for the norm.
+// A wavefront's chunks of a product.  The last chunks first: they are what the memory-side cache still has of the pass for the norm.  The first
+// one is requested before the factor is known, unless a gradient may stay as it is.  (8 workers of 61 M elements in place and not clipped: 389 us, with
+// that request 449.)
 template <bool LAST_USE>
-__device__ __forceinline__ void multiply(const ClipCall& c, const float* g, float* out, double by, uint32_t wave, uint32_t waves) {
-    if (by == 1.0 && out == g) return;
-    for (uint32_t k = wave; k < c.n_chunks; k += waves) {
-        const TensorChunk at = c.chunks[c.n_chunks - 1 - k];
-        words4 v[LOADS];
+struct Multiplier {
+    const ClipCall& c;
+    const float* g;
+    float* out;
+    uint32_t wave, waves;
+    TensorChunk at;
+    words4 v[LOADS];
+    __device__ __forceinline__ void request(uint32_t k) {
+        at = c.chunks[c.n_chunks - 1 - k];
         load_chunk<LAST_USE>(g + at.offset, at.n, v);
-#pragma unroll
-        for (uint32_t j = 0; j < LOADS; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[j][i] = __float_as_uint((float)((double)__uint_as_float(v[j][i]) * by));
-        store_chunk(out + at.offset, at.n, v);
     }
-}
+    __device__ __forceinline__ Multiplier(const ClipCall& c, uint32_t p, uint32_t wave, uint32_t waves) : c(c), g(c.g[p]), out(c.out[p]), wave(wave), waves(waves) {
+        if (out && out != g && wave < c.n_chunks) request(wave);
+    }
+    __device__ __forceinline__ void by(double factor) {
+        if (!out || (factor == 1.0 && out == g)) return;
+        if (out == g && wave < c.n_chunks) request(wave);
+        for (uint32_t k = wave; k < c.n_chunks;) {
+#pragma unroll
+            for (uint32_t j = 0; j < LOADS; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[j][i] = __float_as_uint((float)((double)__uint_as_float(v[j][i]) * factor));
+            store_chunk(out + at.offset, at.n, v);
+            k += waves;
+            if (k < c.n_chunks) request(k);
+        }
+    }
+};
 
 __global__ void __launch_bounds__(256) k_clip_norm(ClipCall c, uint32_t first) {
     const uint32_t p = first + blockIdx.x / c.blocks, block = blockIdx.x % c.blocks;
@@ -146,13 +163,14 @@ __global__ void __launch_bounds__(256) k_clip_apply(ClipCall c, uint32_t first, 
         if (block == 0 && threadIdx.x == 0) c.norm[p] = 0.0f;
         return;
     }
+    Multiplier<LAST_USE> m(c, p, block * 4 + (threadIdx.x >> 6), blocks * 4);
     double s = 0.0;
     for (uint32_t b = threadIdx.x; b < c.blocks; b += 256) s += c.sums[(size_t)p * c.blocks + b];
     s = workgroup_sum<4>(wave_sum(s));
     float norm;
     const double by = factor(c, s, &norm);
     if (block == 0 && threadIdx.x == 0) c.norm[p] = norm;
-    if (c.out[p]) multiply<LAST_USE>(c, c.g[p], c.out[p], by, block * 4 + (threadIdx.x >> 6), blocks * 4);
+    m.by(by);
 }
 
 // All of a worker in one workgroup, for small tables.
@@ -165,7 +183,7 @@ __global__ void __launch_bounds__(1024) k_clip_one(ClipCall c) {
     float norm;
     const double by = factor(c, workgroup_sum<16>(squares(c, c.g[p], wave, 16)), &norm);
     if (threadIdx.x == 0) c.norm[p] = norm;
-    if (c.out[p]) multiply<false>(c, c.g[p], c.out[p], by, wave, 16);
+    Multiplier<false>(c, p, wave, 16).by(by);
 }
 
 constexpr uint32_t GRID = 2048;            // 256 threads each: what the compute units hold at a time

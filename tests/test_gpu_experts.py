@@ -271,3 +271,27 @@ def test_rows_and_matrices_far_apart(experts, T, K, E):
     dx, dw = rows(torch.zeros_like(x0)), matrices(torch.float32)
     gradient(experts, x, w, chosen, y, dx=dx, dw=dw)
     ref.check_gradient(dx.contiguous(), dw.contiguous())
+
+
+def test_rows_beyond_four_gigabytes(experts):
+    """More bytes of rows than 32 bits count: these are gathered.  Whole numbers, so every sum is exact."""
+    T, E, D, F = 540_000, 3, 4096, 8
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    x = torch.randint(-8, 9, (T, D), generator=gen, device=DEV, dtype=torch.int8).to(torch.bfloat16)
+    w = torch.randint(-4, 5, (E, F, D), generator=gen, device=DEV).to(torch.bfloat16)
+    chosen = torch.randint(-1, E, (T, 1), generator=gen, device=DEV, dtype=torch.int32)
+    dy = torch.randint(-1, 2, (T, 1, F), generator=gen, device=DEV).to(torch.bfloat16)
+    y = product(experts, x, w, chosen)
+    dx, dw = gradient(experts, x, w, chosen, dy, dw_kind=torch.float32)
+    want_dw = torch.zeros(E, F, D, dtype=torch.float64, device=DEV)
+    for rows in torch.arange(T, device=DEV).split(60_000):
+        part, of = x[rows].float(), chosen[rows, 0]
+        for e in range(-1, E):
+            mine = of == e
+            if e < 0:
+                assert not y[rows, 0][mine].any() and not dx[rows][mine].any()
+                continue
+            assert torch.equal(y[rows, 0][mine], (part[mine] @ w[e].float().t()).to(torch.bfloat16))
+            assert torch.equal(dx[rows][mine], (dy[rows, 0][mine].float() @ w[e].float()).to(torch.bfloat16))
+            want_dw[e] += (dy[rows, 0][mine].float().t() @ part[mine]).double()
+    assert torch.equal(dw.double(), want_dw)
