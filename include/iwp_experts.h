@@ -67,7 +67,7 @@ int iwp_route_gradient(const void* x, int64_t ld_x, uint32_t tokens, uint32_t ex
  * All of one type, sums in binary32, rounded once.  Matrices of experts without rows are not read.  An infinity or a NaN in a row, or in an
  * expert's matrix, shows in what depends on it by the definition, where an infinity may also make NaN, and nowhere else.
  * Workspace: iwp_expert_product_workspace_bytes with the same sizes, 256-byte aligned; it has room for the rows gathered by expert
- * and, where w's rows cannot be read by 16 bytes where they lie (address, ld_w, step_w and in), for a copy of w.
+ * and, where the rows of a w of 16 bits cannot be read by 16 bytes where they lie (address, ld_w, step_w and in), for a copy of w.
  * IWP_EINVAL: sizes of 0 (tokens may be 0) or above the limits (IWP_MAX_TOKENS, IWP_MAX_ROWS slots, IWP_MAX_EXPERTS, IWP_MAX_DIM for in and
  * out; rows times a width, and elements of all matrices, of some 2^36 and more, which no launch takes), slots above experts, pointers missing, rows that overlap (ld below the width; step below out rows); IWP_EALIGN: a
  * buffer not aligned to its elements, or the workspace; IWP_ERANGE: rows that lie 2^24 bytes or more apart. */

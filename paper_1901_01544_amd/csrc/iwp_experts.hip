@@ -124,6 +124,18 @@ bool readable(const void* w, int64_t ld, int64_t step, uint32_t in, uint32_t dty
     return aligned(w, 16) && ld % chunk == 0 && step % chunk == 0 && in % chunk == 0;
 }
 
+// Matrices that the tiles cannot load by 16 bytes a lane are copied to rows of whole units first, except for binary32's, whose entries are a load's
+// least width: there tiles load them by 4 bytes.  us of a call with the copy and without: 2050 rows of 17 x 1001 x 777 85 and 68; both gradients of 256 rows
+// of 16 x 2047 x 2048 354 and 260.
+bool copies_matrices(const void* w, int64_t ld, int64_t step, uint32_t in, uint32_t dtype) { return dtype != IWP_F32 && !readable(w, ld, step, in, dtype); }
+// f(constant with the bytes of a matrix that a lane loads)
+template <class K, class F>
+int with_lane(bool by_chunks, F f) {
+    if constexpr (K::OUT == OUT_F32)
+        if (!by_chunks) return f(std::integral_constant<int, 4>{});
+    return f(std::integral_constant<int, 16>{});
+}
+
 // One workgroup arranges up to 2048 slots; more are counted first and arranged by up to 64, each of which reads all the others' counts, 1024
 // slots or more each.  us of counting and arranging: 2042 slots by one 10, by two 16; 4096 by one 13, by four 16 (a call with small products 14.5 and
 // 13.8); 16384 of 8 experts by 4 21, by 16 17.  Beside a copy of the matrices, which takes longer, one workgroup is enough for more.
@@ -311,7 +323,7 @@ size_t iwp_expert_product_workspace_bytes(uint32_t tokens, uint32_t slots, uint3
                                           int64_t ld_w, int64_t step_w, uint32_t x_by_slot, uint32_t gradient) {
     const ProductSizes z{tokens, slots, experts, in, out, dtype, x_by_slot != 0, gradient != 0};
     if (!z.ok()) return 0;
-    const ProductPlan p = product_plan(z, !readable(w, ld_w, step_w, in, dtype), nullptr);
+    const ProductPlan p = product_plan(z, copies_matrices(w, ld_w, step_w, in, dtype), nullptr);
     return launches_fit(z, p) ? p.bytes : 0;
 }
 
@@ -325,7 +337,7 @@ int iwp_expert_product(const void* x, int64_t ld_x, uint32_t x_by_slot, const vo
     const size_t e = size_of(dtype);
     if (!aligned(x, e) || !aligned(w, e) || !aligned(y, e) || !aligned(chosen, 4) || !aligned(workspace, 256)) return IWP_EALIGN;
     if (tokens == 0) return IWP_OK;
-    const ProductPlan p = product_plan(z, !readable(w, ld_w, step_w, in, dtype), workspace);
+    const ProductPlan p = product_plan(z, copies_matrices(w, ld_w, step_w, in, dtype), workspace);
     if (!workspace || workspace_bytes < p.bytes) return IWP_EWORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     return with_kind(dtype, [&](auto kind) {
@@ -351,13 +363,15 @@ int iwp_expert_product(const void* x, int64_t ld_x, uint32_t x_by_slot, const vo
         int rc = arrange<SIZE>(z, p, chosen, w, ld_w, step_w, true, &W, copy, s);
         if (!rc && !X.slots) rc = gather<SIZE>(z, p, gather_of(z, x, ld_x, in, per_row, p.x, p.ld_x), RowsGather{}, s);
         if (rc) return rc;
-        return with_tile_of<K>(p.tile, [&](auto tile) {
-            typedef decltype(tile) T;
-            auto kernel = X.slots ? k_expert_rows<typename K::E, T::BP, T::BQ, T::WP, T::WQ, K::OUT, false>
-                                  : k_expert_rows<typename K::E, T::BP, T::BQ, T::WP, T::WQ, K::OUT, true>;
-            const uint32_t more = T::BQ == Big::BQ ? MOST_HALVES : 0;
-            IWP_LAUNCH_BLOCK("k_expert_rows", kernel, (out + T::BP - 1) / T::BP * p.max_tiles + more, T::THREADS, s, W, X, p.R, experts, Y);
-            return (int)IWP_OK;
+        return with_lane<K>(readable(w, ld_w, step_w, in, dtype), [&](auto lane) {
+            return with_tile_of<K>(p.tile, [&](auto tile) {
+                typedef decltype(tile) T;
+                auto kernel = X.slots ? k_expert_rows<typename K::E, T::BP, T::BQ, T::WP, T::WQ, K::OUT, false, decltype(lane)::value>
+                                      : k_expert_rows<typename K::E, T::BP, T::BQ, T::WP, T::WQ, K::OUT, true, decltype(lane)::value>;
+                const uint32_t more = T::BQ == Big::BQ ? MOST_HALVES : 0;
+                IWP_LAUNCH_BLOCK("k_expert_rows", kernel, (out + T::BP - 1) / T::BP * p.max_tiles + more, T::THREADS, s, W, X, p.R, experts, Y);
+                return (int)IWP_OK;
+            });
         });
     });
 }
@@ -378,7 +392,7 @@ int iwp_expert_product_gradient(const void* x, int64_t ld_x, uint32_t x_by_slot,
         !aligned(workspace, 256))
         return IWP_EALIGN;
     if ((tokens == 0 || !dx) && !dw) return IWP_OK;
-    const ProductPlan p = product_plan(z, !readable(w, ld_w, step_w, in, dtype), workspace);
+    const ProductPlan p = product_plan(z, copies_matrices(w, ld_w, step_w, in, dtype), workspace);
     if (!workspace || workspace_bytes < p.bytes) return IWP_EWORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     return with_kind(dtype, [&](auto kind) {
@@ -392,14 +406,16 @@ int iwp_expert_product_gradient(const void* x, int64_t ld_x, uint32_t x_by_slot,
         if (rc) return rc;
         // out_x, out_w: constants with the types of what the kernel writes
         auto products = [&](auto out_x, auto out_w) {
-            return with_tile_of<K>(p.tile, [&](auto tile) {
-                typedef decltype(tile) T;
-                auto kernel = k_expert_gradients<typename K::E, T::BP, T::BQ, T::WP, T::WQ, decltype(out_x)::value, decltype(out_w)::value>;
-                const RowsOut rows = p.sums ? RowsOut{reinterpret_cast<char*>(p.sums), (int64_t)p.ld_x} : RowsOut{static_cast<char*>(dx), ld_dx};
-                const uint32_t tiles = dx ? (in + T::BP - 1) / T::BP * p.max_tiles : 0, matrices = dw ? (uint32_t)(experts * tiles_of<T>(in, out)) : 0;
-                IWP_LAUNCH_BLOCK("k_expert_gradients", kernel, ((tiles + 7) / 8 + (matrices + 7) / 8) * 8, T::THREADS, s, W, X, D, p.R, experts, rows,
-                                 dx && tokens, (MatricesOut{static_cast<char*>(dw), ld_dw, step_dw}), matrices);
-                return (int)IWP_OK;
+            return with_lane<K>(readable(w, ld_w, step_w, in, dtype), [&](auto lane) {
+                return with_tile_of<K>(p.tile, [&](auto tile) {
+                    typedef decltype(tile) T;
+                    auto kernel = k_expert_gradients<typename K::E, T::BP, T::BQ, T::WP, T::WQ, decltype(out_x)::value, decltype(out_w)::value, decltype(lane)::value>;
+                    const RowsOut rows = p.sums ? RowsOut{reinterpret_cast<char*>(p.sums), (int64_t)p.ld_x} : RowsOut{static_cast<char*>(dx), ld_dx};
+                    const uint32_t tiles = dx ? (in + T::BP - 1) / T::BP * p.max_tiles : 0, matrices = dw ? (uint32_t)(experts * tiles_of<T>(in, out)) : 0;
+                    IWP_LAUNCH_BLOCK("k_expert_gradients", kernel, ((tiles + 7) / 8 + (matrices + 7) / 8) * 8, T::THREADS, s, W, X, D, p.R, experts, rows,
+                                     dx && tokens, (MatricesOut{static_cast<char*>(dw), ld_dw, step_dw}), matrices);
+                    return (int)IWP_OK;
+                });
             });
         };
         constexpr std::integral_constant<int, K::OUT> own{};

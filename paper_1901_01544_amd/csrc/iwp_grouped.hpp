@@ -336,10 +336,10 @@ __device__ __forceinline__ void store_tile(const M& mm, char* lds, uint32_t p0, 
 
 // Every expert's rows times its matrix (TRANSPOSED: W, not W^T, as for the rows' gradient), to the slots' rows of the output; zeros for
 // slots of nobody.  at: which of the np x nq tiles, in an order in which some dozens in a row share few rows and columns.
-template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool TRANSPOSED, bool GATHERED>
+template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool TRANSPOSED, bool GATHERED, int W_LANE = 16>
 __device__ __forceinline__ void rows_tile(const Matrices& W, const Packed& X, const ExpertRows& R, uint32_t experts, const RowsOut& Y, uint32_t at, uint32_t np,
                                           uint32_t nq, char* lds, uint32_t down = 0) {
-    typedef Product<E, BP, BQ, WP, WQ, TRANSPOSED, false> M;
+    typedef Product<E, BP, BQ, WP, WQ, TRANSPOSED, false, W_LANE> M;
     const uint32_t columns = TRANSPOSED ? W.columns : W.rows;
     constexpr uint32_t TALL = 8;
     const uint32_t group = at / (np * TALL), rest = at - group * np * TALL, tall = min(TALL, nq - group * TALL);
@@ -368,7 +368,7 @@ __device__ __forceinline__ void rows_tile(const Matrices& W, const Packed& X, co
         return Y.y + (int64_t)R.slot[start + tile.first + q] * Y.ld * SIZE;
     });
 }
-template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool GATHERED>
+template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool GATHERED, int W_LANE>
 __global__ void __launch_bounds__(WP * WQ * 64) k_expert_rows(Matrices W, Packed X, ExpertRows R, uint32_t experts, RowsOut Y) {
     __shared__ __align__(1024) char lds[Product<E, BP, BQ, WP, WQ, false, false>::LDS];
     const uint32_t np = (W.rows + BP - 1) / BP, nq = uniform(*R.tiles);
@@ -380,9 +380,9 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_expert_rows(Matrices W, Packed
             rows_tile<E, BP, BQ / 2, 4, 2, OUT, false, GATHERED>(W, X, R, experts, Y, part.tile, np, nq, lds, (part.half - 1) * (BQ / 2));
             return;
         }
-        rows_tile<E, BP, BQ, WP, WQ, OUT, false, GATHERED>(W, X, R, experts, Y, stretch_place(part.tile, whole), np, nq, lds);
+        rows_tile<E, BP, BQ, WP, WQ, OUT, false, GATHERED, W_LANE>(W, X, R, experts, Y, stretch_place(part.tile, whole), np, nq, lds);
     } else if (blockIdx.x < np * nq) {
-        rows_tile<E, BP, BQ, WP, WQ, OUT, false, GATHERED>(W, X, R, experts, Y, stretch_place(blockIdx.x, np * nq), np, nq, lds);
+        rows_tile<E, BP, BQ, WP, WQ, OUT, false, GATHERED, W_LANE>(W, X, R, experts, Y, stretch_place(blockIdx.x, np * nq), np, nq, lds);
     }
 }
 
@@ -493,7 +493,7 @@ __device__ __forceinline__ void matrix_tile(const Packed& X, const Packed& D, co
 // rows, matrices: whether the rows' gradient is wanted; the tiles of the matrices'.  Experts have more and fewer rows, so the dies take the
 // matrices' neighbouring tiles in turn: with a stretch of the experts each, the die with the liked ones is the last (8 experts of 2048 x 4096, 16384
 // rows: 411 us instead of 275; 64 of 2048 x 1024, 65536 rows: 458 and 400).
-template <class E, int BP, int BQ, int WP, int WQ, int OUT_X, int OUT_W>
+template <class E, int BP, int BQ, int WP, int WQ, int OUT_X, int OUT_W, int W_LANE>
 __global__ void __launch_bounds__(WP * WQ * 64) k_expert_gradients(Matrices W, Packed X, Packed D, ExpertRows R, uint32_t experts, RowsOut dx, bool rows,
                                                                    MatricesOut dw, uint32_t matrices) {
     __shared__ __align__(1024) char lds[Product<E, BP, BQ, WP, WQ, true, true>::LDS];
@@ -503,7 +503,7 @@ __global__ void __launch_bounds__(WP * WQ * 64) k_expert_gradients(Matrices W, P
     const uint32_t before = (uint32_t)((uint64_t)i * eights / all), after = (uint32_t)((uint64_t)(i + 1) * eights / all);
     if (after > before) {
         const uint32_t at = before * 8 + die;
-        if (at < np * nq) rows_tile<E, BP, BQ, WP, WQ, OUT_X, true, true>(W, D, R, experts, dx, stretch_place(at, np * nq), np, nq, lds);
+        if (at < np * nq) rows_tile<E, BP, BQ, WP, WQ, OUT_X, true, true, W_LANE>(W, D, R, experts, dx, stretch_place(at, np * nq), np, nq, lds);
     } else {
         const uint32_t at = (i - before) * 8 + die;
         if (at < matrices) matrix_tile<E, BP, BQ, WP, WQ, OUT_W>(X, D, R, dw, at, lds);

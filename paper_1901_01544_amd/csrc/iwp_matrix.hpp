@@ -113,11 +113,14 @@ struct Operand {
     uint32_t summed;       // valid entries of the summed one
 };
 
-// 16 bytes per lane from `base` + the lane's offset straight to LDS, lane after lane from `lds` (uniform) on.  In assembly,
+// 16 bytes (or 4) per lane from `base` + the lane's offset straight to LDS, lane after lane from `lds` (uniform) on.  In assembly,
 // because the compiler waits for such loads before any transposing read, of whichever tile; wait_for_loads() waits for them.
 // (m0 is no register that the compiler keeps anything in: it sets it where an instruction of its own needs it.)
+template <int BYTES = 16>
 __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
+    static_assert(BYTES == 16 || BYTES == 4, "a lane's bytes");
+    if (BYTES == 4) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
+    else asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
 }
 // Until at most LEFT of this wavefront's loads are on their way and all of its LDS reads are done.
 template <int LEFT>
@@ -148,11 +151,14 @@ struct InOrder {
 // Entries past the operand's extent are read from a valid one: what they contribute to is never stored.  Summed entries past
 // an operand's end are read from the same row, or from its last row; of the two operands one always reaches to a multiple of BK
 // and holds zeros there.
-template <int R, int WAVES, bool COLUMNS, int SIZE = 2>
+// LANE: bytes that a lane loads at once.  By 16, rows begin at multiples of 16 bytes and are whole chunks wide; by an entry of 4, they may begin and
+// end at any.
+template <int R, int WAVES, bool COLUMNS, int SIZE = 2, int LANE = 16>
 struct Tile {
     static constexpr int BYTES = R * ROW_BYTES, CHUNK = 16 / SIZE;
-    static constexpr int LOADS = BYTES / 1024 / WAVES;      // 64 lanes of 16 bytes each
-    static_assert(LOADS * WAVES * 1024 == BYTES, "whole loads");
+    static constexpr int LOADS = BYTES / (64 * LANE) / WAVES, PARTS = 16 / LANE;
+    static_assert(LOADS * WAVES * 64 * LANE == BYTES, "whole loads");
+    static_assert(LANE == 16 || LANE == SIZE, "a chunk or an entry");
     static constexpr int PER_ROW = COLUMNS ? R / CHUNK : ROW_BYTES / 16;
     static constexpr int TURNS = !COLUMNS ? 8 : SIZE == 4 ? 1 : R / 32 < 8 ? R / 32 : 8;
 
@@ -168,14 +174,14 @@ struct Tile {
         row_bytes = o.ld * SIZE;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const uint32_t slot = (wave * LOADS + i) * 64 + lane, row = slot / PER_ROW, place = slot % PER_ROW;
+            const uint32_t load = (wave * LOADS + i) * 64 + lane, slot = load / PARTS, part = load % PARTS, row = slot / PER_ROW, place = slot % PER_ROW;
             if (!COLUMNS) {
                 const uint32_t entry = min(first + row, o.extent - 1) - first, chunk = place ^ turn(row);
-                within[i] = chunk * CHUNK;
-                at[i] = entry * row_bytes + chunk * 16;
+                within[i] = chunk * CHUNK + part;
+                at[i] = entry * row_bytes + chunk * 16 + part * LANE;
             } else {
-                const uint32_t chunk = (((place >> 2) ^ turn(row)) << 2) | (place & 3u);
-                const uint32_t entry = first + chunk * CHUNK < o.extent ? chunk * CHUNK : 0u;
+                const uint32_t chunk = (((place >> 2) ^ turn(row)) << 2) | (place & 3u), mine = chunk * CHUNK + part;
+                const uint32_t entry = first + mine < o.extent ? mine : 0u;
                 within[i] = row;
                 at[i] = entry * SIZE + row * row_bytes;
             }
@@ -184,7 +190,7 @@ struct Tile {
     // The same of rows that lie anywhere, from the matrix's first one on
     template <class Rows>
     __device__ __forceinline__ void init_anywhere(const Operand& o, uint32_t first, int wave, int lane, const Rows& row_of) {
-        static_assert(!COLUMNS, "rows");
+        static_assert(!COLUMNS && PARTS == 1, "rows, by 16 bytes");
         row_bytes = o.ld * SIZE;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
@@ -200,7 +206,7 @@ struct Tile {
     // The i-th load; left: summed entries from the tile's first on (at least 1)
     __device__ __forceinline__ void load(int i, const char* from, uint32_t left, uint32_t lds, int wave) const {
         const uint32_t inside = COLUMNS ? at[i] - (within[i] - (left - 1)) * row_bytes : at[i] - within[i] * SIZE;
-        load_to_lds(from, within[i] < left ? at[i] : inside, lds + (wave * LOADS + i) * 1024);
+        load_to_lds<LANE>(from, within[i] < left ? at[i] : inside, lds + (wave * LOADS + i) * (64 * LANE));
     }
     // Fragment of the 32 entries from `entry` (a multiple of 32) on, bytes 32 s to 32 s + 31 of the summed index: of each half of the
     // wavefront, 16.
@@ -235,11 +241,11 @@ struct Tile {
 // tiles of 32 summed entries instead of two of 64: 8.3, 8.3, 8.15 against 7.8, 7.5, 7.6 (a barrier twice as often costs more than the
 // longer flight of the loads gains).  Wavefronts of 256 x 32, which read half as much LDS again: dH 8.0 to 8.1 against 7.2 to
 // 7.3; of 64 x 128: the same within 1 %.
-template <class E, int BP, int BQ, int WP, int WQ, bool P_COLUMNS, bool Q_COLUMNS>
+template <class E, int BP, int BQ, int WP, int WQ, bool P_COLUMNS, bool Q_COLUMNS, int P_LANE = 16>
 struct Product {
     static constexpr int WAVES = WP * WQ;
     static constexpr int FP = BP / WP / 32, FQ = BQ / WQ / 32;     // fragments of 32 per wavefront
-    typedef Tile<BP, WAVES, P_COLUMNS, E::SIZE> TP;
+    typedef Tile<BP, WAVES, P_COLUMNS, E::SIZE, P_LANE> TP;
     typedef Tile<BQ, WAVES, Q_COLUMNS, E::SIZE> TQ;
     static constexpr uint32_t DEEP = ROW_BYTES / E::SIZE;          // summed entries of a tile
     static constexpr int STAGE = TP::BYTES + TQ::BYTES, LDS = 2 * STAGE;
