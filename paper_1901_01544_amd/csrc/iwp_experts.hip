@@ -170,7 +170,7 @@ ProductPlan product_plan(const ProductSizes& z, bool copy_w, void* workspace) {
     c.take(p.R.count, z.experts + 1);
     c.take(p.R.slot, (size_t)z.padded() + n);
     c.take(p.R.tile, p.max_tiles);
-    c.take(p.R.tiles, 1);
+    c.take(p.R.tiles, 2);
     const size_t size = size_of(z.dtype);
     c.take(p.x, (size_t)z.padded() * p.ld_x * size);
     if (z.gradient) {
@@ -412,8 +412,8 @@ int iwp_expert_product_gradient(const void* x, int64_t ld_x, uint32_t x_by_slot,
                     auto kernel = k_expert_gradients<typename K::E, T::BP, T::BQ, T::WP, T::WQ, decltype(out_x)::value, decltype(out_w)::value, decltype(lane)::value>;
                     const RowsOut rows = p.sums ? RowsOut{reinterpret_cast<char*>(p.sums), (int64_t)p.ld_x} : RowsOut{static_cast<char*>(dx), ld_dx};
                     const uint32_t tiles = dx ? (in + T::BP - 1) / T::BP * p.max_tiles : 0, matrices = dw ? (uint32_t)(experts * tiles_of<T>(in, out)) : 0;
-                    IWP_LAUNCH_BLOCK("k_expert_gradients", kernel, ((tiles + 7) / 8 + (matrices + 7) / 8) * 8, T::THREADS, s, W, X, D, p.R, experts, rows,
-                                     dx && tokens, (MatricesOut{static_cast<char*>(dw), ld_dw, step_dw}), matrices);
+                    IWP_LAUNCH_BLOCK("k_expert_gradients", kernel, ((tiles + 7) / 8 + 1 + (matrices + 7) / 8) * 8, T::THREADS, s, W, X, D, p.R, experts, rows,
+                                     dx && tokens, dx && tokens && !p.sums, (MatricesOut{static_cast<char*>(dw), ld_dw, step_dw}), matrices);
                     return (int)IWP_OK;
                 });
             });

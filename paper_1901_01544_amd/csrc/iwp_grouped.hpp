@@ -27,8 +27,8 @@ struct ExpertRows {        // experts' rows after each other, in the order of sl
     uint32_t* start;       // [experts + 1]
     uint32_t* count;       // [experts + 1]
     uint32_t* slot;        // [padded rows] which slot a row is, NOBODY behind an expert's rows
-    ExpertTile* tile;      // the rows in tiles, those of nobody too
-    uint32_t* tiles;       // [1]
+    ExpertTile* tile;      // the experts' rows in tiles
+    uint32_t* tiles;       // [2]: of the experts, of nobody
     uint32_t* counts;      // [workgroups that arrange, experts + 1]: slots of each one's part
 };
 
@@ -124,7 +124,7 @@ __device__ __forceinline__ void arrange_slots(const int32_t* __restrict__ chosen
         if (blockIdx.x == 0) {
             R.start[e] = start;
             R.count[e] = count;
-            for (uint32_t t = 0; t * height < count; ++t) R.tile[first_tile + t] = ExpertTile{e, t * height};
+            for (uint32_t t = 0; e < experts && t * height < count; ++t) R.tile[first_tile + t] = ExpertTile{e, t * height};
         }
         uint32_t to = start + before;
         for (uint32_t w = 0; w < ARRANGE_WAVES; ++w) {
@@ -141,7 +141,7 @@ __device__ __forceinline__ void arrange_slots(const int32_t* __restrict__ chosen
     }
     if (thread == 0) {
         put(experts, all_rows, none, all_tiles, nobody_of[1]);
-        if (blockIdx.x == 0) *R.tiles = all_tiles + (none + height - 1) / height;
+        if (blockIdx.x == 0) R.tiles[0] = all_tiles, R.tiles[1] = (none + height - 1) / height;
     }
     __syncthreads();
     for (uint32_t base = part.from; base < part.to; base += 64) {
@@ -334,11 +334,11 @@ __device__ __forceinline__ void store_tile(const M& mm, char* lds, uint32_t p0, 
     }
 }
 
-// Every expert's rows times its matrix (TRANSPOSED: W, not W^T, as for the rows' gradient), to the slots' rows of the output; zeros for
-// slots of nobody.  at: which of the np x nq tiles, in an order in which some dozens in a row share few rows and columns.
+// Every expert's rows times its matrix (TRANSPOSED: W, not W^T, as for the rows' gradient), to the slots' rows of the output.
+// at: which of the np x nq tiles, in an order in which some dozens in a row share few rows and columns.
 template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool TRANSPOSED, bool GATHERED, int W_LANE = 16>
-__device__ __forceinline__ void rows_tile(const Matrices& W, const Packed& X, const ExpertRows& R, uint32_t experts, const RowsOut& Y, uint32_t at, uint32_t np,
-                                          uint32_t nq, char* lds, uint32_t down = 0) {
+__device__ __forceinline__ void rows_tile(const Matrices& W, const Packed& X, const ExpertRows& R, const RowsOut& Y, uint32_t at, uint32_t np, uint32_t nq,
+                                          char* lds, uint32_t down = 0) {
     typedef Product<E, BP, BQ, WP, WQ, TRANSPOSED, false, W_LANE> M;
     const uint32_t columns = TRANSPOSED ? W.columns : W.rows;
     constexpr uint32_t TALL = 8;
@@ -348,42 +348,56 @@ __device__ __forceinline__ void rows_tile(const Matrices& W, const Packed& X, co
     tile = ExpertTile{uniform(tile.expert), uniform(tile.first) + down};
     const uint32_t count = uniform(R.count[tile.expert]), start = uniform(R.start[tile.expert]);
     if (tile.first >= count) return;                       // (a lower part of the tile)
+    const uint32_t summed = TRANSPOSED ? W.rows : W.columns, to = (summed + M::DEEP - 1) / M::DEEP * M::DEEP;
+    const Operand P{uniform(W.w + tile.expert * W.step * E::SIZE), nullptr, W.ld, columns, summed};
+    const Operand Q{uniform(GATHERED ? X.x + (size_t)start * X.ld * E::SIZE : X.x), nullptr, X.ld, count, to};
     M mm;
-    if (tile.expert < experts) {
-        const uint32_t summed = TRANSPOSED ? W.rows : W.columns;
-        const Operand P{uniform(W.w + tile.expert * W.step * E::SIZE), nullptr, W.ld, columns, summed};
-        const uint32_t to = (summed + M::DEEP - 1) / M::DEEP * M::DEEP;
-        const Operand Q{uniform(GATHERED ? X.x + (size_t)start * X.ld * E::SIZE : X.x), nullptr, X.ld, count, to};
-        if constexpr (GATHERED) mm.run(P, Q, tp * BP, tile.first, 0, to, lds);
-        else mm.run(P, Q, tp * BP, tile.first, 0, to, lds, SlotRows{R.slot + start, X.slots});
-    } else {
-#pragma unroll
-        for (int a = 0; a < M::FP; ++a)
-#pragma unroll
-            for (int b = 0; b < M::FQ; ++b) mm.acc[a][b] = f32x16{};
-    }
+    if constexpr (GATHERED) mm.run(P, Q, tp * BP, tile.first, 0, to, lds);
+    else mm.run(P, Q, tp * BP, tile.first, 0, to, lds, SlotRows{R.slot + start, X.slots});
     constexpr uint32_t SIZE = OUT == OUT_F32 ? 4 : 2;
     store_tile<M, OUT, BP, WP>(mm, lds, tp * BP, columns, [&](uint32_t q) -> char* {
         if (tile.first + q >= count) return nullptr;
         return Y.y + (int64_t)R.slot[start + tile.first + q] * Y.ld * SIZE;
     });
 }
+// Zeros for the slots of nobody, a tile of their rows and the output's columns.  They come after the experts' tiles, which all dies share: in one order
+// with these, dies with nobody's stretch would have nothing to multiply (an eighth of 65536 slots given, 8 experts of 2048 x 1024, bf16: 219 us
+// instead of 72).
+template <int BP, int BQ, int THREADS, int OUT>
+__device__ __forceinline__ void nobody_tile(const ExpertRows& R, uint32_t experts, const RowsOut& Y, uint32_t at, uint32_t np, uint32_t columns) {
+    constexpr uint32_t SIZE = OUT == OUT_F32 ? 4 : 2, CHUNK = 16 / SIZE, CHUNKS = BP / CHUNK;
+    const uint32_t count = R.count[experts], p0 = at % np * BP, first = at / np * BQ;
+    const uint32_t* slot = R.slot + R.start[experts];
+    for (uint32_t i = threadIdx.x; i < BQ * CHUNKS; i += THREADS) {
+        const uint32_t row = first + i / CHUNKS, p = p0 + i % CHUNKS * CHUNK;
+        if (row >= count || p >= columns) continue;
+        const int64_t to = slot[row] * Y.ld + p;
+        if (p + CHUNK <= columns) {
+            *reinterpret_cast<words4_any*>(Y.y + to * SIZE) = words4_any{};
+        } else {
+            for (uint32_t e = 0; p + e < columns; ++e) put<OUT>(Y.y, to + e, 0.0f);
+        }
+    }
+}
 template <class E, int BP, int BQ, int WP, int WQ, int OUT, bool GATHERED, int W_LANE>
 __global__ void __launch_bounds__(WP * WQ * 64) k_expert_rows(Matrices W, Packed X, ExpertRows R, uint32_t experts, RowsOut Y) {
     __shared__ __align__(1024) char lds[Product<E, BP, BQ, WP, WQ, false, false>::LDS];
-    const uint32_t np = (W.rows + BP - 1) / BP, nq = uniform(*R.tiles);
+    const uint32_t np = (W.rows + BP - 1) / BP, nq = uniform(R.tiles[0]), n = np * nq;
+    uint32_t after = blockIdx.x - n;
     if constexpr (BQ == 256) {                             // large tiles fill a compute unit each
         TilePart part;
         uint32_t whole;
-        if (!part_of(blockIdx.x, np * nq, &part, &whole)) return;
-        if (part.half) {
-            rows_tile<E, BP, BQ / 2, 4, 2, OUT, false, GATHERED>(W, X, R, experts, Y, part.tile, np, nq, lds, (part.half - 1) * (BQ / 2));
+        if (part_of(blockIdx.x, n, &part, &whole)) {
+            if (part.half) rows_tile<E, BP, BQ / 2, 4, 2, OUT, false, GATHERED, W_LANE>(W, X, R, Y, part.tile, np, nq, lds, (part.half - 1) * (BQ / 2));
+            else rows_tile<E, BP, BQ, WP, WQ, OUT, false, GATHERED, W_LANE>(W, X, R, Y, stretch_place(part.tile, whole), np, nq, lds);
             return;
         }
-        rows_tile<E, BP, BQ, WP, WQ, OUT, false, GATHERED, W_LANE>(W, X, R, experts, Y, stretch_place(part.tile, whole), np, nq, lds);
-    } else if (blockIdx.x < np * nq) {
-        rows_tile<E, BP, BQ, WP, WQ, OUT, false, GATHERED, W_LANE>(W, X, R, experts, Y, stretch_place(blockIdx.x, np * nq), np, nq, lds);
+        after -= n - whole;                                // a workgroup more for each that was halved
+    } else if (blockIdx.x < n) {
+        rows_tile<E, BP, BQ, WP, WQ, OUT, false, GATHERED, W_LANE>(W, X, R, Y, stretch_place(blockIdx.x, n), np, nq, lds);
+        return;
     }
+    if (after < np * uniform(R.tiles[1])) nobody_tile<BP, BQ, WP * WQ * 64, OUT>(R, experts, Y, after, np, W.rows);
 }
 
 // Products of few rows, in one launch, without arranging anything: a workgroup has 16 rows of an expert's matrix, each of its wavefronts a
@@ -490,20 +504,24 @@ __device__ __forceinline__ void matrix_tile(const Packed& X, const Packed& D, co
 }
 
 // Both gradients in one launch, eights of tiles of either in turn, so that tiles that write and tiles that multiply run at the same time.
-// rows, matrices: whether the rows' gradient is wanted; the tiles of the matrices'.  Experts have more and fewer rows, so the dies take the
+// rows, nobodys, matrices: whether the rows' gradient is wanted, and zeros in nobody's; the tiles of the matrices'.  Experts have more and fewer rows, so the dies take the
 // matrices' neighbouring tiles in turn: with a stretch of the experts each, the die with the liked ones is the last (8 experts of 2048 x 4096, 16384
 // rows: 411 us instead of 275; 64 of 2048 x 1024, 65536 rows: 458 and 400).
 template <class E, int BP, int BQ, int WP, int WQ, int OUT_X, int OUT_W, int W_LANE>
 __global__ void __launch_bounds__(WP * WQ * 64) k_expert_gradients(Matrices W, Packed X, Packed D, ExpertRows R, uint32_t experts, RowsOut dx, bool rows,
-                                                                   MatricesOut dw, uint32_t matrices) {
+                                                                   bool nobodys, MatricesOut dw, uint32_t matrices) {
     __shared__ __align__(1024) char lds[Product<E, BP, BQ, WP, WQ, true, true>::LDS];
-    const uint32_t np = (W.columns + BP - 1) / BP, nq = rows ? uniform(*R.tiles) : 0;
+    const uint32_t np = (W.columns + BP - 1) / BP, nq = rows ? uniform(R.tiles[0]) : 0;
     const uint32_t eights = (np * nq + 7) / 8, others = (matrices + 7) / 8, all = eights + others, i = blockIdx.x / 8, die = blockIdx.x % 8;
-    if (i >= all) return;
+    if (i >= all) {
+        const uint32_t after = (i - all) * 8 + die;
+        if (nobodys && after < np * uniform(R.tiles[1])) nobody_tile<BP, BQ, WP * WQ * 64, OUT_X>(R, experts, dx, after, np, W.columns);
+        return;
+    }
     const uint32_t before = (uint32_t)((uint64_t)i * eights / all), after = (uint32_t)((uint64_t)(i + 1) * eights / all);
     if (after > before) {
         const uint32_t at = before * 8 + die;
-        if (at < np * nq) rows_tile<E, BP, BQ, WP, WQ, OUT_X, true, true, W_LANE>(W, D, R, experts, dx, stretch_place(at, np * nq), np, nq, lds);
+        if (at < np * nq) rows_tile<E, BP, BQ, WP, WQ, OUT_X, true, true, W_LANE>(W, D, R, dx, stretch_place(at, np * nq), np, nq, lds);
     } else {
         const uint32_t at = (i - before) * 8 + die;
         if (at < matrices) matrix_tile<E, BP, BQ, WP, WQ, OUT_W>(X, D, R, dw, at, lds);

@@ -75,6 +75,21 @@ def test_uneven_experts(experts, kind):
 
 @pytest.mark.parametrize("kind", TYPES, ids=str)
 @pytest.mark.parametrize("by_slot", [False, True])
+@pytest.mark.parametrize("size,nobody", [((700, 4, 8, 96, 130), 0.875), ((3000, 4, 8, 129, 96), 0.875), ((9000, 2, 4, 128, 2304), 0.7), ((2500, 1, 2, 64, 333), 0.9)], ids=str)
+def test_most_slots_are_nobodys(experts, size, nobody, kind, by_slot):
+    """As where a rank has an eighth of the experts, with small, middling and large tiles: zeros behind the experts' tiles, in every row of nobody."""
+    x, w, chosen, dy = inputs(*size, kind, by_slot, nobody)
+    ref = Experts(x, w, chosen, dy)
+    y = product(experts, x, w, chosen)
+    ref.check(y)
+    assert (y[chosen < 0] == 0).all()
+    dx, dw = gradient(experts, x, w, chosen, dy)
+    ref.check_gradient(dx, dw)
+    assert (dx[(chosen < 0) if by_slot else (chosen < 0).all(1)] == 0).all()
+
+
+@pytest.mark.parametrize("kind", TYPES, ids=str)
+@pytest.mark.parametrize("by_slot", [False, True])
 def test_no_rows_at_all(experts, kind, by_slot):
     x, w, chosen, dy = inputs(40, 2, 6, 64, 80, kind, by_slot)
     x.fill_(float("nan")), w.fill_(float("nan")), dy.fill_(float("nan"))
