@@ -3,7 +3,7 @@
 // Bound by memory: a gradient is read for its norm and read again to be scaled and written, 12 bytes an element where 8 cannot be
 // done without; what the memory-side cache still has of it is not read twice (see LONG_BYTES).  A wavefront takes a chunk of 2048 elements at a
 // time, eight loads of 16 bytes a lane on their way.  Squares are exact in binary64, sums in a fixed order: lane, wavefront, workgroup,
-// then the worker's workgroups.  8 workers of 61 M elements: 931 us, 6.3 TB/s of 12 bytes an element; norms alone 323 us, 6.0 TB/s.
+// then the worker's workgroups.  8 workers of 61 M elements: 935 us, 6.3 TB/s of 12 bytes an element; norms alone 323 us, 6.0 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -190,7 +190,7 @@ constexpr uint32_t GRID = 2048;            // 256 threads each: what the compute
 constexpr uint32_t ONE_CHUNKS = 64;        // four a wavefront of the one workgroup
 
 // Where the memory-side cache (256 MiB) ends.  us for 8 workers of 61 M elements: norms and products of all workers after each other 1084; what
-// is written past the cache 1065, what is read last too 996; a worker at a time, whose gradient the cache then has part of, 931.  8 x 25 M:
+// is written past the cache 1065, what is read last too 996; a worker at a time, whose gradient the cache then has part of, 935.  8 x 25 M:
 // all after each other, past the cache, 380, in fours 410.  8 x 8 M, which the cache holds: 115, reading past it 120.  Norms alone of 8 x 61 M: 323,
 // a worker at a time 372.
 constexpr uint64_t CACHE_BYTES = 256ull << 20, LONG_BYTES = 160ull << 20;
