@@ -25,17 +25,17 @@ typedef enum { IWP_SOFTMAX = 0, IWP_SIGMOID = 1 } iwp_scores;
 /* ------------------------------------------------------------------ the choice */
 
 /* Chooses `slots` experts for every token from a router's logits.  x: [tokens, experts]; with s = softmax(x) over
- * the token's experts or 1 / (1 + exp(-x)), and bias: [experts] binary32, or NULL for zeros:
- *   c_e        = s_e + bias_e, by which experts are chosen, in binary64 (without a bias: by the logits themselves, in
- *                whose order the scores are)
+ * the token's experts or 1 / (1 + exp(-x)), and bias: [experts] binary32, or NULL:
+ *   c_e        by which experts are chosen: s_e + bias_e in binary64, without a bias the logit x_e, in whose order the scores are
+ *                (also where binary64 does not tell them apart)
  *   groups     the experts in `groups` equal runs, of which a token may use the top_groups with the largest sum of their
- *                group_top (1 or 2) largest c
+ *                group_top (1 or 2) largest c; without a bias two of a group are added as scores, in binary64
  *   chosen[k]  the experts with the largest c there, the largest first; among equals (of experts and of groups) the lower index
  *   weight[k]  scale * s_e of the k-th, with `renormalise` scale * s_e / (sum of s over the token's chosen experts); the bias has no part in it
  * Experts whose logit is -inf or NaN or whose c is -inf or NaN are never chosen; slots that are left over hold -1 and weight 0, and
  * so do all slots of tokens with keep[i] == 0 (keep: [tokens] bytes, NULL = every token counts).  A token with a NaN among its logits has
  * weights of NaN.  A logit of +inf makes a softmax NaN, as by the definition; such a token's weights are NaN, its choice without a bias is
- * by the logits' order.
+ * by the logits' order, but where groups go by two scores there is none.
  * chosen: [tokens, slots] int32, weight: [tokens, slots] binary32, packed: `chosen` is what iwp_balance and
  * iwp_expert_product take.  No workspace.
  * IWP_EINVAL: experts of 0 or above IWP_MAX_EXPERTS, tokens above IWP_MAX_TOKENS (0 tokens: nothing is done), groups that do not divide the

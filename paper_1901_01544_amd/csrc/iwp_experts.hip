@@ -269,24 +269,25 @@ int iwp_route(const void* x, int64_t ld_x, uint32_t tokens, uint32_t experts, ui
     if (!aligned(x, size_of(dtype)) || !aligned(bias, 4) || !aligned(chosen, 4) || !aligned(weight, 4)) return IWP_EALIGN;
     if (tokens == 0) return IWP_OK;
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    const bool grouped = top_groups < groups, by_score = bias || (grouped && group_top == 2);
+    const bool grouped = top_groups < groups, scored = bias || (grouped && group_top == 2);
     return with_type(dtype, [&](auto in) {
         return with_lanes<in.value>(experts, [&](uint32_t lanes, auto chunks) {
             constexpr int IN = decltype(in)::value, CHUNKS = decltype(chunks)::value;
             const RouteCall r{x, ld_x, tokens, experts, lanes, slots, bias, scores == IWP_SIGMOID, renormalise != 0, groups, top_groups, group_top,
                               scale, keep, chosen, weight};
             const uint32_t at_once = 64 / lanes, row = experts + groups;
-            const uint32_t lds = round_up<uint32_t>(std::max({lanes >= 16 ? at_once * CANDIDATES * (uint32_t)sizeof(Candidate) : 0u, by_score ? row * 8 : 0u,
+            const uint32_t lds = round_up<uint32_t>(std::max({lanes >= 16 ? at_once * CANDIDATES * (uint32_t)sizeof(Candidate) : 0u, scored ? row * 8 : 0u,
                                                               grouped ? at_once * row * 4 : 0u}), 16);
-            const TokenGrid g(tokens, at_once, lds + at_once * (by_score ? 2 * slots + 1 : slots) * 4);
+            const TokenGrid g(tokens, at_once, lds + at_once * (bias ? 2 * slots + 1 : slots) * 4);
             auto launch = [&](auto kernel) {
                 IWP_LAUNCH_AS("k_route", kernel, g.blocks, g.waves * 64, g.lds, s, r, lds);
                 return (int)IWP_OK;
             };
             auto of_lanes = [&](auto known) {
                 constexpr int LANES = decltype(known)::value;
-                if (by_score) return grouped ? launch(k_route<IN, CHUNKS, LANES, true, true>) : launch(k_route<IN, CHUNKS, LANES, true, false>);
-                return grouped ? launch(k_route<IN, CHUNKS, LANES, false, true>) : launch(k_route<IN, CHUNKS, LANES, false, false>);
+                if (bias) return grouped ? launch(k_route<IN, CHUNKS, LANES, ALL_BY_SCORE, true>) : launch(k_route<IN, CHUNKS, LANES, ALL_BY_SCORE, false>);
+                if (scored) return launch(k_route<IN, CHUNKS, LANES, GROUPS_BY_SCORE, true>);
+                return grouped ? launch(k_route<IN, CHUNKS, LANES, BY_LOGITS, true>) : launch(k_route<IN, CHUNKS, LANES, BY_LOGITS, false>);
             };
             if (CHUNKS == 2 || lanes == 16) return of_lanes(std::integral_constant<int, 16>{});
             return of_lanes(std::integral_constant<int, CHUNKS == 2 ? 16 : 0>{});

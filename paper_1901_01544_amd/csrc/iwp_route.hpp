@@ -1,6 +1,6 @@
 // Kernels of the choice of experts and of its gradient.  A token's experts lie over a part of a wavefront as in the expert balance
 // (TokenLanes), so the logits are read once, and everything about a token happens between its lanes:
-//   c = score + bias, or the logits themselves where their order is the scores' order (no bias, no sums over groups);
+//   c = score + bias, or without a bias the logits themselves, in whose order the scores are (sums over groups are of scores all the same);
 //   groups: best one or two c of every group between the lanes that have it, a group's rank by counting;
 //   slots: the largest c that is left, one after the other, or where there are many lanes all at once (see candidates).
 // Scores decide in binary64, but are computed in binary32 first: where no two c that the choice depends on are closer than twice what
@@ -126,8 +126,8 @@ __device__ __forceinline__ void choose_groups(const RouteCall& r, const P& part,
     lanes_exchange();
 }
 
-// A token in binary64, value by value in LDS.
-template <int IN>
+// A token in binary64, value by value in LDS.  SLOTS_BY_LOGIT: by scores only the groups (there is no bias).
+template <int IN, bool SLOTS_BY_LOGIT>
 __device__ __forceinline__ void route_in_binary64(const RouteCall& r, const Part& part, uint32_t lane, uint32_t i, double from, double* row, int32_t* slot) {
     constexpr double NONE = -INFINITY;
     double sum = 0.0;
@@ -143,12 +143,14 @@ __device__ __forceinline__ void route_in_binary64(const RouteCall& r, const Part
         double s = row[e];
         if (s == NONE) continue;
         if (!r.sigmoid) s /= sum;
-        if (r.bias) s += (double)r.bias[e];
+        if (!SLOTS_BY_LOGIT) s += (double)r.bias[e];
         row[e] = s != s ? NONE : s;
     }
     lanes_exchange();
     double least, next;
     if (r.top_groups < r.groups) choose_groups(r, part, lane, row, &least, &next);
+    if (SLOTS_BY_LOGIT)
+        for (uint32_t e = lane; e < r.experts; e += part.lanes) row[e] = row[e] == NONE ? NONE : (double)element<IN>(r.x, (int64_t)i * r.ld + e);
     for (uint32_t k = 0; k < r.slots; ++k) {
         double best = NONE;
         uint32_t at = 0xffffffffu;
@@ -198,11 +200,16 @@ struct Candidate {
     uint32_t expert;
 };
 
-// BY_SCORE: c is a score and a bias, else the logit.  lds: bytes of a wavefront besides its slots (and their c).
-template <int IN, int CHUNKS, int LANES, bool BY_SCORE, bool GROUPS>
+// What groups and slots go by.  Scores saturate where logits still differ (a sigmoid in binary64 is 1 from 37 on), so slots go by the logits unless a bias is
+// added; two scores of a group are added as they are.
+enum RouteBy { BY_LOGITS, GROUPS_BY_SCORE, ALL_BY_SCORE };
+
+// lds: bytes of a wavefront besides its slots (and their c).
+template <int IN, int CHUNKS, int LANES, RouteBy BY, bool GROUPS>
 __global__ void __launch_bounds__(256) k_route(RouteCall r, uint32_t lds) {
     typedef TokenLanes<IN, CHUNKS> L;
     constexpr float NONE = -INFINITY;
+    constexpr bool BY_SCORE = BY == ALL_BY_SCORE, SCORES = BY != BY_LOGITS;
     extern __shared__ __align__(16) char shared[];
     if (LANES) r.lanes = LANES;
     const L l(r.experts, r.lanes);
@@ -249,7 +256,7 @@ __global__ void __launch_bounds__(256) k_route(RouteCall r, uint32_t lds) {
     float by = 1.0f;                                                            // softmax: 1 / sum of e^(x - m)
     bool close = false;
     float off = 0.0f;
-    if (BY_SCORE) {
+    if (SCORES) {
         if (!r.sigmoid) {
             double sum = 0.0;
 #pragma unroll
@@ -259,7 +266,7 @@ __global__ void __launch_bounds__(256) k_route(RouteCall r, uint32_t lds) {
         float bias[L::N];
 #pragma unroll
         for (int v = 0; v < L::N; ++v) bias[v] = 0.0f;
-        if (r.bias) {
+        if (BY_SCORE && r.bias) {         // always there: without the branch its loads go out early and hold registers (131072 x 256: 80 us, with it 76)
 #pragma unroll
             for (int v = 0; v < L::N; v += 4) {
                 if (l.expert(v) + 4 <= r.experts) {
@@ -340,10 +347,16 @@ __global__ void __launch_bounds__(256) k_route(RouteCall r, uint32_t lds) {
             for (int v = 0; v < L::N; ++v) c[v] = l.expert(v) < r.experts ? row[l.expert(v)] : NONE;
         }
         lanes_exchange();
-        if (BY_SCORE) {
+        if (SCORES) {
             least = -part.max(-least);
             next = part.max(next);
             close |= least != NONE && !(least - next > 4.0f * off);             // sums of two, each off; infinities are close
+        }
+        if (BY == GROUPS_BY_SCORE) {
+            float x[L::N];
+            L::unpack(raw, x);
+#pragma unroll
+            for (int v = 0; v < L::N; ++v) c[v] = c[v] == NONE ? NONE : __builtin_canonicalizef(x[v]);
         }
     }
     // All slots at once: the slots' lanes' largest c bound what can be chosen, and few c are not below that; each of those finds its
@@ -415,10 +428,10 @@ __global__ void __launch_bounds__(256) k_route(RouteCall r, uint32_t lds) {
         }
         lanes_exchange();
     }
-    if (BY_SCORE) {
+    if (SCORES) {
         for (uint64_t again = __ballot(close && in && l.lane == 0); again; again &= again - 1) {
             const uint32_t lane = __ffsll((unsigned long long)again) - 1, token = wave * at_once + lane / r.lanes;
-            route_in_binary64<IN>(r, Part(64), threadIdx.x & 63, base + token, (double)__shfl(from, lane), reinterpret_cast<double*>(own),
+            route_in_binary64<IN, !BY_SCORE>(r, Part(64), threadIdx.x & 63, base + token, (double)__shfl(from, lane), reinterpret_cast<double*>(own),
                                   slot + ((int32_t)token - (int32_t)mine) * (int32_t)r.slots);
         }
     }

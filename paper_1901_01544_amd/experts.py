@@ -41,7 +41,7 @@ def _router(x, chosen):
 
 def route(x, chosen, weight, bias=None, scores: str = "softmax", groups: int = 1, top_groups: int = 0, group_top: int = 1,
           renormalise: bool = False, scale: float = 1.0, keep=None, stream=None):
-    """chosen[i], weight[i]: the experts with the largest score + bias, the largest first, and scale * score of each (renormalise: over the sum of
+    """chosen[i], weight[i]: the experts with the largest score + bias (without a bias: the largest logits), the largest first, and scale * score of each (renormalise: over the sum of
     the token's chosen scores).
 
     x: [tokens, experts] logits; chosen: [tokens, slots] int32; weight: [tokens, slots] float32; scores: 'softmax' or 'sigmoid'; bias: [experts]
