@@ -23,7 +23,7 @@ class Tensors:
         rows = [(int(row[0]), int(row[1])) for row in rows]
         tab = (iwp.Layer * max(1, len(rows)))()
         for t, (offset, n) in zip(tab, rows):
-            t.offset, t.n = offset, n
+            t.fill(offset, n)
         handle = C.c_void_p()
         iwp._check(iwp.load().iwp_tensors_create(tab, len(rows), C.byref(handle)), "iwp_tensors_create")
         self._h, self._address = handle, handle.value

@@ -26,9 +26,21 @@ class IwpError(RuntimeError):
         super().__init__(what)
 
 
+def _u32(x) -> int:
+    """What an unsigned 32-bit field takes for x: the largest value for one that it cannot hold, which ctypes would cut to its low bits
+    and the library then might accept."""
+    x = int(x)
+    return x if 0 <= x <= 0xFFFFFFFF else 0xFFFFFFFF
+
+
 class Layer(C.Structure):
     _fields_ = [("offset", C.c_int64), ("n", C.c_uint32), ("k", C.c_uint32),
                 ("out_offset", C.c_uint32), ("pad", C.c_uint32)]
+
+    def fill(self, offset, n, k=0, out_offset=0):
+        """Numbers that the fields cannot hold become ones that no table may have."""
+        self.offset = min(max(int(offset), -1), 1 << 62)
+        self.n, self.k, self.out_offset, self.pad = _u32(n), _u32(k), _u32(out_offset), 0
 
 
 _lib = None
@@ -225,7 +237,7 @@ class Plan:
         rows = list(rows)
         tab = (Layer * max(1, len(rows)))()
         for t, (off, n, k, oo) in zip(tab, rows):
-            t.offset, t.n, t.k, t.out_offset, t.pad = int(off), int(n), int(k), int(oo), 0
+            t.fill(off, n, k, oo)
         handle = _vp()
         _check(load().iwp_plan_create(tab, len(rows), C.byref(handle)), "iwp_plan_create")
         self._h = handle
