@@ -7,7 +7,8 @@
 // each, two workers) 17.4 -> 9.9 us; the first pass on a new state 10 to 40 us less, whatever its size.
 //
 // The converters follow from the functions' types: a pointer takes a tensor (on the device and contiguous), an address or
-// None; a pointer to pointers a sequence of those; numbers what ctypes took.
+// None; a pointer to pointers a sequence of those; numbers what ctypes took, but one that 32 bits do not hold becomes their largest
+// value, which the library turns away, where its low bits might be a size that it takes.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -92,7 +93,15 @@ template <class T> bool unsigned_from(PyObject* o, T* out) {
 }
 template <> struct Arg<uint32_t> {
     uint32_t x = 0;
-    bool from(PyObject* o) { return unsigned_from(o, &x); }
+    bool from(PyObject* o) {
+        PyObject* i = PyNumber_Index(o);
+        if (!i) return false;
+        int beyond = 0;
+        const long long v = PyLong_AsLongLongAndOverflow(i, &beyond);
+        Py_DECREF(i);
+        x = beyond || v < 0 || v > (long long)UINT32_MAX ? UINT32_MAX : (uint32_t)v;
+        return !PyErr_Occurred();
+    }
     uint32_t get() { return x; }
 };
 template <> struct Arg<uint64_t> {

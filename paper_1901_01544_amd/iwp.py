@@ -9,6 +9,7 @@ eager fallback behind these calls.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 from typing import Optional, Sequence
 
@@ -31,6 +32,14 @@ def _u32(x) -> int:
     and the library then might accept."""
     x = int(x)
     return x if 0 <= x <= 0xFFFFFFFF else 0xFFFFFFFF
+
+
+class _U32:
+    """Unsigned 32-bit argument of a call by ctypes, see _u32."""
+
+    @classmethod
+    def from_param(cls, x):
+        return x if isinstance(x, C.c_uint32) else C.c_uint32(_u32(operator.index(x)))
 
 
 class Layer(C.Structure):
@@ -71,68 +80,68 @@ def load() -> C.CDLL:
     call.bind_losses({name: C.cast(getattr(L, name), _vp).value for name in call.loss_names()})
     call.bind_layers({name: C.cast(getattr(L, name), _vp).value for name in call.layer_names()})
     # prototypes of every call, also of those that go through _call: for callers that use the library by ctypes
-    L.iwp_workspace_bytes.argtypes = [C.c_uint32, C.c_uint32]
+    L.iwp_workspace_bytes.argtypes = [_U32, _U32]
     L.iwp_workspace_bytes.restype = C.c_size_t
-    L.compress_layer.argtypes = [_vp, _vp, _vp, C.c_uint32, C.c_uint32, C.c_float, _vp, _vp, _vp, C.c_size_t, _vp]
-    L.select_threshold.argtypes = [_vp, _vp, C.c_uint32, C.c_uint32, C.c_float, _vp, _vp, C.c_size_t, _vp]
-    L.compact_pairs.argtypes = [_vp, _vp, C.c_uint32, C.c_float, _vp, C.c_uint32, _vp, _vp, _vp, C.c_size_t, _vp]
-    L.gather_sum_at_indices.argtypes = [C.POINTER(_vp), C.c_uint32, _vp, C.c_uint32, _vp, _vp]
-    L.apply_sparse_update.argtypes = [_vp, _vp, _vp, C.c_uint32, C.c_float, C.POINTER(_vp), C.c_uint32, _vp]
-    L.iwp_plan_create.argtypes = [C.POINTER(Layer), C.c_uint32, C.POINTER(_vp)]
+    L.compress_layer.argtypes = [_vp, _vp, _vp, _U32, _U32, C.c_float, _vp, _vp, _vp, C.c_size_t, _vp]
+    L.select_threshold.argtypes = [_vp, _vp, _U32, _U32, C.c_float, _vp, _vp, C.c_size_t, _vp]
+    L.compact_pairs.argtypes = [_vp, _vp, _U32, C.c_float, _vp, _U32, _vp, _vp, _vp, C.c_size_t, _vp]
+    L.gather_sum_at_indices.argtypes = [C.POINTER(_vp), _U32, _vp, _U32, _vp, _vp]
+    L.apply_sparse_update.argtypes = [_vp, _vp, _vp, _U32, C.c_float, C.POINTER(_vp), _U32, _vp]
+    L.iwp_plan_create.argtypes = [C.POINTER(Layer), _U32, C.POINTER(_vp)]
     L.iwp_plan_destroy.argtypes = [_vp]
     L.iwp_plan_destroy.restype = None
     L.iwp_plan_workspace_bytes.argtypes = [_vp]
     L.iwp_plan_workspace_bytes.restype = C.c_size_t
-    L.iwp_plan_step_workspace_bytes.argtypes = [_vp, C.c_uint32]
+    L.iwp_plan_step_workspace_bytes.argtypes = [_vp, _U32]
     L.iwp_plan_step_workspace_bytes.restype = C.c_size_t
-    L.iwp_step_segmented.argtypes = [_vp, _vp, C.POINTER(_vp), C.POINTER(_vp), C.c_uint32, _vp, _vp, C.c_float,
+    L.iwp_step_segmented.argtypes = [_vp, _vp, C.POINTER(_vp), C.POINTER(_vp), _U32, _vp, _vp, C.c_float,
                                      C.c_float, _vp, _vp, _vp, _vp, _vp, C.c_size_t, _vp]
     L.iwp_step_segmented.restype = C.c_int
     L.iwp_plan_set_momentum.argtypes = [_vp, C.c_float]
     L.iwp_plan_set_momentum.restype = C.c_int
     L.iwp_plan_mask_bytes.argtypes = [_vp]
     L.iwp_plan_mask_bytes.restype = C.c_size_t
-    L.iwp_plan_threshold_workspace_bytes.argtypes = [_vp, C.c_uint32, C.c_uint32, C.c_uint32]
+    L.iwp_plan_threshold_workspace_bytes.argtypes = [_vp, _U32, _U32, _U32]
     L.iwp_plan_threshold_workspace_bytes.restype = C.c_size_t
-    L.iwp_step_threshold_segmented.argtypes = [_vp, _vp, C.POINTER(_vp), C.POINTER(_vp), C.c_uint32, _vp, C.c_uint32,
-                                               _vp, C.c_float, C.c_float, _vp, _vp, _vp, _vp, C.c_uint32, _vp,
+    L.iwp_step_threshold_segmented.argtypes = [_vp, _vp, C.POINTER(_vp), C.POINTER(_vp), _U32, _vp, _U32,
+                                               _vp, C.c_float, C.c_float, _vp, _vp, _vp, _vp, _U32, _vp,
                                                C.c_size_t, _vp]
     L.iwp_step_threshold_segmented.restype = C.c_int
-    L.iwp_step_threshold_random_segmented.argtypes = [_vp, _vp, C.POINTER(_vp), C.POINTER(_vp), C.c_uint32, _vp,
-                                                      C.c_uint32, _vp, C.c_uint64, C.c_uint64, C.c_float, C.c_float,
-                                                      _vp, _vp, _vp, _vp, C.c_uint32, _vp, C.c_size_t, _vp]
+    L.iwp_step_threshold_random_segmented.argtypes = [_vp, _vp, C.POINTER(_vp), C.POINTER(_vp), _U32, _vp,
+                                                      _U32, _vp, C.c_uint64, C.c_uint64, C.c_float, C.c_float,
+                                                      _vp, _vp, _vp, _vp, _U32, _vp, C.c_size_t, _vp]
     L.iwp_step_threshold_random_segmented.restype = C.c_int
-    L.iwp_step_layerwise_segmented.argtypes = [_vp, _vp, C.POINTER(_vp), C.POINTER(_vp), C.c_uint32, _vp, C.c_uint32,
+    L.iwp_step_layerwise_segmented.argtypes = [_vp, _vp, C.POINTER(_vp), C.POINTER(_vp), _U32, _vp, _U32,
                                                C.c_double, C.c_double, C.c_double, C.c_float, C.c_float, _vp, _vp,
-                                               _vp, _vp, _vp, _vp, C.c_uint32, _vp, C.c_size_t, _vp]
+                                               _vp, _vp, _vp, _vp, _U32, _vp, C.c_size_t, _vp]
     L.iwp_step_layerwise_segmented.restype = C.c_int
     L.iwp_plan_total_pairs.argtypes = [_vp]
     L.iwp_plan_total_pairs.restype = C.c_uint64
-    L.compress_segmented.argtypes = [_vp, _vp, C.POINTER(_vp), C.POINTER(_vp), C.c_uint32, _vp, _vp, C.c_float,
+    L.compress_segmented.argtypes = [_vp, _vp, C.POINTER(_vp), C.POINTER(_vp), _U32, _vp, _vp, C.c_float,
                                      _vp, _vp, _vp, _vp, C.c_size_t, _vp]
-    L.compress_segmented_static.argtypes = [_vp, _vp, C.POINTER(_vp), C.POINTER(_vp), C.c_uint32, _vp, _vp, C.c_float,
+    L.compress_segmented_static.argtypes = [_vp, _vp, C.POINTER(_vp), C.POINTER(_vp), _U32, _vp, _vp, C.c_float,
                                             _vp, _vp, _vp, _vp]
     L.compress_segmented_static.restype = C.c_int
     L.select_threshold_segmented.argtypes = [_vp, _vp, _vp, C.c_float, _vp, _vp, C.c_size_t, _vp]
     L.compact_pairs_segmented.argtypes = [_vp, _vp, _vp, C.c_float, _vp, _vp, _vp, _vp, C.c_size_t, _vp]
-    L.iwp_score_keys.argtypes = [_vp, _vp, C.c_uint32, C.c_float, _vp, _vp]
+    L.iwp_score_keys.argtypes = [_vp, _vp, _U32, C.c_float, _vp, _vp]
     L.iwp_copy_f32.argtypes = [_vp, _vp, C.c_uint64, _vp]
     L.iwp_copy_f32.restype = C.c_int
-    L.iwp_timing_enable.argtypes = [C.c_char_p, C.c_uint32]
+    L.iwp_timing_enable.argtypes = [C.c_char_p, _U32]
     L.iwp_timing_enable.restype = C.c_int
     L.iwp_timing_collect.argtypes = [C.POINTER(C.c_double), C.POINTER(C.c_uint32)]
     L.iwp_timing_collect.restype = C.c_int
-    L.iwp_head_workspace_bytes.argtypes = [C.c_uint32] * 4 + [_vp, C.c_int64, C.c_uint32, C.c_uint32]
+    L.iwp_head_workspace_bytes.argtypes = [_U32] * 4 + [_vp, C.c_int64, _U32, _U32]
     L.iwp_head_workspace_bytes.restype = C.c_size_t
-    L.iwp_balance_workspace_bytes.argtypes = [C.c_uint32, C.c_uint32]
+    L.iwp_balance_workspace_bytes.argtypes = [_U32, _U32]
     L.iwp_balance_workspace_bytes.restype = C.c_size_t
-    L.iwp_expert_product_workspace_bytes.argtypes = [C.c_uint32] * 6 + [_vp, C.c_int64, C.c_int64, C.c_uint32, C.c_uint32]
+    L.iwp_expert_product_workspace_bytes.argtypes = [_U32] * 6 + [_vp, C.c_int64, C.c_int64, _U32, _U32]
     L.iwp_expert_product_workspace_bytes.restype = C.c_size_t
-    L.iwp_tensors_create.argtypes = [C.POINTER(Layer), C.c_uint32, C.POINTER(_vp)]
+    L.iwp_tensors_create.argtypes = [C.POINTER(Layer), _U32, C.POINTER(_vp)]
     L.iwp_tensors_create.restype = C.c_int
     L.iwp_tensors_destroy.argtypes = [_vp]
     L.iwp_tensors_destroy.restype = None
-    L.iwp_tensors_workspace_bytes.argtypes = [_vp, C.c_uint32]
+    L.iwp_tensors_workspace_bytes.argtypes = [_vp, _U32]
     L.iwp_tensors_workspace_bytes.restype = C.c_size_t
     L.iwp_strerror.argtypes = [C.c_int]
     L.iwp_strerror.restype = C.c_char_p
