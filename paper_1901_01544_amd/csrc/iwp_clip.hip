@@ -108,11 +108,12 @@ __device__ __forceinline__ double workgroup_sum(double s) {
     return all;
 }
 
-// What a gradient is multiplied by; its norm.
+// What a gradient is multiplied by; its norm.  Where it is clipped, the scale is left out of quotient and product alike: the norm with it may lie above
+// binary64.
 __device__ __forceinline__ double factor(const ClipCall& c, double square, float* norm) {
-    const double n = fabs(c.scale) * sqrt(square);
+    const double root = sqrt(square), n = fabs(c.scale) * root;
     *norm = (float)n;
-    return c.scale * (n <= c.max_norm ? 1.0 : c.max_norm / n);
+    return n <= c.max_norm ? c.scale : copysign(c.max_norm / root, c.scale);
 }
 
 // A wavefront's chunks of a product.  The last chunks first: they are what the memory-side cache still has of the pass for the norm.  The first
