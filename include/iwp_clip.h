@@ -33,7 +33,8 @@ size_t iwp_tensors_workspace_bytes(const iwp_tensors* tensors, uint32_t W);
  *   out[p][i] = g[p][i] * (scale * min(1, max_norm / norm[p]))
  * The squares and their sum are binary64 (no gradient over- or underflows them), and so is the product, which is rounded once; norm is
  * rounded to binary32 (infinite where it lies above).  A norm of 0 leaves 0; a NaN among the gradients makes the norm and all of out NaN; an
- * infinity makes the norm infinite, what is infinite NaN and everything else 0.  So norm tells whether the step is to be taken.
+ * infinity makes the norm infinite, what is infinite NaN and everything else 0, unless max_norm is INFINITY too: then nothing is clipped, the infinity
+ * stays one and everything else is scaled.  So norm tells whether the step is to be taken.
  * g: host array of W device pointers to flat buffers, NULL for a worker without a gradient (norm 0, nothing written).  out: host array
  * of W device pointers, out[p] may be g[p] (then a gradient that stays as it is is not written), NULL there or as a whole: the norm alone.  norm:
  * device array of W binary32.  max_norm: INFINITY to scale alone.

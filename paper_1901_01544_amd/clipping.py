@@ -60,7 +60,8 @@ def clip(tensors: Tensors, g: Sequence, out: Optional[Sequence], norm, workspace
          stream=None):
     """norm[p] = |scale| * norm of g[p] over all tensors; out[p] = g[p] * (scale * min(1, max_norm / norm[p])).
 
-    g: one flat buffer a worker, None for a worker without a gradient.  out: likewise, out[p] may be g[p]; None: norms alone.  norm: [W].
+    g: one flat buffer a worker, None for a worker without a gradient.  out: likewise, out[p] may be g[p]; None: norms alone.  norm: [W].  max_norm: inf
+    scales alone, with an infinite norm too.
     workspace: ``tensors.workspace_bytes(W)`` bytes."""
     W = len(g)
     out = [None] * W if out is None else out

@@ -34,6 +34,34 @@ def test_norms_beyond_binary64(clipping, n, scale):
     assert ((out.double() - want).abs() <= 1.01 * HALF * want.abs() + 2.0 ** -150).all()
 
 
+@SIZES
+@pytest.mark.parametrize("onto", [False, True], ids=["apart", "in place"])
+def test_infinity_and_nan_without_a_largest_norm(clipping, n, onto):
+    """max_norm = inf scales alone: an infinity stays one, the rest is scaled, the norm tells.  A NaN makes all of it NaN."""
+    for scale in (1.0, -0.25):
+        g = [torch.full((n,), 3.0, device=DEV) for _ in range(3)]
+        g[0][n // 2], g[1][n - 1] = float("inf"), float("nan")
+        out = g if onto else [torch.empty_like(x) for x in g]
+        norm = call(clipping, [(0, n)], g, out, scale=scale)
+        assert norm[0].item() == float("inf") and norm[1].isnan()
+        want = torch.full((n,), 3.0 * scale, device=DEV)
+        assert torch.equal(out[2], want)
+        want[n // 2] = float("inf") * scale
+        assert torch.equal(out[0], want)
+        assert out[1].isnan().all()
+
+
+def test_norms_alone_of_workers_beyond_the_cache(clipping):
+    """Norms alone take a grid of their own; every worker's against its own, the quiet one's too."""
+    rows = [(0, 20_000_001), (20_000_100, 25_000_003)]
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    g = [size * torch.randn(45_000_103, generator=gen, device=DEV) for size in (1.0, 2.0, 4e-3)]
+    norm = call(clipping, rows, g, None, max_norm=100.0)
+    for p, x in enumerate(g):
+        want = sum(x[o:o + n].double().square().sum() for o, n in rows).sqrt()
+        assert abs(norm[p].double() - want) <= 1.01 * HALF * want, p
+
+
 def test_workers_that_32_bits_do_not_hold(clipping):
     tensors = clipping.Tensors([(0, 10)])
     for W in (0, -1, 33, 2 ** 32 + 1):
