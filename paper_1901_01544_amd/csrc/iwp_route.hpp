@@ -498,104 +498,101 @@ __global__ void __launch_bounds__(256) k_route_gradient(RouteGradient r) {
     f32_bytes* row = reinterpret_cast<f32_bytes*>(shared) + (size_t)mine * units;
     SlotGradient* slot = reinterpret_cast<SlotGradient*>(shared + (size_t)tokens * units * sizeof(float)) + (size_t)mine * r.slots;
     const bool dense = !r.sigmoid && !r.renormalise;
-    for (uint32_t base = blockIdx.x * tokens; base < r.tokens; base += gridDim.x * tokens) {
-        const uint32_t i = base + mine;
-        bool in = i < r.tokens && !(r.keep && !r.keep[i]);
-        float y[L::N], by = 0.0f, m = -INFINITY, log_sum;
+    const uint32_t i = blockIdx.x * tokens + mine;
+    bool in = i < r.tokens && !(r.keep && !r.keep[i]);
+    float y[L::N], by = 0.0f, m = -INFINITY, log_sum;
 #pragma unroll
-        for (int v = 0; v < L::N; ++v) y[v] = 0.0f;
-        if (dense) {
-            words4 raw[CHUNKS] = {};
-            if (in) l.load(r.x, (int64_t)i * r.ld, raw);
-            L::unpack(raw, y);
-#pragma unroll
-            for (int v = 0; v < L::N; ++v) {
-                if (l.expert(v) >= r.experts) y[v] = -INFINITY;
-                m = fmaxf(m, y[v]);
-            }
-            m = part.max(m);
-            in = l.softmax(y, &by, &log_sum) && in;
-        }
-        auto expert_of = [&](uint32_t k) { return in ? (uint32_t)r.chosen[(size_t)i * r.slots + k] : 0xffffffffu; };
-        auto logit_of = [&](uint32_t e) { return element<IN>(r.x, (int64_t)i * r.ld + e); };
-        if (r.renormalise) {
-            for (uint32_t k = l.lane; k < r.slots; k += r.lanes) {
-                const uint32_t e = expert_of(k);
-                if (e < r.experts) m = fmaxf(m, r.sigmoid ? fminf(logit_of(e), 0.0f) : logit_of(e));
-            }
-            m = part.max(m);
-        }
-        // every slot's part: its dweight times the scale, and what the sums take
-        auto value_of = [&](float x) {
-            return r.sigmoid ? sigmoid_over(x, r.renormalise ? m : 0.0f) : r.renormalise ? expf(x - m) : exp_raised(x - m) * by;
-        };
-        float all = 0.0f, inner = 0.0f;
-        for (uint32_t k = l.lane; k < r.slots; k += r.lanes) {
-            const uint32_t e = expert_of(k);
-            if (e >= r.experts) continue;
-            const float q = value_of(logit_of(e));
-            all += q;
-            inner += q * r.dweight[(size_t)i * r.slots + k];
-        }
-        inner = part.sum(inner);
-        if (r.renormalise) {
-            all = part.sum(all);
-            inner = inner / all;
-        }
-        for (uint32_t k = l.lane; k < r.slots; k += r.lanes) {
-            const uint32_t e = expert_of(k);
-            float d = 0.0f;
-            if (e < r.experts) {
-                const float x = logit_of(e), dw = r.dweight[(size_t)i * r.slots + k];
-                d = dense ? dw : r.renormalise ? value_of(x) / all * (dw - inner) : value_of(x) * dw;
-                if (r.sigmoid) d *= sigmoid_over(-x, 0.0f);
-                d *= r.scale;
-            }
-            slot[k] = SlotGradient{e, d};
-        }
-        // by expert: the slots' parts in their order, so that the sum of an expert's is the same every time
-#pragma unroll
-        for (int v = 0; v < L::N; v += 4)
-            if (l.expert(v) < units) *reinterpret_cast<f32x4_bytes*>(row + l.expert(v)) = f32x4{};
-        lanes_exchange();
-        for (uint32_t k = l.lane; k < r.slots; k += r.lanes) {
-            const SlotGradient s = slot[k];
-            if (s.expert >= r.experts) continue;
-            bool first = true;
-            float sum = s.d;
-            for (uint32_t o = 0; o < r.slots; ++o) {
-                if (o == k || slot[o].expert != s.expert) continue;
-                first &= o > k;
-                sum += slot[o].d;
-            }
-            if (first) row[s.expert] = sum;
-        }
-        lanes_exchange();
-        float d[L::N];
-#pragma unroll
-        for (int v = 0; v < L::N; v += 4) {
-            f32x4 four = {};
-            if (l.expert(v) < units) four = *reinterpret_cast<const f32x4_bytes*>(row + l.expert(v));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) d[v + e] = four[e];
-        }
-        lanes_exchange();
-        if (i >= r.tokens) continue;
-        float plus[L::N];
-#pragma unroll
-        for (int v = 0; v < L::N; ++v) plus[v] = 0.0f;
-        if (r.plus) {
-            words4 raw[CHUNKS];
-            l.load(r.plus, (int64_t)i * r.ld_plus, raw);
-            L::unpack(raw, plus);
-        }
+    for (int v = 0; v < L::N; ++v) y[v] = 0.0f;
+    if (dense) {
+        words4 raw[CHUNKS] = {};
+        if (in) l.load(r.x, (int64_t)i * r.ld, raw);
+        L::unpack(raw, y);
 #pragma unroll
         for (int v = 0; v < L::N; ++v) {
-            const float g = dense ? y[v] * by * (d[v] - inner * r.scale) : d[v];
-            y[v] = in ? plus[v] + g : plus[v];
+            if (l.expert(v) >= r.experts) y[v] = -INFINITY;
+            m = fmaxf(m, y[v]);
         }
-        l.store(r.dx, (int64_t)i * r.ld_dx, y);
+        m = part.max(m);
+        in = l.softmax(y, &by, &log_sum) && in;
     }
+    auto expert_of = [&](uint32_t k) { return in ? (uint32_t)r.chosen[(size_t)i * r.slots + k] : 0xffffffffu; };
+    auto logit_of = [&](uint32_t e) { return element<IN>(r.x, (int64_t)i * r.ld + e); };
+    if (r.renormalise) {
+        for (uint32_t k = l.lane; k < r.slots; k += r.lanes) {
+            const uint32_t e = expert_of(k);
+            if (e < r.experts) m = fmaxf(m, r.sigmoid ? fminf(logit_of(e), 0.0f) : logit_of(e));
+        }
+        m = part.max(m);
+    }
+    // every slot's part: its dweight times the scale, and what the sums take
+    auto value_of = [&](float x) {
+        return r.sigmoid ? sigmoid_over(x, r.renormalise ? m : 0.0f) : r.renormalise ? expf(x - m) : exp_raised(x - m) * by;
+    };
+    float all = 0.0f, inner = 0.0f;
+    for (uint32_t k = l.lane; k < r.slots; k += r.lanes) {
+        const uint32_t e = expert_of(k);
+        if (e >= r.experts) continue;
+        const float q = value_of(logit_of(e));
+        all += q;
+        inner += q * r.dweight[(size_t)i * r.slots + k];
+    }
+    inner = part.sum(inner);
+    if (r.renormalise) {
+        all = part.sum(all);
+        inner = inner / all;
+    }
+    for (uint32_t k = l.lane; k < r.slots; k += r.lanes) {
+        const uint32_t e = expert_of(k);
+        float d = 0.0f;
+        if (e < r.experts) {
+            const float x = logit_of(e), dw = r.dweight[(size_t)i * r.slots + k];
+            d = dense ? dw : r.renormalise ? value_of(x) / all * (dw - inner) : value_of(x) * dw;
+            if (r.sigmoid) d *= sigmoid_over(-x, 0.0f);
+            d *= r.scale;
+        }
+        slot[k] = SlotGradient{e, d};
+    }
+    // by expert: the slots' parts in their order, so that the sum of an expert's is the same every time
+#pragma unroll
+    for (int v = 0; v < L::N; v += 4)
+        if (l.expert(v) < units) *reinterpret_cast<f32x4_bytes*>(row + l.expert(v)) = f32x4{};
+    lanes_exchange();
+    for (uint32_t k = l.lane; k < r.slots; k += r.lanes) {
+        const SlotGradient s = slot[k];
+        if (s.expert >= r.experts) continue;
+        bool first = true;
+        float sum = s.d;
+        for (uint32_t o = 0; o < r.slots; ++o) {
+            if (o == k || slot[o].expert != s.expert) continue;
+            first &= o > k;
+            sum += slot[o].d;
+        }
+        if (first) row[s.expert] = sum;
+    }
+    lanes_exchange();
+    float d[L::N];
+#pragma unroll
+    for (int v = 0; v < L::N; v += 4) {
+        f32x4 four = {};
+        if (l.expert(v) < units) four = *reinterpret_cast<const f32x4_bytes*>(row + l.expert(v));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) d[v + e] = four[e];
+    }
+    if (i >= r.tokens) return;
+    float plus[L::N];
+#pragma unroll
+    for (int v = 0; v < L::N; ++v) plus[v] = 0.0f;
+    if (r.plus) {
+        words4 raw[CHUNKS];
+        l.load(r.plus, (int64_t)i * r.ld_plus, raw);
+        L::unpack(raw, plus);
+    }
+#pragma unroll
+    for (int v = 0; v < L::N; ++v) {
+        const float g = dense ? y[v] * by * (d[v] - inner * r.scale) : d[v];
+        y[v] = in ? plus[v] + g : plus[v];
+    }
+    l.store(r.dx, (int64_t)i * r.ld_dx, y);
 }
 
 }  // namespace iwp
