@@ -64,8 +64,9 @@ int iwp_route_gradient(const void* x, int64_t ld_x, uint32_t tokens, uint32_t ex
  *   w       [experts, out, in]: ld_w elements from row to row, step_w from matrix to matrix
  *   chosen  [tokens, slots] int32, packed, as iwp_route writes it; entries outside [0, experts) are slots that nobody got
  *   y       [tokens * slots, out]: y_r = W_chosen[r] x_r, zeros for slots of nobody
- * All of one type, sums in binary32, rounded once.  Matrices of experts without rows are not read.  An infinity or a NaN in a row, or in an
- * expert's matrix, shows in what depends on it by the definition, where an infinity may also make NaN, and nowhere else.
+ * All of one type, sums in binary32, rounded once.  Matrices of experts without rows are not read, except where w is copied (below), which takes all of
+ * it.  An infinity or a NaN in a row, or in an expert's matrix, shows in what depends on it by the definition, where an infinity may also make NaN,
+ * and nowhere else.
  * Workspace: iwp_expert_product_workspace_bytes with the same sizes, 256-byte aligned; it has room for the rows gathered by expert
  * and, where the rows of a w of 16 bits cannot be read by 16 bytes where they lie (address, ld_w, step_w and in), for a copy of w.
  * IWP_EINVAL: sizes of 0 (tokens may be 0) or above the limits (IWP_MAX_TOKENS, IWP_MAX_ROWS slots, IWP_MAX_EXPERTS, IWP_MAX_DIM for in and

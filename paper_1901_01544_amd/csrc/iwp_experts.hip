@@ -143,7 +143,9 @@ constexpr uint32_t ARRANGE_ONE = 2048, ARRANGE_SLOTS = 1024, ARRANGE_MOST = 64;
 
 // Products of few rows an expert need no arrangement.  us here and by tiles, mean rows of an expert that has any: bf16 1 token x 8 of 64 experts x 2048 x 1024
 // 10 and 33, 16 tokens 42 and 53 (2 rows), 32 x 4 of 16 x 2048 x 2048 34 and 42 (8), 64 x 4 of 16 50 and 42 (16); binary32 60 x 2 of 8 x 1024 x 1024
-// 16 and 29 (15).
+// 16 and 29 (15).  The host knows no more than the mean.  Where all rows are one expert's, its matrix is read again for every 16 of them by the few
+// workgroups that it has: 512 rows of 64 x 2048 x 1024 in bf16 126 (evenly 57; 520 rows, by tiles, 28 and 48), 128 rows 33 (40), 32 rows 10 (20); 1024 rows of
+// 64 x 1024 x 1024 in binary32 258 (90; 1025 rows, by tiles, 49 and 85).
 bool few_rows(const ProductSizes& z) {
     const uint32_t n = z.rows();
     return n <= FEW_SLOTS && n <= (z.dtype == IWP_F32 ? FEW_ROWS : FEW_ROWS / 2) * std::min(z.experts, n);

@@ -4,12 +4,14 @@
 //   groups: best one or two c of every group between the lanes that have it, a group's rank by counting;
 //   slots: the largest c that is left, one after the other, or where there are many lanes all at once (see candidates).
 // Scores decide in binary64, but are computed in binary32 first: where no two c that the choice depends on are closer than twice what
-// binary32 may be off, it is the choice.  Else the wavefront does the token again in binary64, value by value in LDS (6 of 10000 tokens of the
-// case below).
+// binary32 may be off, it is the choice.  Else the wavefront does the token again in binary64, value by value in LDS.  That is 6 of 10000 tokens of the
+// case below (81 by softmax), 71 (154) in bf16 with its biases of 81 values.  Scores that are equal are close as well: with one bias for all experts a third of
+// the tokens in bf16, 5 % in fp16, and every token of a router whose logits are all alike.
 //
-// Bound by instructions where experts are many.  131072 tokens x 256 experts in binary32, 8 slots: by logits alone 30 us, which is reading them (134 MB,
-// 4.5 TB/s); sigmoid scores with a bias 53; of 4 of 8 groups by their best two 75, some 1250 vector instructions a wavefront of four tokens.  In
-// binary64 throughout 264; slots one after the other instead of all at once 120.
+// Bound by instructions where experts are many.  131072 tokens x 256 experts in binary32, 8 slots: by logits alone 28 to 30 us, which is reading them
+// (134 MB, 4.5 TB/s); sigmoid scores with a bias 51; of 4 of 8 groups by their best two 76 to 79, 1258 vector instructions a wavefront of four tokens, which
+// the vector units issue in all cycles; without a bias 65.  In bf16 98, without a bias 70, with a bias of zeros 270 to 281; logits all alike 455.  In binary64
+// throughout 264; slots one after the other instead of all at once 120.
 #pragma once
 
 #include <hip/hip_runtime.h>
